@@ -71,6 +71,7 @@ typedef enum {
   TURNKL_ERR_TOPK_ID = -9,       /* device: a top-K support id outside [0, vocab) */
   TURNKL_ERR_OUTCOME = -10,      /* device: outcome flag not constant over a trajectory */
   TURNKL_ERR_SCRATCH = -11,      /* turnkl_fwd_bwd_noalloc: problem larger than its scratch */
+  TURNKL_ERR_TOKEN_ID = -12,     /* device: a given token's id outside [0, vocab) */
 } turnkl_status;
 
 /* Statistics of one turn index t over the supervised tokens at that turn. */
@@ -366,6 +367,63 @@ int turnkl_fwd_bwd_topk(const void* student_logits, int64_t ld_student, int dtyp
                         turnkl_turn_stat* turn_stats_out, int32_t max_turns, int accumulate_stats,
                         float* token_kl_out, const turnkl_options* options, void* workspace,
                         size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Log probabilities of given tokens, with entropy and top alternatives.  A
+ * teacher scored this way gives turnkl_fwd_bwd_topk its support (top_ids_out,
+ * top_logp_out); the sampled tokens' log probabilities and the entropy of each
+ * row (Fig. 2 plots the teacher's per turn) are what a policy term or a rollout
+ * engine needs.  For row i with logits z, M = max_v z_v and
+ * L = ln sum_v exp(z_v - M):
+ *   log p_v  = (z_v - M) - L,
+ *   logp_i   = log p_t at the given token t = token_ids[i],
+ *   H_i      = L - sum_v p_v (z_v - M)      (entropy, in nats),
+ *   top      = the K largest logits in descending order, the lower id first
+ *              among equal ones (-0 and +0 are equal), with their log p.
+ * A logit of -inf is a forbidden token: log p = -inf, and it adds nothing to H.
+ * A row of which every logit is -inf has M = -inf, L = 0, H = 0 and
+ * log p = -inf throughout.  A row that holds +inf or NaN has NaN in L, H and
+ * every log p; its top ids then rank NaN as -inf.
+ * ------------------------------------------------------------------------ */
+
+/* The most alternatives of one row. */
+#define TURNKL_MAX_ALTERNATIVES 128
+
+/*
+ * Bytes of device workspace turnkl_token_logprobs needs (host; a pure function
+ * of its arguments), 0 when they are invalid (n_tokens < 0, vocab < 1 or above
+ * 2^24, k outside 0 .. min(TURNKL_MAX_ALTERNATIVES, vocab)).  The workspace
+ * needs no initialisation; it must be 256-byte aligned.
+ */
+size_t turnkl_token_logprobs_workspace_bytes(int64_t n_tokens, int64_t vocab, int32_t k);
+
+/*
+ * logits         [n_tokens x vocab] of `dtype`, row stride ld (elements, >= vocab),
+ *                rows of any start.
+ * token_ids      [n_tokens] the given tokens, or NULL (then logp_out must be NULL).
+ *                An id outside [0, vocab) in a row that is asked for makes logp_out
+ *                NaN there and is recorded as TURNKL_ERR_TOKEN_ID; every other
+ *                output is as specified.
+ * mask           [n_tokens] nonzero: the row is asked for; NULL: every row is.
+ *                Rows not asked for are never read: logp 0, H 0, log_z NaN, top ids
+ *                -1 with log p -inf.
+ * k              alternatives of a row, 0 .. min(TURNKL_MAX_ALTERNATIVES, vocab).
+ * logp_out       [n_tokens] float, or NULL.
+ * entropy_out    [n_tokens] float, or NULL.
+ * log_z_out      [n_tokens x 2] float (M, L), or NULL: the log-partition function
+ *                as a sum of two floats, as turnkl_token_logprobs_bwd takes it.
+ * top_ids_out    int32 [n_tokens][ld_top], top_logp_out float [n_tokens][ld_top]:
+ *                the alternatives (ld_top >= k); both NULL when k = 0.
+ * No output may overlap an input or another output (TURNKL_ERR_ALIAS).  Sizes
+ * above 2^31 - 1 rows or row strides are TURNKL_ERR_INVALID_ARG.  The device-side
+ * status is read with turnkl_get_status (of several bad ids the first row's
+ * decides).
+ */
+int turnkl_token_logprobs(const void* logits, int64_t ld, int dtype, int64_t n_tokens,
+                          int64_t vocab, const int32_t* token_ids, const uint8_t* mask, int32_t k,
+                          float* logp_out, float* entropy_out, float* log_z_out,
+                          int32_t* top_ids_out, float* top_logp_out, int64_t ld_top,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Adaptive rollout-depth controller (Sec. 5.1; App. D, Algorithm 1 and the

@@ -5,7 +5,6 @@
 #include <math.h>
 #include <string.h>
 
-#include <initializer_list>
 #include <mutex>
 
 #include "turnkl_internal.h"
@@ -199,28 +198,6 @@ int workspace_chunks(long long vocab, int dtype, bool aligned_rows, int vpt) {
 
 size_t workspace_bytes_for(int64_t n_tokens, int64_t vocab, int dtype, int32_t max_turns,
                            int aligned_rows, int vpt);
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const char* pa = static_cast<const char*>(a);
-  const char* pb = static_cast<const char*>(b);
-  return pa < pb + nb && pb < pa + na;
-}
-
-size_t matrix_bytes(long long rows, long long ld, long long vocab, size_t es) {
-  return rows > 0 ? (size_t)((rows - 1) * ld + vocab) * es : 0;
-}
-
-// A byte range of a caller buffer (p may be null: no range).
-struct Region {
-  const void* p;
-  size_t n;
-};
-
-bool overlaps_any(const void* p, size_t n, std::initializer_list<Region> rs) {
-  for (const Region& r : rs)
-    if (r.p && r.n && overlaps(p, n, r.p, r.n)) return true;
-  return false;
-}
 
 // What the options add to a call besides the segment parameters.
 struct Extras {
@@ -682,6 +659,7 @@ const char* turnkl_status_string(int status) {
     case TURNKL_ERR_OUTCOME: return "outcome flag not constant over a trajectory";
     case TURNKL_ERR_SCRATCH:
       return "problem larger than the built-in scratch of turnkl_fwd_bwd_noalloc";
+    case TURNKL_ERR_TOKEN_ID: return "a given token's id outside [0, vocab)";
     default: return "unknown status";
   }
 }

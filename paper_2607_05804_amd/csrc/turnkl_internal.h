@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "turnkl.h"
 
 namespace turnkl {
@@ -22,6 +24,7 @@ enum : unsigned {
   kPrioTimeout = 3,
   kPrioTopkId = 4,  // top-K path: a support id outside [0, vocab)
   kPrioOutcome = 5,  // outcome flag not constant over a trajectory
+  kPrioTokenId = 6,  // a given token's id outside [0, vocab)
 };
 
 __host__ __device__ inline unsigned long long err_key(long long pos, unsigned prio) {
@@ -36,8 +39,34 @@ __host__ __device__ inline int status_from_key(unsigned long long key) {
     case kPrioUnsorted: return TURNKL_ERR_UNSORTED;
     case kPrioTopkId: return TURNKL_ERR_TOPK_ID;
     case kPrioOutcome: return TURNKL_ERR_OUTCOME;
+    case kPrioTokenId: return TURNKL_ERR_TOKEN_ID;
     default: return TURNKL_ERR_SYNC_TIMEOUT;
   }
+}
+
+// ---------------------------------------------------------------------------
+// byte ranges of caller buffers (host)
+
+inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  const char* pa = static_cast<const char*>(a);
+  const char* pb = static_cast<const char*>(b);
+  return pa < pb + nb && pb < pa + na;
+}
+
+inline size_t matrix_bytes(long long rows, long long ld, long long vocab, size_t es) {
+  return rows > 0 ? (size_t)((rows - 1) * ld + vocab) * es : 0;
+}
+
+// A byte range of a caller buffer (p may be null: no range).
+struct Region {
+  const void* p;
+  size_t n;
+};
+
+inline bool overlaps_any(const void* p, size_t n, std::initializer_list<Region> rs) {
+  for (const Region& r : rs)
+    if (r.p && r.n && overlaps(p, n, r.p, r.n)) return true;
+  return false;
 }
 
 // ---------------------------------------------------------------------------
@@ -345,6 +374,38 @@ constexpr int kMaxTopK = 1024;
 hipError_t launch_topk_rows(const TopkParams& p, hipStream_t s);
 hipError_t launch_topk_fill(const TopkParams& p, hipStream_t s);
 hipError_t launch_topk_scatter(const TopkParams& p, hipStream_t s);
+
+// Token log probabilities (logprobs.hip).  A row is cut into n_chunks chunks of
+// packs (chunk_start); with more than one, every chunk leaves its partial sums and
+// its own top k in the workspace, and a second kernel joins them.
+struct LogprobParams {
+  const void* z;
+  const int* ids;             // given tokens, or null
+  const unsigned char* mask;  // or null: every row
+  float* logp;                // or null, like the next two
+  float* entropy;
+  float* log_z;
+  int* top_ids;
+  float* top_logp;
+  Header* hdr;
+  float* part;                // [n_rows][n_chunks][kLogprobPart]
+  unsigned long long* cand;   // [n_rows][n_chunks][k]
+  long long ld;
+  long long ld_top;
+  int n_rows;
+  int vocab;
+  int k;
+  int n_chunks;
+  int bf16;
+  int ragged;  // rows of any start and length (else whole aligned packs)
+};
+
+constexpr int kMaxAlternatives = TURNKL_MAX_ALTERNATIVES;
+constexpr int kLogprobPart = 4;             // maximum, S, A, unused
+constexpr int kMaxLogprobVocab = 1 << 24;
+
+int logprob_chunks(long long n_rows, long long vocab);
+hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s);
 
 // status_out: optional device int32 that receives the call's status
 // (TURNKL_OK or the device-detected error) once the loss is written.

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import threading
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -29,6 +30,7 @@ ERR_SYNC_TIMEOUT = -8
 ERR_TOPK_ID = -9
 ERR_OUTCOME = -10
 ERR_SCRATCH = -11
+ERR_TOKEN_ID = -12
 
 # Size of the scratch array of turnkl_fwd_bwd_noalloc (TURNKL_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -36,13 +38,17 @@ NOALLOC_SCRATCH_BYTES = 32 << 20
 BF16 = 0
 F32 = 1
 
+# The most alternatives of one row (TURNKL_MAX_ALTERNATIVES).
+MAX_ALTERNATIVES = 128
+
 # Names of every entry point include/turnkl.h declares.
 EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
            "turnkl_get_status", "turnkl_get_segments", "turnkl_alpha_schedule",
            "turnkl_status_string", "turnkl_topk_workspace_bytes", "turnkl_fwd_bwd_topk",
            "turnkl_depth_default_config", "turnkl_depth_init", "turnkl_depth_plan",
            "turnkl_depth_update", "turnkl_loss_share", "turnkl_budget_report",
-           "turnkl_outcome_gap")
+           "turnkl_outcome_gap", "turnkl_token_logprobs_workspace_bytes",
+           "turnkl_token_logprobs")
 # ... and every entry point include/turnkl_testing.h declares (measurement and
 # test hooks).
 TESTING_EXPORTS = ("turnkl_profile_row_kernel", "turnkl_set_row_tiling",
@@ -162,6 +168,13 @@ def lib() -> ctypes.CDLL:
                                            c.POINTER(Budget)]
         l.turnkl_outcome_gap.restype = c.c_int
         l.turnkl_outcome_gap.argtypes = [c.c_void_p, c.c_int32, c.c_void_p]
+        l.turnkl_token_logprobs_workspace_bytes.restype = c.c_size_t
+        l.turnkl_token_logprobs_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32]
+        l.turnkl_token_logprobs.restype = c.c_int
+        l.turnkl_token_logprobs.argtypes = [
+            c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int32,
+            c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p,
+            c.c_size_t, c.c_void_p]
         _lib = l
     return _lib
 
@@ -544,6 +557,101 @@ def fwd_bwd_topk(student: torch.Tensor, teacher_ids: torch.Tensor, teacher_vals:
         if st != OK:
             raise TurnKLError(st, "turnkl_fwd_bwd_topk (device)")
     return loss, grad_t, gk, turn_stats, kl_t, workspace
+
+
+class TokenLogprobs(NamedTuple):
+    """Outputs of token_logprobs, one entry per row (None: not asked for)."""
+    logp: torch.Tensor | None      # float32 [N], log p of the given token
+    entropy: torch.Tensor | None   # float32 [N]
+    log_z: torch.Tensor | None     # float32 [N, 2], (M, L): log-partition function M + L
+    top_ids: torch.Tensor | None   # int32 [N, k]
+    top_logp: torch.Tensor | None  # float32 [N, k]
+
+
+def new_token_logprobs(n_tokens: int, k: int = 0, device="cuda", logp: bool = True) -> TokenLogprobs:
+    """Output buffers for token_logprobs (logp=False: no tokens are given)."""
+    f = dict(dtype=torch.float32, device=device)
+    return TokenLogprobs(
+        torch.empty(n_tokens, **f) if logp else None, torch.empty(n_tokens, **f),
+        torch.empty((n_tokens, 2), **f),
+        torch.empty((n_tokens, k), dtype=torch.int32, device=device) if k else None,
+        torch.empty((n_tokens, k), **f) if k else None)
+
+
+class LogprobsWorkspace(Workspace):
+    """Caller-owned device scratch for turnkl_token_logprobs."""
+
+    def __init__(self, n_tokens: int, vocab: int, k: int = 0, device="cuda"):
+        nbytes = int(lib().turnkl_token_logprobs_workspace_bytes(n_tokens, vocab, k))
+        if nbytes == 0:
+            raise TurnKLError(ERR_INVALID_ARG, "turnkl_token_logprobs_workspace_bytes")
+        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.nbytes = nbytes
+        self.n_tokens = n_tokens
+
+
+def _check_token_rows(logits, token_ids, mask):
+    """dtype code, n_tokens and vocab of a call on rows of logits, after checking
+    the given tokens and the mask against them."""
+    dt = _dtype_code(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits must be 2-D with unit column stride")
+    n, v = int(logits.shape[0]), int(logits.shape[1])
+    for t, dtype, name in ((token_ids, torch.int32, "token_ids"), (mask, torch.uint8, "mask")):
+        if t is None:
+            continue
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} with one entry per row")
+        if t.device != logits.device:
+            raise ValueError(f"{name} must be on {logits.device}, not {t.device}")
+    return dt, n, v
+
+
+def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, *, k: int = 0,
+                   mask: torch.Tensor | None = None, out: TokenLogprobs | None = None,
+                   workspace: LogprobsWorkspace | None = None, check: bool = True) -> TokenLogprobs:
+    """turnkl_token_logprobs on the current stream: log p of the given tokens, each
+    row's entropy and log-partition function, and its k largest logits' ids and
+    log p (descending; the lower id first among equal logits).
+
+    logits: [N, V] bf16 or float32 of any row stride; token_ids: int32 [N] or
+    None; mask: uint8 [N] or None (rows with 0 are not read: logp and entropy 0,
+    log_z NaN, ids -1); out: buffers to write (new_token_logprobs), of which any
+    but the alternatives may be None; check: read the device status once at the
+    end and raise on an id outside [0, V).  Returns out.
+    """
+    dt, n, v = _check_token_rows(logits, token_ids, mask)
+    dev = logits.device
+    if not 0 <= k <= min(MAX_ALTERNATIVES, v):
+        raise ValueError(f"k must be in 0 .. min({MAX_ALTERNATIVES}, vocab), not {k}")
+    if out is None:
+        out = new_token_logprobs(n, k, device=dev, logp=token_ids is not None)
+    for t, need, name in ((out.logp, 4 * n, "logp"), (out.entropy, 4 * n, "entropy"),
+                          (out.log_z, 8 * n, "log_z")):
+        _need(t, need, name, dev, torch.float32)
+    if k:
+        for t, dtype, name in ((out.top_ids, torch.int32, "top_ids"),
+                               (out.top_logp, torch.float32, "top_logp")):
+            if t is None or t.device != dev or t.dtype != dtype or t.dim() != 2 or \
+                    t.shape != (n, k) or (n and t.stride(1) != 1):
+                raise ValueError(f"{name} must be {dtype} [n_tokens, k] on {dev} with unit column stride")
+        if out.top_ids.stride() != out.top_logp.stride():
+            raise ValueError("top_ids and top_logp must share a row stride")
+    if workspace is None:
+        workspace = LogprobsWorkspace(n, v, k, device=dev)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    rc = lib().turnkl_token_logprobs(
+        _ptr(logits), _row_stride(logits) if n else v, dt, n, v, _ptr(token_ids), _ptr(mask), k,
+        _ptr(out.logp), _ptr(out.entropy), _ptr(out.log_z), _ptr(out.top_ids) if k else None,
+        _ptr(out.top_logp) if k else None, (max(int(out.top_ids.stride(0)), k) if k else 0),
+        _ptr(workspace.tensor), workspace.nbytes, ctypes.c_void_p(stream))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_token_logprobs")
+    if check:
+        st = workspace.status()
+        if st != OK:
+            raise TurnKLError(st, "turnkl_token_logprobs (device)")
+    return out
 
 
 def new_turn_stats(max_turns: int, device="cuda") -> torch.Tensor:

@@ -1,0 +1,379 @@
+"""turnkl_token_logprobs against its definition in 64 bits (torch on float64).
+
+Tolerances.  M is a logit: equal.  S = sum 2^y adds at most about 200 terms in
+sequence per lane and a tree of 16 after it, each rounding 2^-24, and every term
+carries |y| 2^-24 from its exponent and an ulp of exp2; terms below 2^-30 of the
+sum do not matter, so S is within 200 2^-24 + 30 2^-24 + ... < 1.6e-5 relative,
+which is L's absolute error; L's own logarithm and the subtractions add a few
+ulps of L and of z - M: |d log p| <= 2e-5 + 1e-6 |log p|.  H = L - ln2 A / S has
+A's error too, each at most 2e-5 relative, of a quotient of at most H:
+|dH| <= 4e-5 (1 + H).  Ids are whole numbers and equal.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_05804_amd import turnkl as T
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def reference(z, ids, k, mask=None):
+    """(logp, entropy, M, L, top ids, top log p) in float64 on z's device."""
+    z = z.double()
+    n, v = z.shape
+    m = z.max(1).values  # NaN if the row holds one
+    clean = torch.where(z.isnan(), -math.inf, z)
+    mm = clean.max(1).values
+    empty = (m == -math.inf)
+    bad = m.isnan() | (m == math.inf)
+    x = z - torch.where(empty, 0.0, m)[:, None]
+    e = x.exp()
+    s = e.sum(1)
+    l = torch.where(empty, 0.0, s.log())
+    h = l - torch.where(e == 0, 0.0, e * x).sum(1) / torch.where(empty, 1.0, s)
+    lp = x - l[:, None]
+    lp = torch.where(bad[:, None], math.nan, lp)
+    l, h = torch.where(bad, math.nan, l), torch.where(bad, math.nan, h)
+    order = (clean + 0.0).sort(dim=1, descending=True, stable=True).indices[:, :k]
+    out = {"entropy": h, "M": mm, "L": l, "top_ids": order.int(), "top_logp": lp.gather(1, order)}
+    if ids is not None:
+        ok = (ids >= 0) & (ids < v)
+        t = torch.where(ok, ids, 0).long()
+        out["logp"] = torch.where(ok, lp.gather(1, t[:, None])[:, 0], math.nan)
+    if mask is not None:
+        on = mask != 0
+        for name, off in (("logp", 0.0), ("entropy", 0.0), ("M", math.nan), ("L", math.nan)):
+            if name in out:
+                out[name] = torch.where(on, out[name], off)
+        out["top_ids"] = torch.where(on[:, None], out["top_ids"], -1)
+        out["top_logp"] = torch.where(on[:, None], out["top_logp"], -math.inf)
+    return out
+
+
+def close(got, ref, abs_tol, rel_tol, what):
+    got = got.double()
+    same = (got == ref) | (got.isnan() & ref.isnan())
+    err = torch.where(same, 0.0, (got - ref).abs())
+    bound = abs_tol + rel_tol * ref.abs()
+    bad = ~same & ~(err <= bound)
+    assert not bool(bad.any()), (what, bad.nonzero()[:5].tolist(), got[bad][:5].tolist(), ref[bad][:5].tolist())
+
+
+def check(z, ids, k, mask=None, **kw):
+    out = T.token_logprobs(z, ids, k=k, mask=mask, **kw)
+    ref = reference(z, ids, k, mask)
+    assert torch.equal(torch.nan_to_num(out.log_z[:, 0].double(), nan=7.0),
+                       torch.nan_to_num(ref["M"], nan=7.0))
+    close(out.log_z[:, 1], ref["L"], 2e-5, 1e-6, "L")
+    h = ref["entropy"]
+    close(out.entropy, h, 4e-5, 4e-5, "entropy")
+    if ids is not None:
+        close(out.logp, ref["logp"], 2e-5, 1e-6, "logp")
+    if k:
+        assert torch.equal(out.top_ids, ref["top_ids"]), \
+            (out.top_ids != ref["top_ids"]).nonzero()[:5].tolist()
+        close(out.top_logp, ref["top_logp"], 2e-5, 1e-6, "top_logp")
+    return out
+
+
+def matrix(n, v, dtype, pad=0, start=0, fill=None):
+    """[n, v] with `pad` columns between rows, its first element `start` elements
+    past an allocation's; the rest is NaN."""
+    buf = torch.full((start + n * (v + pad) + 8,), math.nan, dtype=DT[dtype], device="cuda")
+    z = buf[start:start + n * (v + pad)].view(n, v + pad)[:, :v]
+    if fill is not None:
+        z.copy_(fill)
+    return z
+
+
+def normal(n, v, seed, scale=3.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn((n, v), generator=g, device="cuda") * scale
+
+
+def some_ids(n, v, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed + 1000)
+    return torch.randint(0, v, (n,), generator=g, device="cuda").int()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [1, 2, 3, 4, 5, 7, 8, 9, 15, 64, 127, 250, 1000, 1024, 2047, 4096, 8191,
+                               8192, 8193, 16385, 32000, 50257, 65536, 151936])
+def test_vocabularies(v, dtype, gpu):
+    n = 5
+    for k in sorted({0, 1, min(3, v), min(50, v), min(128, v)}):
+        check(matrix(n, v, dtype, fill=normal(n, v, v + k)), some_ids(n, v, v), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [196400, 196416, 196417, 262144, 400001])
+def test_rows_of_several_chunks(v, dtype, gpu):
+    for k in (0, 20, 128):
+        check(matrix(3, v, dtype, fill=normal(3, v, v + k)), some_ids(3, v, v), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v,pad,start", [(1000, 1, 0), (1000, 24, 1), (1003, 5, 3), (8200, 0, 7),
+                                         (50257, 47, 0), (50257, 1, 5), (33, 3, 1), (6, 2, 1), (151936, 3, 2)])
+def test_starts_and_strides(v, pad, start, dtype, gpu):
+    for k in (0, min(v, 50)):
+        check(matrix(7, v, dtype, pad, start, normal(7, v, v)), some_ids(7, v, v), k)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 17, 64, 300, 1100, 2500])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_batches(n, dtype, gpu):
+    for v, k in ((5000, 7), (20001, 50)):
+        check(matrix(n, v, dtype, fill=normal(n, v, n)), some_ids(n, v, n), k)
+
+
+def pattern(name, n, v):
+    """Rows on which a selection can go wrong."""
+    i = torch.arange(v, device="cuda", dtype=torch.float32)
+    if name == "constant":
+        return torch.full((n, v), 1.25, device="cuda")
+    if name == "ascending":
+        return (i * (40.0 / v) - 20.0).expand(n, v)
+    if name == "descending":
+        return (20.0 - i * (40.0 / v)).expand(n, v)
+    if name == "steps":  # few values, each many times
+        return (normal(n, v, 3) * 0.3).round()
+    if name == "zeros":  # +0 and -0 are equal
+        return torch.where(normal(n, v, 4) > 0, 0.0, -0.0)
+    if name == "run":  # the largest lie together
+        z = normal(n, v, 5)
+        z[:, v // 3:v // 3 + 700] += 30.0
+        return z
+    if name == "narrow":  # differences below 2^-8 of the values
+        return 100.0 + normal(n, v, 6) * 0.05
+    if name == "one_thread":  # large ones 2,048 elements apart
+        z = normal(n, v, 7)
+        z[:, 5::2048] += 50.0
+        return z
+    if name == "far":  # far from zero
+        return normal(n, v, 8) + 2000.0
+    if name == "spread":  # terms from 1 to nothing, references that move
+        return normal(n, v, 9) * 60.0
+    if name == "rising":  # the reference moves with every group
+        return i / v * 600.0 + normal(n, v, 10)
+    if name == "peaked":
+        z = normal(n, v, 11)
+        z[:, v // 2] = 90.0
+        return z
+    if name == "few_allowed":
+        z = torch.full((n, v), -math.inf, device="cuda")
+        z[:, ::max(1, v // 9)] = normal(n, len(range(0, v, max(1, v // 9))), 12)
+        return z
+    if name == "one_allowed":
+        z = torch.full((n, v), -math.inf, device="cuda")
+        z[:, v - 1] = 3.0
+        return z
+    if name == "late":  # nothing allowed for a long while
+        z = normal(n, v, 13)
+        z[:, :v * 2 // 3] = -math.inf
+        return z
+    if name == "lowest":
+        z = normal(n, v, 14)
+        z[:, ::3] = torch.finfo(torch.bfloat16).min
+        return z
+    if name == "all_lowest":
+        return torch.full((n, v), torch.finfo(torch.bfloat16).min, device="cuda")
+    if name == "huge":
+        z = normal(n, v, 15)
+        z[:, v // 4] = torch.finfo(torch.bfloat16).max
+        z[:, v // 5] = torch.finfo(torch.bfloat16).min
+        return z
+    raise ValueError(name)
+
+
+PATTERNS = ["constant", "ascending", "descending", "steps", "zeros", "run", "narrow", "one_thread",
+            "far", "spread", "rising", "peaked", "few_allowed", "one_allowed", "late", "lowest",
+            "all_lowest", "huge"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", PATTERNS)
+def test_patterns(name, dtype, gpu):
+    for n, v, k in ((3, 32000, 50), (2, 151936, 128), (3, 3001, 128), (3, 5001, 1), (3, 50257, 0),
+                    (2, 200000, 100)):
+        z = matrix(n, v, dtype, fill=pattern(name, n, v))
+        check(z, some_ids(n, v, k), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_without_a_distribution(dtype, gpu):
+    """Empty rows, and rows with NaN or +inf, beside ordinary ones."""
+    for v in (5, 3000, 50257, 200001):
+        z = normal(8, v, 1)
+        z[1] = -math.inf
+        z[2, v // 2] = math.nan
+        z[3, v // 2] = math.inf
+        z[4] = math.nan
+        z[5, :v - 1] = -math.inf
+        z[5, v - 1] = math.nan
+        z[6, 0] = math.inf
+        z[6, v - 1] = math.inf
+        k = min(v, 40)
+        out = check(matrix(8, v, dtype, fill=z), some_ids(8, v, 1), k)
+        assert out.logp[1] == -math.inf and out.entropy[1] == 0.0
+        assert torch.equal(out.top_ids[1].cpu(), torch.arange(k, dtype=torch.int32))
+        for r in (2, 3, 4, 5, 6):
+            assert out.logp[r].isnan() and out.entropy[r].isnan() and out.top_logp[r].isnan().all()
+
+
+@pytest.mark.parametrize("v", [1000, 50257, 200000])
+def test_masked_rows_are_not_read(v, gpu):
+    n = 40
+    mask = (torch.arange(n, device="cuda") % 3 != 1).to(torch.uint8)
+    for dtype in ("bf16", "f32"):
+        z = matrix(n, v, dtype, fill=normal(n, v, 2))
+        z[mask == 0] = math.nan
+        ids = some_ids(n, v, 2)
+        ids[mask == 0] = -5  # not looked at either
+        for k in (0, 9):
+            check(z, ids, k, mask)
+    none = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    check(z, ids, 9, none)
+
+
+def test_ids_out_of_range_are_reported(gpu):
+    n, v = 70, 2000
+    z = matrix(n, v, "bf16", fill=normal(n, v, 3))
+    for bad in (-1, v, 2 ** 31 - 1, -2 ** 31):
+        ids = some_ids(n, v, 3)
+        ids[11] = bad
+        ids[40] = bad
+        ws = T.LogprobsWorkspace(n, v, 4)
+        out = check(z, ids, 4, workspace=ws, check=False)
+        assert out.logp[11].isnan() and out.logp[40].isnan()
+        assert ws.status() == T.ERR_TOKEN_ID
+        with pytest.raises(T.TurnKLError, match="id outside"):
+            T.token_logprobs(z, ids, workspace=ws)
+        mask = torch.ones(n, dtype=torch.uint8, device="cuda")
+        mask[11] = mask[40] = 0
+        check(z, ids, 4, mask, workspace=ws)  # the same workspace, without an error
+        assert ws.status() == T.OK
+
+
+def test_empty_batch_and_no_tokens(gpu):
+    z = torch.empty((0, 500), dtype=torch.bfloat16, device="cuda")
+    out = T.token_logprobs(z, torch.empty(0, dtype=torch.int32, device="cuda"), k=3)
+    assert out.logp.shape == (0,) and out.top_ids.shape == (0, 3)
+    z = matrix(4, 3000, "f32", fill=normal(4, 3000, 1))
+    out = check(z, None, 5)
+    assert out.logp is None
+
+
+def test_some_outputs_and_strided_alternatives(gpu):
+    n, v, k = 6, 9000, 11
+    z = matrix(n, v, "bf16", fill=normal(n, v, 8))
+    ids = some_ids(n, v, 8)
+    full = check(z, ids, k)
+    wide_i = torch.full((n, k + 5), 77, dtype=torch.int32, device="cuda")
+    wide_p = torch.full((n, k + 5), 77.0, device="cuda")
+    out = T.TokenLogprobs(full.logp.clone(), None, None, wide_i[:, :k], wide_p[:, :k])
+    T.token_logprobs(z, ids, k=k, out=out)
+    assert torch.equal(wide_i[:, :k], full.top_ids) and torch.equal(wide_p[:, :k], full.top_logp)
+    assert bool((wide_i[:, k:] == 77).all()) and bool((wide_p[:, k:] == 77).all())
+    assert torch.equal(out.logp, full.logp)
+
+
+def test_same_bits_every_time_and_on_two_streams(gpu):
+    n, v, k = 200, 50257, 50
+    z = [matrix(n, v, "bf16", fill=normal(n, v, s)) for s in (1, 2)]
+    ids = some_ids(n, v, 1)
+    first = [T.token_logprobs(a, ids, k=k) for a in z]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(T.token_logprobs(z[i], ids, k=k, check=False))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in outs[i]:
+            for a, b in zip(o, first[i]):
+                assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+
+
+@pytest.mark.parametrize("n,v", [(1, 151936), (3, 200000), (40, 32000)])
+def test_graph_replays_equal_eager(n, v, gpu):
+    k = 20
+    z = matrix(n, v, "bf16", fill=normal(n, v, 5))
+    ids = some_ids(n, v, 5)
+    ws, out = T.LogprobsWorkspace(n, v, k), T.new_token_logprobs(n, k)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        T.token_logprobs(z, ids, k=k, out=out, workspace=ws)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            T.token_logprobs(z, ids, k=k, out=out, workspace=ws, check=False)
+    torch.cuda.current_stream().wait_stream(s)
+    for r in range(4):
+        z.copy_(normal(n, v, 50 + r))  # new inputs in the captured buffers
+        for t in out:
+            t.zero_()
+        ws.tensor.fill_(r)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        eager = check(z, ids, k)
+        for a, b in zip(got, eager):
+            assert torch.equal(a.view(torch.int32), b.view(torch.int32)), r
+
+
+def test_offsets_past_32_bits(gpu):
+    """The last rows of a matrix of more than 2^32 elements and bytes."""
+    n, v = 30000, 151936
+    z = torch.zeros((n, v), dtype=torch.bfloat16, device="cuda")
+    last = normal(4, v, 6).to(torch.bfloat16)
+    z[-4:] = last
+    mask = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    mask[-4:] = 1
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ids[-4:] = some_ids(4, v, 6)
+    out = T.token_logprobs(z, ids, k=5, mask=mask)
+    ref = check(last.contiguous(), ids[-4:].contiguous(), 5)
+    for a, b in zip(out, ref):
+        assert torch.equal(a[-4:], b)
+
+
+def test_support_for_the_top_k_loss(gpu):
+    """A teacher's alternatives are turnkl_fwd_bwd_topk's support."""
+    n, v, k = 64, 32000, 50
+    zs, zt = (matrix(n, v, "bf16", fill=normal(n, v, s)) for s in (1, 2))
+    turn = torch.arange(n, device="cuda", dtype=torch.int32) // 16
+    traj = torch.zeros(n, device="cuda", dtype=torch.int32)
+    mask = torch.ones(n, device="cuda", dtype=torch.uint8)
+    top = T.token_logprobs(zt, k=k)
+    loss, _, _, _, kl, _ = T.fwd_bwd_topk(zs, top.top_ids, top.top_logp, turn, traj, mask, 0.5,
+                                          grad=None, token_kl=True)
+    ids = zt.double().sort(dim=1, descending=True, stable=True).indices[:, :k]
+    a, b = (x.double().gather(1, ids).log_softmax(1) for x in (zs, zt))
+    ref = (a.exp() * (a - b)).sum(1)
+    assert torch.allclose(kl.double(), ref, rtol=2e-4, atol=5e-6)
+
+
+def test_binding_refuses(gpu):
+    z = matrix(4, 100, "bf16", fill=normal(4, 100, 1))
+    ids = some_ids(4, 100, 1)
+    with pytest.raises(TypeError):
+        T.token_logprobs(z.half(), ids)
+    for kw in (dict(token_ids=ids.long()), dict(token_ids=ids[:3]), dict(token_ids=ids.cpu()),
+               dict(mask=ids), dict(k=3, out=T.new_token_logprobs(4, 2)),
+               dict(out=T.new_token_logprobs(3))):
+        with pytest.raises(ValueError):
+            T.token_logprobs(z, **{"token_ids": ids, **kw})
+    for k in (-1, 101, 129):
+        with pytest.raises(ValueError, match="k must be"):
+            T.token_logprobs(z, ids, k=k)
+    with pytest.raises(ValueError):
+        T.token_logprobs(z.t(), ids)
