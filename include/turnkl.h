@@ -425,6 +425,85 @@ int turnkl_token_logprobs(const void* logits, int64_t ld, int dtype, int64_t n_t
                           int32_t* top_ids_out, float* top_logp_out, int64_t ld_top,
                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * The gradient of sum_i (gl_i logp_i + gh_i H_i) with respect to the logits:
+ *   G[i, v] = gl_i ([v = t] - p_v) - gh_i p_v (log p_v + H_i).
+ * logits, ld, token_ids, mask   as in turnkl_token_logprobs.  token_ids may be
+ *                NULL when grad_logp is.  An id outside [0, vocab) has no column
+ *                of its own: its row's gradient keeps the -gl_i p_v part.
+ * log_z          [n_tokens x 2] (M, L) of turnkl_token_logprobs.
+ * entropy        [n_tokens] H of the same call; NULL when grad_entropy is.
+ * grad_logp      [n_tokens] gl, or NULL for zeros.
+ * grad_entropy   [n_tokens] gh, or NULL for zeros.  One of the two is given.
+ * grad_out       [n_tokens x vocab] of `dtype`, row stride ld_grad >= vocab, rounded
+ *                to nearest even; may equal logits with ld_grad == ld (in place),
+ *                any other overlap with an input is TURNKL_ERR_ALIAS.  Rows not
+ *                asked for are written as zeros, and so are empty rows (M = -inf);
+ *                a row with NaN in L is NaN throughout.
+ * vocab is at most 2^24.  No workspace, no device-detected errors.
+ */
+int turnkl_token_logprobs_bwd(const void* logits, int64_t ld, int dtype, int64_t n_tokens,
+                              int64_t vocab, const int32_t* token_ids, const uint8_t* mask,
+                              const float* log_z, const float* entropy, const float* grad_logp,
+                              const float* grad_entropy, void* grad_out, int64_t ld_grad,
+                              hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Normalisation of the rows that a vocabulary projection turns into logits,
+ * and its gradient.  For a row x of D elements, with mu = mean x (layer) or 0
+ * (root mean square), r = 1 / sqrt(mean (x - mu)^2 + eps) and xh = (x - mu) r:
+ *   y  = xh w + b,
+ *   and for the gradient g of y, with q = g w:
+ *   dx = r (q - mean q - xh mean(q xh))    (root mean square: no mean q),
+ *   dw = sum over rows of g xh,   db = sum over rows of g.
+ * Means, sums and statistics are float or wider; y and dx are rounded to nearest
+ * even once.  NaN and infinities spread as in the formulas.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  TURNKL_NORM_LAYER = 0,
+  TURNKL_NORM_RMS = 1,
+} turnkl_norm_kind;
+
+/* The widest row, in elements. */
+#define TURNKL_MAX_NORM_WIDTH 16384
+
+/*
+ * x              [n_rows x width] of `dtype`, row stride ld_x (elements, >= width),
+ *                rows of any start.
+ * weight, bias   [width] of param_dtype, or NULL (ones, zeros).
+ * eps            finite, >= 0.
+ * y              [n_rows x width] of `dtype`, row stride ld_y; may equal x with
+ *                ld_y == ld_x (in place).
+ * stats_out      [n_rows x 2] float (mu, r), or NULL.
+ */
+int turnkl_norm_fwd(const void* x, int64_t ld_x, int dtype, int64_t n_rows, int64_t width,
+                    const void* weight, const void* bias, int param_dtype, int kind, double eps,
+                    void* y, int64_t ld_y, float* stats_out, hipStream_t stream);
+
+/* Bytes of device workspace for turnkl_norm_bwd (host; a pure function of its
+ * arguments), 0 for invalid ones (n_rows < 0 or above 2^31 - 1, width < 1 or above
+ * TURNKL_MAX_NORM_WIDTH).  No initialisation; 256-byte aligned. */
+size_t turnkl_norm_workspace_bytes(int64_t n_rows, int64_t width);
+
+/*
+ * grad_y, x      [n_rows x width] of `dtype`, row strides ld_gy, ld_x.
+ * weight, param_dtype, kind   those of turnkl_norm_fwd.
+ * stats          its stats_out.
+ * grad_x         [n_rows x width] of `dtype`, or NULL; may equal grad_y or x with
+ *                the same row stride (in place).
+ * grad_weight, grad_bias   [width] float, or NULL; summed in a fixed order (the same
+ *                bits from call to call).  accumulate != 0 adds to their contents,
+ *                0 overwrites (with zeros when n_rows = 0).
+ * workspace      turnkl_norm_workspace_bytes(n_rows, width); may be NULL when
+ *                neither sum is asked for.
+ * Any other overlap of an output with an input or output is TURNKL_ERR_ALIAS.
+ */
+int turnkl_norm_bwd(const void* grad_y, int64_t ld_gy, const void* x, int64_t ld_x, int dtype,
+                    int64_t n_rows, int64_t width, const void* weight, int param_dtype, int kind,
+                    const float* stats, void* grad_x, int64_t ld_gx, float* grad_weight,
+                    float* grad_bias, int accumulate, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream);
+
 /* ------------------------------------------------------------------------
  * Adaptive rollout-depth controller (Sec. 5.1; App. D, Algorithm 1 and the
  * full-configuration table).  HOST functions: all pointers are host memory,

@@ -22,7 +22,7 @@
 
 #include <type_traits>
 
-#include "row_ops.h"
+#include "row_span.h"
 
 namespace turnkl {
 namespace {
@@ -220,44 +220,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     const int lo = (int)chunk_start(n_row, p.n_chunks, 8, c);
     const int n = (int)chunk_start(n_row, p.n_chunks, 8, c + 1) - lo;
     const int col = lo * kEpv - pre;  // first element of the chunk
-    const auto rz = chunk_rsrc(at_row);
+    const RowSpan<kBf16, kRagged> span{at_row, chunk_rsrc(at_row), p.vocab, col, n};
     const int groups = (n + kLpThreads * kLpPacks - 1) / (kLpThreads * kLpPacks);
-
-    // Pack i of the chunk, moved inside the row where it sticks out: its first
-    // element, and which elements are its own.
-    auto place = [&](int i, unsigned& bits) -> int {
-      const int e = col + i * kEpv;
-      if constexpr (kRagged) {
-        const int at = inside_row(e, p.vocab > kEpv ? p.vocab - kEpv : 0);
-        bits = i < n ? own_bits<kEpv>(e - at) : 0u;
-        if (p.vocab < kEpv) bits &= (1u << p.vocab) - 1u;
-        return at;
-      } else {
-        bits = i < n ? (1u << kEpv) - 1u : 0u;
-        return i < n ? e : 0;
-      }
-    };
-    auto load_at = [&](P& x, int at) {
-      if constexpr (kRagged) {
-        if (p.vocab < kEpv) {  // a row shorter than a pack: element by element
-          if constexpr (kBf16) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x.w[j] = 0u;
-#pragma unroll
-            for (int j = 0; j < kEpv; ++j) {
-              const unsigned w = j < p.vocab ? reinterpret_cast<const unsigned short*>(at_row)[j] : 0u;
-              x.w[j >> 1] |= w << (16 * (j & 1));
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < kEpv; ++j)
-              x.f[j] = j < p.vocab ? reinterpret_cast<const float*>(at_row)[j] : 0.0f;
-          }
-          return;
-        }
-      }
-      x.load(rz, at * kEs, 0);
-    };
 
     float ref = -INFINITY, ss = 0.0f, aa = 0.0f;  // the wave's reference and lane sums
     float best = -INFINITY;                       // the lane's largest logit
@@ -269,10 +233,10 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
       for (int q = 0; q < kLpPacks; ++q) {
         const int v = g * kLpPacks + q;
         if constexpr (kEdge) {
-          const int at = place(v * kLpThreads + tid, bits[q]);
-          load_at(x[q], at);
+          const int at = span.place(v * kLpThreads + tid, bits[q]);
+          span.load(x[q], at);
         } else {
-          x[q].load(rz, tid * 16, col * kEs + v * kStepBytes);
+          x[q].load(span.rsrc, tid * 16, col * kEs + v * kStepBytes);
         }
       }
       float top[kLpPacks / kUnitPacks];
@@ -351,6 +315,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
         out[0] = t.m;
         out[1] = t.s;
         out[2] = t.a;
+        drain_stores();  // their data registers are free
       }
     }
     if constexpr (kTop) {
@@ -383,9 +348,9 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
         if (tid < kStep && j < total) {
           const int i = listed ? s_list[j / kUnitPacks] + j % kUnitPacks * kLpThreads : j;
           unsigned bits;
-          const int at = place(i, bits);
+          const int at = span.place(i, bits);
           P x;
-          load_at(x, at);
+          span.load(x, at);
           const unsigned long long least = s_floor;
 #pragma unroll
           for (int q = 0; q < kEpv; ++q) {

@@ -1,0 +1,407 @@
+// Normalisation of rows (layer norm, or by the root mean square) and its gradient.
+//
+// A row is held in registers, kPacks 16-byte packs a thread, by the kThreads
+// threads of one workgroup, so that it is read once and its mean and the sum of
+// squared differences from it are taken one after the other.  Every workgroup goes
+// from row to row and keeps its columns' weights (and, backward, the columns' sums
+// over its rows) in registers; the next row is on its way while one is reduced.
+// Backward a second kernel adds the workgroups' sums in their order.  Bound: HBM.
+
+#include "row_span.h"
+
+namespace turnkl {
+namespace {
+
+constexpr int kSumPacks = 2048;  // packs of a row whose columns' sums fit the registers
+
+// Sums of kN values over a workgroup, the same in every thread.  `lds` holds
+// 2 x kWaves x kN floats; `turn` alternates from call to call, so that one barrier
+// serves: the other half is rewritten only after the next call's barrier.
+template <int kThreads, int kN>
+__device__ inline void row_sums(float (&v)[kN], float* lds, int& turn) {
+  constexpr int kWaves = kThreads / kWave;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (kWaves > 1) {
+    float* const s = lds + turn * (kWaves * kN);
+    turn ^= 1;
+    if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) s[(threadIdx.x / kWave) * kN + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      v[i] = s[i];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v[i] += s[w * kN + i];
+    }
+  }
+}
+
+// A pack's own elements of a vector of parameters (`fill` where there is none, and
+// for elements that are another thread's).
+template <int kEpv>
+__device__ inline void load_params(const void* v, bool bf16, float fill, int at, unsigned bits,
+                                   float (&out)[kEpv]) {
+#pragma unroll
+  for (int j = 0; j < kEpv; ++j) out[j] = fill;
+  if (!v || !bits) return;
+  const auto r = chunk_rsrc(v);
+  const bool whole = bits == (1u << kEpv) - 1u;
+  if (bf16 && whole) {
+    unsigned u[kEpv / 2];
+    if constexpr (kEpv == 8) {
+      const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at * 2, 0, 0);
+      u[0] = x[0]; u[1] = x[1]; u[2] = x[2]; u[3] = x[3];
+    } else {
+      const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, at * 2, 0, 0);
+      u[0] = x[0]; u[1] = x[1];
+    }
+#pragma unroll
+    for (int j = 0; j < kEpv; ++j)
+      out[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xFFFF0000u : u[j >> 1] << 16);
+  } else if (whole) {
+#pragma unroll
+    for (int k = 0; k < kEpv / 4; ++k) {
+      const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 16 * k, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[4 * k + j] = __uint_as_float(x[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kEpv; ++j) {
+      if (!((bits >> j) & 1u)) continue;
+      out[j] = bf16 ? __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, (at + j) * 2, 0, 0) << 16)
+                    : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (at + j) * 4, 0, 0));
+    }
+  }
+}
+
+template <bool kBf16, bool kRagged>
+__device__ inline RowSpan<kBf16, kRagged> row_of(const void* base, long long ld, long long row, int width,
+                                                 int packs) {
+  const char* const at = static_cast<const char*>(base) + row * ld * (kBf16 ? 2 : 4);
+  return RowSpan<kBf16, kRagged>{at, chunk_rsrc(at), width, 0, packs};
+}
+
+template <bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
+__global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
+  using Span = RowSpan<kBf16, kRagged>;
+  using P = typename Span::P;
+  constexpr int kEpv = Span::kEpv;
+  __shared__ float s_sum[2 * (kThreads / kWave)];
+  const int tid = threadIdx.x;
+  const int packs = (p.width + kEpv - 1) / kEpv;
+  const float width = (float)p.width;
+  int at[kPacks], turn = 0;
+  unsigned bits[kPacks];
+  {
+    const Span s = row_of<kBf16, kRagged>(p.x, 0, 0, p.width, packs);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * kThreads + tid, bits[q]);
+  }
+  float w[kPacks][kEpv], b[kPacks][kEpv];
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q) {
+    load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[q]);
+    load_params(p.bias, p.param_bf16, 0.0f, at[q], bits[q], b[q]);
+  }
+  P next[kPacks];
+  auto fetch = [&](long long row) {
+    const Span s = row_of<kBf16, kRagged>(p.x, p.ld_x, row, p.width, packs);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q)
+      if (bits[q]) s.load(next[q], at[q]);
+  };
+  long long row = blockIdx.x;
+  if (row < p.n_rows) fetch(row);
+  for (; row < p.n_rows; row += gridDim.x) {
+    P x[kPacks];
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) x[q] = next[q];
+    if (row + gridDim.x < p.n_rows) fetch(row + gridDim.x);
+    float mean = 0.0f;
+    if constexpr (!kRms) {
+      float v[1] = {0.0f};
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+        for (int j = 0; j < kEpv; ++j) v[0] += (bits[q] >> j) & 1u ? x[q].get(j) : 0.0f;
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q) x[q].fence();  // unpacked again, rather than kept
+      row_sums<kThreads>(v, s_sum, turn);
+      mean = v[0] / width;
+    }
+    float v[1] = {0.0f};
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) {
+        const float d = (bits[q] >> j) & 1u ? x[q].get(j) - mean : 0.0f;
+        v[0] = fmaf(d, d, v[0]);
+      }
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) x[q].fence();
+    row_sums<kThreads>(v, s_sum, turn);
+    const float rstd = 1.0f / sqrtf(v[0] / width + p.eps);
+    const Span out = row_of<kBf16, kRagged>(p.out, p.ld_out, row, p.width, packs);
+    typename P::Data data[kPacks];
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      float y[kEpv];
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) y[j] = fmaf((x[q].get(j) - mean) * rstd, w[q][j], b[q][j]);
+      data[q] = P::encode(y, 0u);
+    }
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) settle(data[q]);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) out.store_own(data[q], at[q], bits[q]);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) out.store_whole(data[q], at[q], bits[q]);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
+    if (p.stats && tid == 0) {
+      p.stats[2 * row] = mean;
+      p.stats[2 * row + 1] = rstd;
+    }
+    drain_stores();  // their data registers are free for the next row
+  }
+}
+
+template <bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
+__global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
+  using Span = RowSpan<kBf16, kRagged>;
+  using P = typename Span::P;
+  constexpr int kEpv = Span::kEpv;
+  // The widest rows fill the registers: there the weights are loaded for every row,
+  // no row ahead, and the columns' sums are left to norm_bwd_columns.
+  constexpr bool kLean = kThreads * kPacks > kSumPacks;
+  __shared__ float s_sum[2 * 2 * (kThreads / kWave)];
+  const int tid = threadIdx.x;
+  const int packs = (p.width + kEpv - 1) / kEpv;
+  const float width = (float)p.width;
+  int at[kPacks], turn = 0;
+  unsigned bits[kPacks];
+  {
+    const Span s = row_of<kBf16, kRagged>(p.x, 0, 0, p.width, packs);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * kThreads + tid, bits[q]);
+  }
+  float w[kLean ? 1 : kPacks][kEpv], gw[kLean ? 1 : kPacks][kEpv], gb[kLean ? 1 : kPacks][kEpv];
+  if constexpr (!kLean)
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[q]);
+  auto weights = [&](int q) -> const float* {
+    if constexpr (kLean) load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[0]);
+    return w[kLean ? 0 : q];
+  };
+#pragma unroll
+  for (int q = 0; q < (kLean ? 1 : kPacks); ++q)
+#pragma unroll
+    for (int j = 0; j < kEpv; ++j) {
+      gw[q][j] = 0.0f;
+      gb[q][j] = 0.0f;
+    }
+  P next_x[kPacks], next_g[kPacks];
+  auto fetch = [&](long long row) {
+    const Span sx = row_of<kBf16, kRagged>(p.x, p.ld_x, row, p.width, packs);
+    const Span sg = row_of<kBf16, kRagged>(p.gy, p.ld_gy, row, p.width, packs);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      if (!bits[q]) continue;
+      sx.load(next_x[q], at[q]);
+      sg.load(next_g[q], at[q]);
+    }
+  };
+  long long row = blockIdx.x;
+  if (!kLean && row < p.n_rows) fetch(row);
+  for (; row < p.n_rows; row += gridDim.x) {
+    if constexpr (kLean) fetch(row);
+    P x[kPacks], g[kPacks];
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      x[q] = next_x[q];
+      g[q] = next_g[q];
+    }
+    const float mean = kRms ? 0.0f : p.stats[2 * row];
+    const float rstd = p.stats[2 * row + 1];
+    if (!kLean && row + gridDim.x < p.n_rows) fetch(row + gridDim.x);
+    float v[2] = {0.0f, 0.0f};  // sums of q xh and q
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      const float* const wq = weights(q);
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) {
+        if (!((bits[q] >> j) & 1u)) continue;
+        const float gy = g[q].get(j);
+        const float xh = (x[q].get(j) - mean) * rstd;
+        const float qq = gy * wq[j];
+        v[0] = fmaf(qq, xh, v[0]);
+        if constexpr (!kRms) v[1] += qq;
+        if constexpr (!kLean) {
+          gw[q][j] = fmaf(gy, xh, gw[q][j]);
+          gb[q][j] += gy;
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {  // unpacked again, rather than kept
+      x[q].fence();
+      g[q].fence();
+    }
+    row_sums<kThreads>(v, s_sum, turn);
+    if (p.out) {
+      const float c1 = v[0] / width, c0 = v[1] / width;
+      const Span out = row_of<kBf16, kRagged>(p.out, p.ld_out, row, p.width, packs);
+      typename P::Data data[kPacks];
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q) {
+        float d[kEpv];
+        const float* const wq = weights(q);
+#pragma unroll
+        for (int j = 0; j < kEpv; ++j) {
+          const float xh = (x[q].get(j) - mean) * rstd;
+          const float qq = g[q].get(j) * wq[j];
+          d[j] = rstd * fmaf(-xh, c1, kRms ? qq : qq - c0);
+        }
+        data[q] = P::encode(d, 0u);
+      }
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q) settle(data[q]);
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q) out.store_own(data[q], at[q], bits[q]);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) out.store_whole(data[q], at[q], bits[q]);
+      drain_stores();  // their data registers are free for the next row
+    }
+  }
+  if (!kLean && p.part) {
+    float* const part = p.part + (long long)blockIdx.x * 2 * p.width;
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) {
+        if (!((bits[q] >> j) & 1u)) continue;
+        if (p.gw) part[at[q] + j] = gw[kLean ? 0 : q][j];
+        if (p.gb) part[p.width + at[q] + j] = gb[kLean ? 0 : q][j];
+      }
+  }
+}
+
+// The column sums of the widest rows, which are read again: a thread per column, each
+// of the n_groups runs of rows by workgroups of its own.
+constexpr int kColumnThreads = 256;
+__global__ __launch_bounds__(kColumnThreads) void norm_bwd_columns(NormParams p) {  // fp32 rows only
+  const int col = blockIdx.x * kColumnThreads + threadIdx.x;
+  if (col >= p.width) return;
+  const float* const g = static_cast<const float*>(p.gy);
+  const float* const x = static_cast<const float*>(p.x);
+  float gw = 0.0f, gb = 0.0f;
+#pragma unroll 4
+  for (long long row = blockIdx.y; row < p.n_rows; row += p.n_groups) {
+    const float gy = g[row * p.ld_gy + col];
+    const float mean = p.rms ? 0.0f : p.stats[2 * row];
+    gw = fmaf(gy, (x[row * p.ld_x + col] - mean) * p.stats[2 * row + 1], gw);
+    gb += gy;
+  }
+  float* const part = p.part + (long long)blockIdx.y * 2 * p.width;
+  if (p.gw) part[col] = gw;
+  if (p.gb) part[p.width + col] = gb;
+}
+
+// Adds the workgroups' column sums, in their order: 64 columns a workgroup, four
+// runs of partial rows side by side.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void norm_bwd_join(NormParams p) {
+  __shared__ float s_run[kJoinThreads / kWave][kWave];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int run = threadIdx.x / kWave;
+  constexpr int kRuns = kJoinThreads / kWave;
+  const int col = blockIdx.x * kWave + lane;
+  for (int which = 0; which < 2; ++which) {
+    float* const out = which ? p.gb : p.gw;
+    if (!out) continue;
+    float s = 0.0f;
+    if (col < p.width) {
+      const float* at = p.part + (long long)which * p.width + col;
+      const int lo = p.n_groups * run / kRuns, hi = p.n_groups * (run + 1) / kRuns;
+      for (int i = lo; i < hi; ++i) s += at[(long long)i * 2 * p.width];
+    }
+    s_run[run][lane] = s;
+    __syncthreads();
+    if (run == 0 && col < p.width) {
+      float t = s_run[0][lane];
+#pragma unroll
+      for (int r = 1; r < kRuns; ++r) t += s_run[r][lane];
+      out[col] = p.accumulate ? out[col] + t : t;
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int kNormGrid = 2048;    // workgroups that go from row to row
+constexpr int kNormGroups = 1024;  // the same backward: each leaves a partial sum
+
+template <bool kBwd, bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
+void launch_one(const NormParams& p, hipStream_t s) {
+  if constexpr (kBwd) {
+    norm_bwd_rows<kBf16, kRagged, kRms, kThreads, kPacks><<<p.n_groups, kThreads, 0, s>>>(p);
+  } else {
+    const int grid = p.n_rows < kNormGrid ? p.n_rows : kNormGrid;
+    norm_fwd_rows<kBf16, kRagged, kRms, kThreads, kPacks><<<grid, kThreads, 0, s>>>(p);
+  }
+}
+
+template <bool kBwd, bool kBf16, bool kRagged, bool kRms>
+void launch_sized(const NormParams& p, hipStream_t s) {
+  const int epv = kBf16 ? 8 : 4;
+  const int packs = (p.width + epv - 1) / epv;
+  if (packs <= 64) launch_one<kBwd, kBf16, kRagged, kRms, 64, 1>(p, s);
+  else if (packs <= 256) launch_one<kBwd, kBf16, kRagged, kRms, 256, 1>(p, s);
+  else if (packs <= 512) launch_one<kBwd, kBf16, kRagged, kRms, 256, 2>(p, s);
+  else if (packs <= 1024) launch_one<kBwd, kBf16, kRagged, kRms, 512, 2>(p, s);
+  else if (packs <= kSumPacks) launch_one<kBwd, kBf16, kRagged, kRms, 512, 4>(p, s);
+  else if constexpr (!kBf16) launch_one<kBwd, kBf16, kRagged, kRms, 512, 8>(p, s);
+}
+
+template <bool kBwd>
+void launch_norm(const NormParams& p, hipStream_t s) {
+#define TURNKL_NORM(B, R, M)                                                      \
+  if ((p.bf16 != 0) == B && (p.ragged != 0) == R && (p.rms != 0) == M)            \
+    launch_sized<kBwd, B, R, M>(p, s);
+  TURNKL_NORM(true, false, false) TURNKL_NORM(true, false, true) TURNKL_NORM(true, true, false)
+  TURNKL_NORM(true, true, true) TURNKL_NORM(false, false, false) TURNKL_NORM(false, false, true)
+  TURNKL_NORM(false, true, false) TURNKL_NORM(false, true, true)
+#undef TURNKL_NORM
+}
+
+}  // namespace
+
+int norm_groups(long long n_rows, long long width) {
+  (void)width;
+  const long long g = (n_rows + 7) / 8;  // eight rows a workgroup at least
+  return (int)(g < 1 ? 1 : g < kNormGroups ? g : kNormGroups);
+}
+
+hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s) {
+  if (p.n_rows == 0) return hipSuccess;
+  launch_norm<false>(p, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s) {
+  const bool sums = p.gw || p.gb;
+  if (sums && !p.bf16 && (p.width + 3) / 4 > kSumPacks) {  // before the rows: they may be in place
+    const dim3 grid((p.width + kColumnThreads - 1) / kColumnThreads, p.n_groups);
+    norm_bwd_columns<<<grid, kColumnThreads, 0, s>>>(p);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  launch_norm<true>(p, s);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (!sums) return hipSuccess;
+  norm_bwd_join<<<(p.width + kWave - 1) / kWave, kJoinThreads, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace turnkl

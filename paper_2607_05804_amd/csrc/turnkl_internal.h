@@ -404,8 +404,56 @@ constexpr int kMaxAlternatives = TURNKL_MAX_ALTERNATIVES;
 constexpr int kLogprobPart = 4;             // maximum, S, A, unused
 constexpr int kMaxLogprobVocab = 1 << 24;
 
+// The gradient of the log probabilities and entropies (logprobs_bwd.hip).
+struct LogprobGradParams {
+  const void* z;
+  const int* ids;             // or null
+  const unsigned char* mask;  // or null: every row
+  const float* log_z;
+  const float* entropy;       // or null, like the next two
+  const float* g_logp;
+  const float* g_entropy;
+  void* grad;
+  long long ld;
+  long long ld_g;
+  int n_rows;
+  int vocab;
+  int bf16;
+  int ragged;  // rows of any start and length, the gradient's among them
+};
+
 int logprob_chunks(long long n_rows, long long vocab);
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s);
+hipError_t launch_logprobs_bwd(const LogprobGradParams& p, hipStream_t s);
+
+// Row normalisation (norm.hip), forward and backward.
+struct NormParams {
+  const void* x;
+  const void* gy;      // backward: the gradient of y
+  const void* weight;  // or null: ones
+  const void* bias;    // or null: zeros
+  void* out;           // y, or the gradient of x (backward: may be null)
+  float* stats;        // forward: output or null; backward: input
+  float* part;         // backward: [n_groups][2][width] partial sums, or null
+  float* gw;           // backward: sums, or null
+  float* gb;
+  long long ld_x;
+  long long ld_gy;
+  long long ld_out;
+  int n_rows;
+  int width;
+  int n_groups;        // backward: workgroups over the rows
+  float eps;
+  int bf16;
+  int param_bf16;
+  int rms;
+  int ragged;          // rows of any start and length
+  int accumulate;
+};
+
+int norm_groups(long long n_rows, long long width);
+hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s);
+hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s);
 
 // status_out: optional device int32 that receives the call's status
 // (TURNKL_OK or the device-detected error) once the loss is written.

@@ -40,6 +40,9 @@ F32 = 1
 
 # The most alternatives of one row (TURNKL_MAX_ALTERNATIVES).
 MAX_ALTERNATIVES = 128
+# Kinds of normalisation (turnkl_norm_kind).
+NORM_LAYER = 0
+NORM_RMS = 1
 
 # Names of every entry point include/turnkl.h declares.
 EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
@@ -48,7 +51,8 @@ EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
            "turnkl_depth_default_config", "turnkl_depth_init", "turnkl_depth_plan",
            "turnkl_depth_update", "turnkl_loss_share", "turnkl_budget_report",
            "turnkl_outcome_gap", "turnkl_token_logprobs_workspace_bytes",
-           "turnkl_token_logprobs")
+           "turnkl_token_logprobs", "turnkl_token_logprobs_bwd", "turnkl_norm_fwd",
+           "turnkl_norm_workspace_bytes", "turnkl_norm_bwd")
 # ... and every entry point include/turnkl_testing.h declares (measurement and
 # test hooks).
 TESTING_EXPORTS = ("turnkl_profile_row_kernel", "turnkl_set_row_tiling",
@@ -175,6 +179,21 @@ def lib() -> ctypes.CDLL:
             c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int32,
             c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p,
             c.c_size_t, c.c_void_p]
+        l.turnkl_token_logprobs_bwd.restype = c.c_int
+        l.turnkl_token_logprobs_bwd.argtypes = [
+            c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64] + [c.c_void_p] * 7 + [
+            c.c_int64, c.c_void_p]
+        l.turnkl_norm_fwd.restype = c.c_int
+        l.turnkl_norm_fwd.argtypes = [
+            c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int,
+            c.c_int, c.c_double, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p]
+        l.turnkl_norm_workspace_bytes.restype = c.c_size_t
+        l.turnkl_norm_workspace_bytes.argtypes = [c.c_int64, c.c_int64]
+        l.turnkl_norm_bwd.restype = c.c_int
+        l.turnkl_norm_bwd.argtypes = [
+            c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p,
+            c.c_int, c.c_int, c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p, c.c_int,
+            c.c_void_p, c.c_size_t, c.c_void_p]
         _lib = l
     return _lib
 
@@ -652,6 +671,148 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
         if st != OK:
             raise TurnKLError(st, "turnkl_token_logprobs (device)")
     return out
+
+
+def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log_z: torch.Tensor,
+                       entropy: torch.Tensor | None = None, *,
+                       grad_logp: torch.Tensor | None = None,
+                       grad_entropy: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                       grad: str | torch.Tensor = "new") -> torch.Tensor:
+    """turnkl_token_logprobs_bwd on the current stream: the gradient of
+    sum_i (grad_logp_i logp_i + grad_entropy_i H_i) with respect to the logits.
+
+    log_z, entropy: those of token_logprobs on the same logits, tokens and mask
+    (entropy is needed with grad_entropy only); grad: "new" allocates it,
+    "inplace" writes it over the logits, a tensor of their shape receives it.
+    """
+    dt, n, v = _check_token_rows(logits, token_ids, mask)
+    dev = logits.device
+    for t, size, name in ((log_z, 8 * n, "log_z"), (entropy, 4 * n, "entropy"),
+                          (grad_logp, 4 * n, "grad_logp"), (grad_entropy, 4 * n, "grad_entropy")):
+        _need(t, size, name, dev, torch.float32)
+    if isinstance(grad, str):
+        if grad not in ("new", "inplace"):
+            raise ValueError(grad)
+        grad = torch.empty_like(logits) if grad == "new" else logits
+    elif grad.device != dev or grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad must match the logits' device, dtype and shape")
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    rc = lib().turnkl_token_logprobs_bwd(
+        _ptr(logits), _row_stride(logits) if n else v, dt, n, v, _ptr(token_ids), _ptr(mask),
+        _ptr(log_z), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad),
+        _row_stride(grad) if n else v, ctypes.c_void_p(stream))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_token_logprobs_bwd")
+    return grad
+
+
+class NormWorkspace(Workspace):
+    """Caller-owned device scratch for turnkl_norm_bwd."""
+
+    def __init__(self, n_rows: int, width: int, device="cuda"):
+        nbytes = int(lib().turnkl_norm_workspace_bytes(n_rows, width))
+        if nbytes == 0:
+            raise TurnKLError(ERR_INVALID_ARG, "turnkl_norm_workspace_bytes")
+        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.nbytes = nbytes
+
+
+def _rows_like(t: torch.Tensor | None, x: torch.Tensor, name: str) -> None:
+    if t is not None and (t.device != x.device or t.dtype != x.dtype or t.shape != x.shape):
+        raise ValueError(f"{name} must match the rows' device, dtype and shape")
+
+
+def _check_norm(x, params):
+    """dtype code, rows, width and the parameters' dtype code of a normalisation."""
+    dt = _dtype_code(x)
+    if x.dim() != 2:
+        raise ValueError("rows must be 2-D with unit column stride")
+    pt = None
+    for t, name in params:
+        if t is None:
+            continue
+        if t.dim() != 1 or t.numel() != x.shape[1] or t.device != x.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous with one entry per column, on {x.device}")
+        code = _dtype_code(t)
+        if pt is not None and code != pt:
+            raise TypeError("weight and bias must share a dtype")
+        pt = code
+    return dt, int(x.shape[0]), int(x.shape[1]), dt if pt is None else pt
+
+
+def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None,
+             bias: torch.Tensor | None = None, *, rms: bool = False, eps: float = 1e-6,
+             y: str | torch.Tensor = "new", stats: bool | torch.Tensor = True):
+    """turnkl_norm_fwd on the current stream: layer norm of every row of x, or
+    (rms) its division by the root mean square.
+
+    x: [N, D] bf16 or float32 of any row stride; weight, bias: [D] of either type
+    or None; y: "new", "inplace" (over x) or a tensor of x's shape; stats: True
+    allocates, or a float32 [N, 2] tensor receives, each row's (mean, 1 / standard
+    deviation), which norm_bwd takes.  Returns (y, stats or None).
+    """
+    dt, n, d, pt = _check_norm(x, ((weight, "weight"), (bias, "bias")))
+    dev = x.device
+    if isinstance(y, str):
+        if y not in ("new", "inplace"):
+            raise ValueError(y)
+        y = torch.empty_like(x) if y == "new" else x
+    _rows_like(y, x, "y")
+    if isinstance(stats, bool):
+        stats = torch.empty((n, 2), dtype=torch.float32, device=dev) if stats else None
+    _need(stats, 8 * n, "stats", dev, torch.float32)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    rc = lib().turnkl_norm_fwd(
+        _ptr(x), _row_stride(x) if n else d, dt, n, d, _ptr(weight), _ptr(bias), pt,
+        NORM_RMS if rms else NORM_LAYER, eps, _ptr(y), _row_stride(y) if n else d, _ptr(stats),
+        ctypes.c_void_p(stream))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_norm_fwd")
+    return y, stats
+
+
+def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
+             stats: torch.Tensor, *, rms: bool = False, grad_x: str | torch.Tensor | None = "new",
+             grad_weight: bool | torch.Tensor | None = True,
+             grad_bias: bool | torch.Tensor | None = False, accumulate: bool = False,
+             workspace: NormWorkspace | None = None):
+    """turnkl_norm_bwd on the current stream: the gradients of norm_fwd's input,
+    weight and bias from that of its output.
+
+    stats: norm_fwd's.  grad_x: "new", "inplace" (over grad_y), a tensor of x's
+    shape, or None; grad_weight, grad_bias: True allocates, or a float32 [D]
+    tensor receives, the sums over all rows (accumulate: is added to).  Returns
+    (grad_x, grad_weight, grad_bias), None where not asked for.
+    """
+    dt, n, d, pt = _check_norm(x, ((weight, "weight"),))
+    dev = x.device
+    _rows_like(grad_y, x, "grad_y")
+    if isinstance(grad_x, str):
+        if grad_x not in ("new", "inplace"):
+            raise ValueError(grad_x)
+        grad_x = torch.empty_like(x) if grad_x == "new" else grad_y
+    _rows_like(grad_x, x, "grad_x")
+    sums = []
+    for t, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")):
+        if t is None or isinstance(t, bool):
+            if t and accumulate:
+                raise ValueError(f"accumulate needs a tensor for {name}")
+            t = torch.empty(d, dtype=torch.float32, device=dev) if t else None
+        _need(t, 4 * d, name, dev, torch.float32)
+        sums.append(t)
+    _need(stats, 8 * n, "stats", dev, torch.float32)
+    if workspace is None and (sums[0] is not None or sums[1] is not None):
+        workspace = NormWorkspace(n, d, device=dev)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    rc = lib().turnkl_norm_bwd(
+        _ptr(grad_y), _row_stride(grad_y) if n else d, _ptr(x), _row_stride(x) if n else d, dt, n, d,
+        _ptr(weight), pt, NORM_RMS if rms else NORM_LAYER, _ptr(stats), _ptr(grad_x),
+        (_row_stride(grad_x) if n else d) if grad_x is not None else 0, _ptr(sums[0]), _ptr(sums[1]),
+        int(bool(accumulate)), _ptr(workspace.tensor) if workspace is not None else None,
+        workspace.nbytes if workspace is not None else 0, ctypes.c_void_p(stream))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_norm_bwd")
+    return grad_x, sums[0], sums[1]
 
 
 def new_turn_stats(max_turns: int, device="cuda") -> torch.Tensor:
