@@ -12,29 +12,29 @@
 namespace turnkl {
 namespace {
 
-constexpr int kSumPacks = 2048;  // packs of a row whose columns' sums fit the registers
+constexpr int kNormThreads = 512;               // of a workgroup, at most
+constexpr int kSumPacks = kNormThreads * 4;     // packs of a row whose columns' sums fit the registers
 
-// Sums of kN values over a workgroup, the same in every thread.  `lds` holds
-// 2 x kWaves x kN floats; `turn` alternates from call to call, so that one barrier
-// serves: the other half is rewritten only after the next call's barrier.
-template <int kThreads, int kN>
-__device__ inline void row_sums(float (&v)[kN], float* lds, int& turn) {
-  constexpr int kWaves = kThreads / kWave;
+// Sums of kN values over the threads of a row, the same in each of them.  `lds`
+// holds 2 x kMaxWaves x kN floats; `turn` alternates from call to call, so that one
+// barrier serves: the other half is rewritten only after the next call's barrier.
+constexpr int kMaxWaves = 8;
+template <bool kOneWave, int kN>
+__device__ inline void row_sums(float (&v)[kN], float* lds, int waves, int& turn) {
 #pragma unroll
   for (int i = 0; i < kN; ++i) v[i] = wave_sum(v[i]);
-  if constexpr (kWaves > 1) {
-    float* const s = lds + turn * (kWaves * kN);
+  if constexpr (!kOneWave) {
+    float* const s = lds + turn * (kMaxWaves * kN);
     turn ^= 1;
     if ((threadIdx.x & (kWave - 1)) == 0)
 #pragma unroll
       for (int i = 0; i < kN; ++i) s[(threadIdx.x / kWave) * kN + i] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      v[i] = s[i];
+    for (int i = 0; i < kN; ++i) v[i] = s[i];
+    for (int w = 1; w < waves; ++w)
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v[i] += s[w * kN + i];
-    }
+      for (int i = 0; i < kN; ++i) v[i] += s[w * kN + i];
   }
 }
 
@@ -84,13 +84,17 @@ __device__ inline RowSpan<kBf16, kRagged> row_of(const void* base, long long ld,
   return RowSpan<kBf16, kRagged>{at, chunk_rsrc(at), width, 0, packs};
 }
 
-template <bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
-__global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
+template <bool kBf16, bool kRagged, bool kRms, bool kOneWave, int kPacks>
+__global__ __launch_bounds__(kNormThreads) void norm_fwd_rows(NormParams p) {
   using Span = RowSpan<kBf16, kRagged>;
   using P = typename Span::P;
   constexpr int kEpv = Span::kEpv;
-  __shared__ float s_sum[2 * (kThreads / kWave)];
-  const int tid = threadIdx.x;
+  __shared__ float s_sum[2 * kMaxWaves];
+  const int waves = blockDim.x / kWave;
+  const int threads = kOneWave ? kWave : blockDim.x;            // of a row
+  const int tid = kOneWave ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const int slot = kOneWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0;
+  const long long stride = (long long)gridDim.x * (kOneWave ? waves : 1);
   const int packs = (p.width + kEpv - 1) / kEpv;
   const float width = (float)p.width;
   int at[kPacks], turn = 0;
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
   {
     const Span s = row_of<kBf16, kRagged>(p.x, 0, 0, p.width, packs);
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * kThreads + tid, bits[q]);
+    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * threads + tid, bits[q]);
   }
   float w[kPacks][kEpv], b[kPacks][kEpv];
 #pragma unroll
@@ -113,13 +117,18 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
     for (int q = 0; q < kPacks; ++q)
       if (bits[q]) s.load(next[q], at[q]);
   };
-  long long row = blockIdx.x;
+  // The stores of a row may read their data while the next row is summed: it stays
+  // in registers of its own until then.
+  typename P::Data data[kPacks];
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q) data[q] = P::zero();
+  long long row = kOneWave ? (long long)blockIdx.x * waves + slot : blockIdx.x;
   if (row < p.n_rows) fetch(row);
-  for (; row < p.n_rows; row += gridDim.x) {
+  for (; row < p.n_rows; row += stride) {
     P x[kPacks];
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) x[q] = next[q];
-    if (row + gridDim.x < p.n_rows) fetch(row + gridDim.x);
+    if (row + stride < p.n_rows) fetch(row + stride);
     float mean = 0.0f;
     if constexpr (!kRms) {
       float v[1] = {0.0f};
@@ -129,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
         for (int j = 0; j < kEpv; ++j) v[0] += (bits[q] >> j) & 1u ? x[q].get(j) : 0.0f;
 #pragma unroll
       for (int q = 0; q < kPacks; ++q) x[q].fence();  // unpacked again, rather than kept
-      row_sums<kThreads>(v, s_sum, turn);
+      row_sums<kOneWave>(v, s_sum, waves, turn);
       mean = v[0] / width;
     }
     float v[1] = {0.0f};
@@ -142,10 +151,11 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
       }
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) x[q].fence();
-    row_sums<kThreads>(v, s_sum, turn);
+    row_sums<kOneWave>(v, s_sum, waves, turn);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
     const float rstd = 1.0f / sqrtf(v[0] / width + p.eps);
     const Span out = row_of<kBf16, kRagged>(p.out, p.ld_out, row, p.width, packs);
-    typename P::Data data[kPacks];
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) {
       float y[kEpv];
@@ -159,26 +169,29 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_rows(NormParams p) {
     for (int q = 0; q < kPacks; ++q) out.store_own(data[q], at[q], bits[q]);
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) out.store_whole(data[q], at[q], bits[q]);
-#pragma unroll
-    for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
     if (p.stats && tid == 0) {
       p.stats[2 * row] = mean;
       p.stats[2 * row + 1] = rstd;
     }
-    drain_stores();  // their data registers are free for the next row
   }
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
 }
 
-template <bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
-__global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
+template <bool kBf16, bool kRagged, bool kRms, bool kOneWave, int kPacks>
+__global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
   using Span = RowSpan<kBf16, kRagged>;
   using P = typename Span::P;
   constexpr int kEpv = Span::kEpv;
   // The widest rows fill the registers: there the weights are loaded for every row,
   // no row ahead, and the columns' sums are left to norm_bwd_columns.
-  constexpr bool kLean = kThreads * kPacks > kSumPacks;
-  __shared__ float s_sum[2 * 2 * (kThreads / kWave)];
-  const int tid = threadIdx.x;
+  constexpr bool kLean = kPacks > 4;
+  __shared__ float s_sum[2 * 2 * kMaxWaves];
+  const int waves = blockDim.x / kWave;
+  const int threads = kOneWave ? kWave : blockDim.x;            // of a row
+  const int tid = kOneWave ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const int slot = kOneWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0;
+  const long long stride = (long long)gridDim.x * (kOneWave ? waves : 1);
   const int packs = (p.width + kEpv - 1) / kEpv;
   const float width = (float)p.width;
   int at[kPacks], turn = 0;
@@ -186,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
   {
     const Span s = row_of<kBf16, kRagged>(p.x, 0, 0, p.width, packs);
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * kThreads + tid, bits[q]);
+    for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * threads + tid, bits[q]);
   }
   float w[kLean ? 1 : kPacks][kEpv], gw[kLean ? 1 : kPacks][kEpv], gb[kLean ? 1 : kPacks][kEpv];
   if constexpr (!kLean)
@@ -204,6 +217,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
       gb[q][j] = 0.0f;
     }
   P next_x[kPacks], next_g[kPacks];
+  float next_mean = 0.0f, next_rstd = 0.0f;
   auto fetch = [&](long long row) {
     const Span sx = row_of<kBf16, kRagged>(p.x, p.ld_x, row, p.width, packs);
     const Span sg = row_of<kBf16, kRagged>(p.gy, p.ld_gy, row, p.width, packs);
@@ -213,10 +227,15 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
       sx.load(next_x[q], at[q]);
       sg.load(next_g[q], at[q]);
     }
+    if constexpr (!kRms) next_mean = p.stats[2 * row];
+    next_rstd = p.stats[2 * row + 1];
   };
-  long long row = blockIdx.x;
+  typename P::Data data[kPacks];  // as in norm_fwd_rows
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q) data[q] = P::zero();
+  long long row = kOneWave ? (long long)blockIdx.x * waves + slot : blockIdx.x;
   if (!kLean && row < p.n_rows) fetch(row);
-  for (; row < p.n_rows; row += gridDim.x) {
+  for (; row < p.n_rows; row += stride) {
     if constexpr (kLean) fetch(row);
     P x[kPacks], g[kPacks];
 #pragma unroll
@@ -224,9 +243,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
       x[q] = next_x[q];
       g[q] = next_g[q];
     }
-    const float mean = kRms ? 0.0f : p.stats[2 * row];
-    const float rstd = p.stats[2 * row + 1];
-    if (!kLean && row + gridDim.x < p.n_rows) fetch(row + gridDim.x);
+    const float mean = next_mean, rstd = next_rstd;
+    if (!kLean && row + stride < p.n_rows) fetch(row + stride);
     float v[2] = {0.0f, 0.0f};  // sums of q xh and q
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) {
@@ -250,11 +268,12 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
       x[q].fence();
       g[q].fence();
     }
-    row_sums<kThreads>(v, s_sum, turn);
+    row_sums<kOneWave>(v, s_sum, waves, turn);
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
     if (p.out) {
       const float c1 = v[0] / width, c0 = v[1] / width;
       const Span out = row_of<kBf16, kRagged>(p.out, p.ld_out, row, p.width, packs);
-      typename P::Data data[kPacks];
 #pragma unroll
       for (int q = 0; q < kPacks; ++q) {
         float d[kEpv];
@@ -276,16 +295,46 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_rows(NormParams p) {
       drain_stores();  // their data registers are free for the next row
     }
   }
-  if (!kLean && p.part) {
+  if constexpr (!kLean) {
+    if (!p.part) return;
     float* const part = p.part + (long long)blockIdx.x * 2 * p.width;
+    if constexpr (kOneWave) {
+      // the waves' sums one after the other
+      __shared__ float s_col[kWave * kPacks * kEpv];
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q)
+      for (int which = 0; which < 2; ++which) {
+        if (!(which ? p.gb : p.gw)) continue;
+        for (int w = 0; w < waves; ++w) {
+          if (w == slot)
 #pragma unroll
-      for (int j = 0; j < kEpv; ++j) {
-        if (!((bits[q] >> j) & 1u)) continue;
-        if (p.gw) part[at[q] + j] = gw[kLean ? 0 : q][j];
-        if (p.gb) part[p.width + at[q] + j] = gb[kLean ? 0 : q][j];
+            for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+              for (int j = 0; j < kEpv; ++j) {
+                const int i = (q * kEpv + j) * kWave + tid;
+                const float v = which ? gb[q][j] : gw[q][j];
+                s_col[i] = w ? s_col[i] + v : v;
+              }
+          __syncthreads();
+        }
+        if (slot == 0)
+#pragma unroll
+          for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+            for (int j = 0; j < kEpv; ++j)
+              if ((bits[q] >> j) & 1u)
+                part[which * p.width + at[q] + j] = s_col[(q * kEpv + j) * kWave + tid];
+        __syncthreads();
       }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+        for (int j = 0; j < kEpv; ++j) {
+          if (!((bits[q] >> j) & 1u)) continue;
+          if (p.gw) part[at[q] + j] = gw[q][j];
+          if (p.gb) part[p.width + at[q] + j] = gb[q][j];
+        }
+    }
   }
 }
 
@@ -310,59 +359,103 @@ __global__ __launch_bounds__(kColumnThreads) void norm_bwd_columns(NormParams p)
   if (p.gb) part[p.width + col] = gb;
 }
 
-// Adds the workgroups' column sums, in their order: 64 columns a workgroup, four
-// runs of partial rows side by side.
-constexpr int kJoinThreads = 256;
+// Adds the workgroups' column sums in their order: 64 columns a workgroup, sixteen
+// runs of partial rows side by side (blockIdx.y: the weight's sums or the bias's).
+constexpr int kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join(NormParams p) {
-  __shared__ float s_run[kJoinThreads / kWave][kWave];
+  constexpr int kRuns = kJoinThreads / kWave;
+  __shared__ float s_run[kRuns][kWave];
   const int lane = threadIdx.x & (kWave - 1);
   const int run = threadIdx.x / kWave;
-  constexpr int kRuns = kJoinThreads / kWave;
   const int col = blockIdx.x * kWave + lane;
-  for (int which = 0; which < 2; ++which) {
-    float* const out = which ? p.gb : p.gw;
-    if (!out) continue;
-    float s = 0.0f;
-    if (col < p.width) {
-      const float* at = p.part + (long long)which * p.width + col;
-      const int lo = p.n_groups * run / kRuns, hi = p.n_groups * (run + 1) / kRuns;
-      for (int i = lo; i < hi; ++i) s += at[(long long)i * 2 * p.width];
-    }
-    s_run[run][lane] = s;
-    __syncthreads();
-    if (run == 0 && col < p.width) {
-      float t = s_run[0][lane];
+  float* const out = blockIdx.y ? p.gb : p.gw;
+  if (!out) return;
+  float s = 0.0f;
+  if (col < p.width) {
+    const float* at = p.part + (long long)blockIdx.y * p.width + col;
+    const int lo = p.n_groups * run / kRuns, hi = p.n_groups * (run + 1) / kRuns;
+#pragma unroll 8
+    for (int i = lo; i < hi; ++i) s += at[(long long)i * 2 * p.width];
+  }
+  s_run[run][lane] = s;
+  __syncthreads();
+  if (run == 0 && col < p.width) {
+    float t = s_run[0][lane];
 #pragma unroll
-      for (int r = 1; r < kRuns; ++r) t += s_run[r][lane];
-      out[col] = p.accumulate ? out[col] + t : t;
-    }
-    __syncthreads();
+    for (int r = 1; r < kRuns; ++r) t += s_run[r][lane];
+    out[col] = p.accumulate ? out[col] + t : t;
   }
 }
 
-constexpr int kNormGrid = 2048;    // workgroups that go from row to row
-constexpr int kNormGroups = 1024;  // the same backward: each leaves a partial sum
+// How rows of a width are laid out over the threads, and how many workgroups go from
+// row to row.
+struct NormShape {
+  bool one_wave;  // a wave per row, four or eight rows side by side in a workgroup
+  int packs;      // of a thread
+  int threads;    // of a workgroup
+  int rows;       // side by side in a workgroup
+  int groups;     // workgroups that fill the card
+};
 
-template <bool kBwd, bool kBf16, bool kRagged, bool kRms, int kThreads, int kPacks>
-void launch_one(const NormParams& p, hipStream_t s) {
-  if constexpr (kBwd) {
-    norm_bwd_rows<kBf16, kRagged, kRms, kThreads, kPacks><<<p.n_groups, kThreads, 0, s>>>(p);
+// Rows of up to 128 packs (backward 256) take one wave, which needs no barrier:
+// 65,536 bf16 rows of 2,048 backward (root mean square) take 144 us with four packs
+// a lane and four rows a workgroup, 145 to 153 with two or four waves to a row; of
+// 512, 45 us with eight rows a workgroup, 48 with four, 54 with two.  Wider rows take
+// two packs a thread while 512 threads suffice (65,536 of 4,096 backward: 300 us, with
+// four packs 310, with one 320), then four, and eight for fp32 rows past 8,192.
+// The workgroups are those that the registers let the card hold at once, 16 waves a
+// CU up to two packs and eight beyond: more would wait for the first to end, and
+// backward would leave more partial sums (8,192 rows of 16,384: 228 us with 256, 247
+// with 512, 292 with 1,024; 65,536 of 4,096: 322 with 512, 300 with 1,024, 315 with
+// 2,048).
+NormShape norm_shape(long long width, int epv, bool bwd) {
+  const int packs = (int)((width + epv - 1) / epv);
+  NormShape s{};
+  s.one_wave = packs <= (bwd ? 256 : 128);
+  if (s.one_wave) {
+    s.packs = packs <= 64 ? 1 : packs <= 128 ? 2 : 4;
+    s.rows = bwd && s.packs < 4 ? 8 : 4;
+    s.threads = s.rows * kWave;
   } else {
-    const int grid = p.n_rows < kNormGrid ? p.n_rows : kNormGrid;
-    norm_fwd_rows<kBf16, kRagged, kRms, kThreads, kPacks><<<grid, kThreads, 0, s>>>(p);
+    s.packs = packs <= 2 * kNormThreads ? 2 : packs <= kSumPacks ? 4 : 8;
+    s.rows = 1;
+    s.threads = ((packs + s.packs - 1) / s.packs + kWave - 1) / kWave * kWave;
   }
+  const int per_cu = (s.packs <= 2 ? 16 : 8) / (s.threads / kWave);
+  s.groups = 256 * (per_cu < 1 ? 1 : per_cu);
+  return s;
+}
+
+// Workgroups for a number of rows: backward every wave takes two rows at least, so
+// that small batches leave fewer partial sums.
+int groups_of(const NormShape& s, long long n_rows, bool bwd) {
+  const long long per = (bwd ? 2 : 1) * s.rows;
+  const long long g = (n_rows + per - 1) / per;
+  return (int)(g < 1 ? 1 : g < s.groups ? g : s.groups);
+}
+
+template <bool kBwd, bool kBf16, bool kRagged, bool kRms, bool kOneWave, int kPacks>
+void launch_one(const NormParams& p, const NormShape& n, hipStream_t s) {
+  if constexpr (kBwd)
+    norm_bwd_rows<kBf16, kRagged, kRms, kOneWave, kPacks><<<p.n_groups, n.threads, 0, s>>>(p);
+  else
+    norm_fwd_rows<kBf16, kRagged, kRms, kOneWave, kPacks>
+        <<<groups_of(n, p.n_rows, false), n.threads, 0, s>>>(p);
 }
 
 template <bool kBwd, bool kBf16, bool kRagged, bool kRms>
 void launch_sized(const NormParams& p, hipStream_t s) {
-  const int epv = kBf16 ? 8 : 4;
-  const int packs = (p.width + epv - 1) / epv;
-  if (packs <= 64) launch_one<kBwd, kBf16, kRagged, kRms, 64, 1>(p, s);
-  else if (packs <= 256) launch_one<kBwd, kBf16, kRagged, kRms, 256, 1>(p, s);
-  else if (packs <= 512) launch_one<kBwd, kBf16, kRagged, kRms, 256, 2>(p, s);
-  else if (packs <= 1024) launch_one<kBwd, kBf16, kRagged, kRms, 512, 2>(p, s);
-  else if (packs <= kSumPacks) launch_one<kBwd, kBf16, kRagged, kRms, 512, 4>(p, s);
-  else if constexpr (!kBf16) launch_one<kBwd, kBf16, kRagged, kRms, 512, 8>(p, s);
+  const NormShape n = norm_shape(p.width, kBf16 ? 8 : 4, kBwd);
+  if (n.one_wave && n.packs == 1) launch_one<kBwd, kBf16, kRagged, kRms, true, 1>(p, n, s);
+  else if (n.one_wave && n.packs == 2) launch_one<kBwd, kBf16, kRagged, kRms, true, 2>(p, n, s);
+  else if (n.packs == 2) launch_one<kBwd, kBf16, kRagged, kRms, false, 2>(p, n, s);
+  else if (!n.one_wave && n.packs == 4) launch_one<kBwd, kBf16, kRagged, kRms, false, 4>(p, n, s);
+  else if constexpr (kBwd) {
+    if (n.one_wave) launch_one<kBwd, kBf16, kRagged, kRms, true, 4>(p, n, s);
+    else if constexpr (!kBf16) launch_one<kBwd, kBf16, kRagged, kRms, false, 8>(p, n, s);
+  } else if constexpr (!kBf16) {
+    launch_one<kBwd, kBf16, kRagged, kRms, false, 8>(p, n, s);
+  }
 }
 
 template <bool kBwd>
@@ -378,10 +471,8 @@ void launch_norm(const NormParams& p, hipStream_t s) {
 
 }  // namespace
 
-int norm_groups(long long n_rows, long long width) {
-  (void)width;
-  const long long g = (n_rows + 7) / 8;  // eight rows a workgroup at least
-  return (int)(g < 1 ? 1 : g < kNormGroups ? g : kNormGroups);
+int norm_groups(long long n_rows, long long width, bool bf16) {
+  return groups_of(norm_shape(width, bf16 ? 8 : 4, true), n_rows, true);
 }
 
 hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s) {
@@ -400,7 +491,7 @@ hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s) {
   launch_norm<true>(p, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (!sums) return hipSuccess;
-  norm_bwd_join<<<(p.width + kWave - 1) / kWave, kJoinThreads, 0, s>>>(p);
+  norm_bwd_join<<<dim3((p.width + kWave - 1) / kWave, p.gb ? 2 : 1), kJoinThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -207,7 +207,8 @@ int turnkl_norm_fwd(const void* x, int64_t ld_x, int dtype, int64_t n_rows, int6
 
 size_t turnkl_norm_workspace_bytes(int64_t n_rows, int64_t width) {
   if (n_rows < 0 || n_rows > 0x7FFFFFFFll || width < 1 || width > TURNKL_MAX_NORM_WIDTH) return 0;
-  return align256((size_t)norm_groups(n_rows, width) * 2 * (size_t)width * sizeof(float));
+  const int b = norm_groups(n_rows, width, true), f = norm_groups(n_rows, width, false);
+  return align256((size_t)(b > f ? b : f) * 2 * (size_t)width * sizeof(float));
 }
 
 int turnkl_norm_bwd(const void* grad_y, int64_t ld_gy, const void* x, int64_t ld_x, int dtype,
@@ -258,8 +259,8 @@ int turnkl_norm_bwd(const void* grad_y, int64_t ld_gy, const void* x, int64_t ld
   p.ld_out = ld_gx;
   p.n_rows = (int)n_rows;
   p.width = (int)width;
-  p.n_groups = norm_groups(n_rows, width);
   p.bf16 = dtype == TURNKL_BF16;
+  p.n_groups = norm_groups(n_rows, width, p.bf16 != 0);
   p.param_bf16 = param_dtype == TURNKL_BF16;
   p.rms = kind == TURNKL_NORM_RMS;
   p.accumulate = accumulate != 0;

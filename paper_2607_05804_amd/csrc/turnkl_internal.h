@@ -451,7 +451,7 @@ struct NormParams {
   int accumulate;
 };
 
-int norm_groups(long long n_rows, long long width);
+int norm_groups(long long n_rows, long long width, bool bf16);
 hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s);
 hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s);
 
