@@ -28,6 +28,45 @@ __device__ inline T wave_max(T v) {
   return v;
 }
 
+// The same by data-parallel moves between lanes (rows of 16 by shifts, then the
+// rows' last lanes broadcast), without going through LDS; in a fixed order of its
+// own.  Every lane receives the result.
+template <int kCtrl, int kRows>
+__device__ inline float lane_move(float v, float fill) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(fill), __float_as_uint(v), kCtrl,
+                                                     kRows, 0xF, false));
+}
+template <typename F>
+__device__ inline float wave_reduce_dpp(float v, float none, F op) {
+  v = op(v, lane_move<0x111, 0xF>(v, none));  // row_shr:1, 2, 4, 8
+  v = op(v, lane_move<0x112, 0xF>(v, none));
+  v = op(v, lane_move<0x114, 0xF>(v, none));
+  v = op(v, lane_move<0x118, 0xF>(v, none));
+  v = op(v, lane_move<0x142, 0xA>(v, none));  // row_bcast:15 into rows 1 and 3
+  v = op(v, lane_move<0x143, 0xC>(v, none));  // row_bcast:31 into rows 2 and 3
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), kWave - 1));
+}
+__device__ inline float wave_sum_dpp(float v) {
+  return wave_reduce_dpp(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ inline float wave_max_dpp(float v) {
+  return wave_reduce_dpp(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The numbers of the lanes before this one, added; *total gets the wave's sum.  All
+// lanes call it.
+__device__ inline int wave_exclusive_dpp(int v, int* total) {
+  int s = v;
+  s += __builtin_amdgcn_update_dpp(0, s, 0x111, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x112, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x114, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x118, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x142, 0xA, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x143, 0xC, 0xF, false);
+  *total = __builtin_amdgcn_readlane(s, kWave - 1);
+  return s - v;
+}
+
 __device__ inline unsigned long long wave_min_u64(unsigned long long v) {
 #pragma unroll
   for (int o = kWave / 2; o > 0; o >>= 1) {

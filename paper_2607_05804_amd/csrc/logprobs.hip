@@ -3,16 +3,19 @@
 //
 // Math.  With M = max z, S = sum 2^x, A = sum 2^x x over x = (z - M) log2 e:
 //   L = ln S,  H = L - ln2 A / S,  log p_v = (z_v - M) - L.
-// A wave sums against a reference of its own that follows the maximum: it moves
-// (and the sums with it) when a group of packs holds a logit more than kSlack
-// above it, so that no sum overflows and no second pass is needed; A / S then
-// cancels a few units at most.  A is summed over max(x, kFloor): a forbidden
-// token (-inf) gives 0 * kFloor, not 0 * -inf.
+// A wave sums against a reference r of its own that follows the maximum, with
+// x = fma(z, log2 e, -r): r is any float, the product is not rounded, and r is set
+// against M log2 e in the same way when the waves are joined, so that no error of
+// r enters.  The reference moves (and the sums with it) when a lane meets a logit
+// more than kSlack above it, so that no sum overflows and no second pass is needed;
+// A / S then cancels a few units at most.  A is summed over max(x, kFloor): a
+// forbidden token (-inf) gives 0 * kFloor, not 0 * -inf.  Rows beyond the reach of
+// that (|M| > kHuge, NaN, +inf) are summed again against their exact maximum.
 //
 // Alternatives.  Ranking works on 64-bit numbers that order logits and ids at
 // once: the logit's bits, made monotone, above the complement of its id.  While
 // the row streams by, each thread keeps its largest logit, and the upper 16 bits
-// of the largest of every eight elements (a unit) go to LDS.  The k-th largest of
+// of the largest of every sixteen elements (a unit) go to LDS.  The k-th largest of
 // the threads' maxima is a bound that at least k elements reach, and few more do
 // (about 56 for k = 50 and 256 threads when the large ones are spread evenly).
 // Only the units that reach it are read again, and the elements that do are
@@ -29,13 +32,13 @@ namespace {
 
 constexpr int kLpThreads = 256;
 constexpr int kLpWaves = kLpThreads / kWave;
-constexpr int kLpPacks = 4;        // packs in flight per lane
-constexpr int kLpGrid = 1 << 22;   // workgroups; beyond, each takes several tasks
-constexpr float kSlack = 8.0f;     // logit units
-constexpr float kFloor = -256.0f;  // log2 units: 2^kFloor is zero
-constexpr int kStep = 128;                            // packs looked at again at a time
-constexpr int kCand = kMaxAlternatives + kStep * 8;   // elements held for ranking
-constexpr int kList = 512;                            // units held for a second look
+constexpr int kGroupElems = 32 * kLpThreads;  // elements of a group: 32 a lane
+__host__ __device__ constexpr int group_packs(bool bf16) { return bf16 ? 4 : 8; }  // a lane's packs of it
+constexpr float kSlack = 8.0f;           // logit units
+constexpr float kFloor = -256.0f;        // log2 units: 2^kFloor is zero
+constexpr float kHuge = 1e38f;           // log2 e times it is a float still
+constexpr int kCand = 896;        // elements held for ranking: k and a step's, at least
+constexpr int kList = 384;         // units held for a second look
 
 // The logit's bits in an order of unsigned numbers (-0 and +0 alike, NaN as -inf).
 __device__ inline unsigned order_of(float z) {
@@ -49,95 +52,133 @@ __device__ inline unsigned long long ranked(unsigned order, int id) {
   return ((unsigned long long)order << 32) | (unsigned)~id;
 }
 
+// Maxima in one instruction each (the compiler's would quiet signalling NaNs with
+// one more per operand; here a number beside one may be lost, which a row with NaN
+// never uses).
+__device__ inline float max2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // The largest t with at least k of a wave's kPer numbers per lane >= t (0 if
-// there are fewer): the k-th largest, bit by bit.
-template <int kPer>
+// there are fewer), its kLow lowest bits zero: the k-th largest, two bits at a time.
+template <int kLow, int kPer>
 __device__ inline unsigned kth_largest(const unsigned (&v)[kPer], int k) {
   unsigned t = 0;
 #pragma unroll 1
-  for (int b = 31; b >= 0; --b) {
-    const unsigned c = t | (1u << b);
-    int n = 0;
+  for (int b = 30; b >= kLow; b -= 2) {
+    int n[3] = {0, 0, 0};
 #pragma unroll
-    for (int q = 0; q < kPer; ++q) n += __popcll(__ballot(v[q] >= c));
-    if (n >= k) t = c;
+    for (int q = 0; q < kPer; ++q)
+#pragma unroll
+      for (unsigned d = 0; d < 3; ++d) n[d] += __popcll(__ballot(v[q] >= (t | ((d + 1) << b))));
+    t |= (n[2] >= k ? 3u : n[1] >= k ? 2u : n[0] >= k ? 1u : 0u) << b;
   }
   return t;
 }
 
-// The workgroup's list of candidates.  All threads call every function.
+// The workgroup's list of candidates.  All threads call every function, with the
+// list complete.
+constexpr int kRankers = 4;   // lanes that rank one candidate
+constexpr int kRankTurn = 8;  // numbers a lane compares with at a time
+constexpr int kRankPad = kRankers * kRankTurn;
 struct Best {
-  unsigned long long* cand;  // LDS, kCand
-  int* n;                    // LDS
+  unsigned long long* cand;   // LDS, kCand + kRankPad
+  unsigned long long* kept;   // LDS, kMaxAlternatives
+  int* n;                     // LDS
   unsigned long long* floor;  // LDS: numbers below it are out
 
-  // the rank of each of this thread's candidates tid, tid + 256, ...
-  static constexpr int kMine = (kCand + kLpThreads - 1) / kLpThreads;
-  __device__ void ranks(int count, unsigned long long (&x)[kMine], int (&r)[kMine]) const {
+  // Hands every candidate's number and rank among `count` to use(), in one thread
+  // each: four lanes compare it with a quarter of the list each.  One barrier.
+  template <typename F>
+  __device__ void ranks(int count, F use) const {
+    if (threadIdx.x < kRankPad) cand[count + threadIdx.x] = 0ull;
+    __syncthreads();
+    const int part = threadIdx.x % kRankers;
+    for (int i = threadIdx.x / kRankers; i < count; i += kLpThreads / kRankers) {
+      const unsigned long long x = cand[i];
+      int r = 0;
+      for (int j = part; j < count; j += kRankPad) {
+        unsigned long long c[kRankTurn];
 #pragma unroll
-    for (int q = 0; q < kMine; ++q) {
-      const int i = threadIdx.x + q * kLpThreads;
-      x[q] = i < count ? cand[i] : 0ull;
-      r[q] = 0;
-    }
-    const int mine = (count + kLpThreads - 1) / kLpThreads;
-#pragma unroll 4
-    for (int j = 0; j < count; ++j) {
-      const unsigned long long c = cand[j];
-      r[0] += c > x[0];
+        for (int q = 0; q < kRankTurn; ++q) c[q] = cand[j + q * kRankers];
 #pragma unroll
-      for (int q = 1; q < kMine; ++q)
-        if (q < mine) r[q] += c > x[q];
+        for (int q = 0; q < kRankTurn; ++q) r += c[q] > x;
+      }
+      r += __shfl_xor(r, 1, kWave);
+      r += __shfl_xor(r, 2, kWave);
+      if (part == 0) use(x, r);
     }
   }
-  // keeps the k best and raises the floor above the k-th
-  __device__ void cut(int k) {
-    unsigned long long x[kMine];
-    int r[kMine];
-    const int count = *n;
-    ranks(count, x, r);
+  // Keeps the k best of `count` and raises the floor above the k-th.
+  __device__ void cut(int count, int k) {
+    ranks(count, [&](unsigned long long x, int r) {
+      if (r >= k) return;
+      kept[r] = x;
+      if (r == k - 1) *floor = x + 1ull;
+    });
     __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kMine; ++q) {
-      if (x[q] == 0ull || r[q] >= k) continue;
-      cand[r[q]] = x[q];
-      if (r[q] == k - 1) *floor = x[q] + 1ull;
-    }
+    for (int i = threadIdx.x; i < k && i < count; i += kLpThreads) cand[i] = kept[i];
     if (threadIdx.x == 0) *n = count < k ? count : k;
     __syncthreads();
   }
 };
 
-// What a row's outputs need once its maximum and sums are known.
+// The given token of a row and its logit, read while the row streams by.
+struct Given {
+  int id;
+  bool in;
+  float z;
+};
+__device__ inline Given given_of(const LogprobParams& p, long long row) {
+  Given g{0, false, __builtin_nanf("")};
+  if (!p.ids) return g;
+  g.id = p.ids[row];
+  g.in = g.id >= 0 && g.id < p.vocab;
+  if (g.in && p.logp) {
+    const long long at = row * p.ld + g.id;
+    g.z = p.bf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
+                 : static_cast<const float*>(p.z)[at];
+  }
+  return g;
+}
+
+// L of a row: 0 for one of nothing but -inf.
+__device__ inline float log_sum(float m, float s) {
+  return m == -INFINITY && s == 0.0f ? 0.0f : kLn2 * log2f(s);
+}
+
+// One thread writes a row's outputs but the alternatives.
 __device__ inline void write_row(const LogprobParams& p, long long row, float m, float s, float a,
-                                 float* s_row) {
+                                 const Given& g) {
   const bool empty = m == -INFINITY && s == 0.0f;
-  const float l = empty ? 0.0f : kLn2 * log2f(s);
-  s_row[0] = m;
-  s_row[1] = l;
+  const float l = log_sum(m, s);
   if (p.entropy) p.entropy[row] = empty ? 0.0f : l - kLn2 * (a / s);
   if (p.log_z) {
     p.log_z[2 * row] = m;
     p.log_z[2 * row + 1] = l;
   }
-  if (p.ids) {
-    const int t = p.ids[row];
-    const bool in = t >= 0 && t < p.vocab;
-    if (!in) atomicMin(&p.hdr->err_key, err_key(row, kPrioTokenId));
-    if (p.logp) {
-      float z = __builtin_nanf("");
-      if (in) {
-        const long long at = row * p.ld + t;
-        z = p.bf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
-                   : static_cast<const float*>(p.z)[at];
-      }
-      p.logp[row] = empty && in ? -INFINITY : (z - m) - l;
-    }
-  }
+  if (p.ids && !g.in) atomicMin(&p.hdr->err_key, err_key(row, kPrioTokenId));
+  if (p.logp) p.logp[row] = empty && g.in ? -INFINITY : (g.z - m) - l;
 }
 
-__device__ inline void write_masked_row(const LogprobParams& p, long long row) {
-  if (threadIdx.x == 0) {
+__device__ inline void write_alternative(const LogprobParams& p, long long row, int rank,
+                                         unsigned long long x, float m, float l) {
+  const float z = logit_of((unsigned)(x >> 32));
+  p.top_ids[row * p.ld_top + rank] = (int)~(unsigned)x;
+  // -inf - -inf is -inf here, but rows of NaN say so everywhere
+  p.top_logp[row * p.ld_top + rank] = z == -INFINITY && l == l ? -INFINITY : (z - m) - l;
+}
+
+// A row that is not asked for, by the `n` threads that call with i = 0 .. n - 1.
+__device__ inline void write_masked_row(const LogprobParams& p, long long row, int i, int n) {
+  if (i == 0) {
     if (p.logp) p.logp[row] = 0.0f;
     if (p.entropy) p.entropy[row] = 0.0f;
     if (p.log_z) {
@@ -145,29 +186,13 @@ __device__ inline void write_masked_row(const LogprobParams& p, long long row) {
       p.log_z[2 * row + 1] = __builtin_nanf("");
     }
   }
-  for (int j = threadIdx.x; j < p.k; j += kLpThreads) {
+  for (int j = i; j < p.k; j += n) {
     p.top_ids[row * p.ld_top + j] = -1;
     p.top_logp[row * p.ld_top + j] = -INFINITY;
   }
 }
 
-// Ranks the candidates and writes the row's alternatives.
-__device__ inline void write_top(const LogprobParams& p, long long row, const Best& best, float m,
-                                 float l) {
-  unsigned long long x[Best::kMine];
-  int r[Best::kMine];
-  best.ranks(*best.n, x, r);
-#pragma unroll
-  for (int q = 0; q < Best::kMine; ++q) {
-    if (x[q] == 0ull || r[q] >= p.k) continue;
-    const float z = logit_of((unsigned)(x[q] >> 32));
-    p.top_ids[row * p.ld_top + r[q]] = (int)~(unsigned)x[q];
-    // NaN rows say so everywhere; -inf - -inf is -inf here
-    p.top_logp[row * p.ld_top + r[q]] = z == -INFINITY && l == l ? -INFINITY : (z - m) - l;
-  }
-}
-
-// The join of waves' or chunks' sums against their own references.
+// Chunks' sums, each against its own maximum, joined against the row's.
 struct Sums {
   float m, s, a;
 };
@@ -183,115 +208,181 @@ __device__ inline void add_part(Sums& t, float m, float s, float a) {
   t.a = fmaf(f, fmaf(s, f == 0.0f ? 0.0f : d, a), t.a);
 }
 
-__global__ void logprob_begin(Header* hdr) { hdr->err_key = kNoError; }
+// Clears the status; with a mask, lists the rows that are asked for, in order.
+constexpr int kBeginThreads = 1024;
+__global__ __launch_bounds__(kBeginThreads) void logprob_begin(LogprobParams p) {
+  if (threadIdx.x == 0) p.hdr->err_key = kNoError;
+  if (!p.rows) return;
+  __shared__ int s_scan[kBeginThreads / kWave];
+  constexpr int kEach = 16;  // rows of a thread and turn
+  int done = 0;
+  for (long long base = 0; base < p.n_rows; base += kBeginThreads * kEach) {
+    const long long first = base + (long long)threadIdx.x * kEach;
+    unsigned on = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (first + j < p.n_rows && p.mask[first + j]) on |= 1u << j;
+    int total;
+    int at = done + block_exclusive_scan<kBeginThreads>(__popc(on), s_scan, &total);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if ((on >> j) & 1u) p.rows[at++] = (int)(first + j);
+    done += total;
+  }
+  if (threadIdx.x == 0) p.hdr->n_sup = done;
+}
 
-// One workgroup per chunk of a row.
+// One chunk of a row after the other (task = row of the list x chunk), by workgroups
+// that fill the card.
 template <bool kBf16, bool kRagged, bool kTop>
 __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
-  constexpr int kEpv = kBf16 ? 8 : 4;
-  constexpr int kEs = kBf16 ? 2 : 4;
-  constexpr int kUnitPacks = 8 / kEpv;                      // packs of a unit
-  constexpr int kWords = kLpPacks / (2 * kUnitPacks);       // LDS words of a group: two units each
-  constexpr int kStepBytes = kLpThreads * 16;
-  using P = Pack<kBf16, kEpv>;
+  constexpr int kLpPacks = group_packs(kBf16);
+  using Span = RowSpan<kBf16, kRagged>;
+  using P = typename Span::P;
+  constexpr int kEpv = Span::kEpv;
+  constexpr int kEs = Span::kEs;
+  constexpr int kUnitPacks = kLpPacks / 2;  // packs of a unit: a group is two, in one LDS word
+  constexpr int kGroup = kLpThreads * kLpPacks;        // packs of a group
   extern __shared__ unsigned s_unit[];
   __shared__ float s_wave[kLpWaves][4];
-  __shared__ float s_row[2];
   __shared__ unsigned s_max[kLpThreads];
-  __shared__ unsigned long long s_cand[kCand];
+  __shared__ unsigned long long s_cand[kCand + kRankPad];
+  __shared__ unsigned long long s_kept[kMaxAlternatives];
   __shared__ unsigned long long s_floor;
   __shared__ int s_list[kList];
   __shared__ int s_n, s_units;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const long long n_tasks = (long long)p.n_rows * p.n_chunks;
-  for (long long task = blockIdx.x; task < n_tasks; task += gridDim.x) {
-    const long long row = task / p.n_chunks;
-    const int c = (int)(task - row * p.n_chunks);
-    if (p.mask && !p.mask[row]) {
-      if (c == 0) write_masked_row(p, row);
-      continue;
+  const long long count = p.rows ? p.hdr->n_sup : p.n_rows;
+
+  if (p.mask)  // the rows that are not asked for
+    for (long long base = blockIdx.x; base < p.n_rows; base += (long long)gridDim.x * kWave) {
+      const long long row = base + (long long)lane * gridDim.x;
+      unsigned long long off = __ballot(row < p.n_rows && !p.mask[row < p.n_rows ? row : 0]);
+      for (; off; off &= off - 1)
+        write_masked_row(p, base + (long long)(__ffsll((long long)off) - 1) * gridDim.x, tid, kLpThreads);
     }
-    // packs [lo, hi) of the row; ragged rows: on the grid of 128-byte lines
-    const char* const at_row = static_cast<const char*>(p.z) + row * p.ld * kEs;
-    const int pre = kRagged ? (int)(reinterpret_cast<uintptr_t>(at_row) & 127u) / kEs : 0;
+
+  // A task: a chunk of a row, packs [lo, lo + n) of it (of ragged rows on the grid of
+  // 128-byte lines); g0 to g1: its groups of whole packs that lie in the row, all but
+  // the last, and of ragged rows all but the first.
+  struct Task {
+    Span span;
+    int groups, g0, g1;
+  };
+  auto task_of = [&](long long row, int c) {
+    const char* const at = static_cast<const char*>(p.z) + row * p.ld * kEs;
+    const int pre = kRagged ? (int)(reinterpret_cast<uintptr_t>(at) & 127u) / kEs : 0;
     const int n_row = (int)(((long long)pre + p.vocab + kEpv - 1) / kEpv);
     const int lo = (int)chunk_start(n_row, p.n_chunks, 8, c);
     const int n = (int)chunk_start(n_row, p.n_chunks, 8, c + 1) - lo;
-    const int col = lo * kEpv - pre;  // first element of the chunk
-    const RowSpan<kBf16, kRagged> span{at_row, chunk_rsrc(at_row), p.vocab, col, n};
-    const int groups = (n + kLpThreads * kLpPacks - 1) / (kLpThreads * kLpPacks);
+    const int groups = (n + kGroup - 1) / kGroup;
+    return Task{Span{at, chunk_rsrc(at), p.vocab, lo * kEpv - pre, n}, groups, kRagged ? 1 : 0,
+                kRagged ? groups - 1 : n / kGroup};
+  };
+  auto row_of = [&](long long task) -> long long {
+    return p.rows ? p.rows[task / p.n_chunks] : task / p.n_chunks;
+  };
+  P next[kLpPacks];  // the group that comes next, of this task or the next one
+  auto fetch = [&](const Task& of, int g) {
+    if (g >= of.g1) return;
+#pragma unroll
+    for (int q = 0; q < kLpPacks; ++q)
+      next[q].load(of.span.rsrc, tid * 16, of.span.col * kEs + (g * kLpPacks + q) * (kLpThreads * 16));
+  };
+  const long long n_tasks = count * p.n_chunks;
+  long long task = blockIdx.x;
+  if (task >= n_tasks) return;
+  long long row = row_of(task);
+  Task now = task_of(row, (int)(task % p.n_chunks));
+  fetch(now, now.g0);
+  for (;;) {
+    const int c = (int)(task % p.n_chunks);
+    const bool more = task + gridDim.x < n_tasks;
+    const long long next_row = more ? row_of(task + gridDim.x) : 0;
+    const Given given = p.n_chunks == 1 ? given_of(p, row) : Given{};
+    const Span& span = now.span;
+    const int n = span.n, groups = now.groups;
 
-    float ref = -INFINITY, ss = 0.0f, aa = 0.0f;  // the wave's reference and lane sums
-    float best = -INFINITY;                       // the lane's largest logit
-    auto group = [&](int g, auto edge) {
+    float ref = -kHuge, ss = 0.0f, aa = 0.0f;  // the wave's reference and lane sums
+    float best = -INFINITY;                            // the lane's largest logit
+    auto sums = [&](int g, const P (&x)[kLpPacks], const unsigned (&bits)[kLpPacks], auto edge) {
       constexpr bool kEdge = decltype(edge)::value;
-      P x[kLpPacks];
-      unsigned bits[kLpPacks];
+      float z[kLpPacks][kEpv];
 #pragma unroll
-      for (int q = 0; q < kLpPacks; ++q) {
-        const int v = g * kLpPacks + q;
-        if constexpr (kEdge) {
-          const int at = span.place(v * kLpThreads + tid, bits[q]);
-          span.load(x[q], at);
-        } else {
-          x[q].load(span.rsrc, tid * 16, col * kEs + v * kStepBytes);
-        }
-      }
-      float top[kLpPacks / kUnitPacks];
-      float gm = -INFINITY;
-#pragma unroll
-      for (int q = 0; q < kLpPacks; ++q) {
-        float m = -INFINITY;
+      for (int q = 0; q < kLpPacks; ++q)
 #pragma unroll
         for (int j = 0; j < kEpv; ++j) {
-          const float z = x[q].get(j);
-          m = fmaxf(m, kEdge && !((bits[q] >> j) & 1u) ? -INFINITY : z);
+          z[q][j] = x[q].get(j);
+          if constexpr (kEdge)
+            if (!((bits[q] >> j) & 1u)) z[q][j] = -INFINITY;
         }
-        top[q / kUnitPacks] = q % kUnitPacks ? fmaxf(top[q / kUnitPacks], m) : m;
-        gm = fmaxf(gm, m);
-      }
-      best = fmaxf(best, gm);
-      if constexpr (kTop) {
+      float top[2];
 #pragma unroll
-        for (int w = 0; w < kWords; ++w)
-          s_unit[(g * kWords + w) * kLpThreads + tid] =
-              (order_of(top[2 * w]) >> 16) | (order_of(top[2 * w + 1]) & 0xFFFF0000u);
+      for (int u = 0; u < 2; ++u) {
+        auto e = [&](int i) { return z[u * kUnitPacks + i / kEpv][i % kEpv]; };
+        top[u] = max3(e(0), e(1), e(2));
+#pragma unroll
+        for (int i = 3; i + 1 < kUnitPacks * kEpv; i += 2) top[u] = max3(top[u], e(i), e(i + 1));
+        top[u] = max2(top[u], e(kUnitPacks * kEpv - 1));
       }
-      if (__any(gm > ref + kSlack)) {
-        const float to = fmaxf(ref, wave_max(gm));
-        const float d = ref == -INFINITY ? 0.0f : (ref - to) * kLog2e;
+      best = max3(best, top[0], top[1]);
+      if constexpr (kTop) {
+        // the upper halves of both
+        s_unit[g * kLpThreads + tid] =
+            __builtin_amdgcn_perm(__float_as_uint(top[1]), __float_as_uint(top[0]), 0x07060302u);
+      }
+      if (__any(best > ref + kSlack)) {
+        const float to = wave_max_dpp(best);
+        const float d = (ref - to) * kLog2e;
         const float f = exp2f(d);
         aa = f == 0.0f ? 0.0f : fmaf(ss, d, aa) * f;
         ss *= f;
-        ref = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(to)));
+        ref = to;
       }
-      const float u = ref == -INFINITY ? 0.0f : ref;
 #pragma unroll
       for (int q = 0; q < kLpPacks; ++q) {
-        x[q].fence();  // unpacked again, rather than kept
         float ps = 0.0f, pa = 0.0f;
 #pragma unroll
         for (int j = 0; j < kEpv; ++j) {
-          float y = (x[q].get(j) - u) * kLog2e;
-          if (kEdge && !((bits[q] >> j) & 1u)) y = kFloor;
+          const float y = (z[q][j] - ref) * kLog2e;
           const float e = exp2_fast(y);
-          ps += e;
-          pa = fmaf(e, fmaxf(y, kFloor), pa);
+          ps = j ? ps + e : e;
+          pa = j ? fmaf(e, fmaxf(y, kFloor), pa) : e * fmaxf(y, kFloor);
         }
         ss += ps;
         aa += pa;
       }
     };
-    group(0, std::true_type{});
+    auto edge_group = [&](int g) {
+      P x[kLpPacks];
+      unsigned bits[kLpPacks];
+#pragma unroll
+      for (int q = 0; q < kLpPacks; ++q)
+        span.load(x[q], span.place((g * kLpPacks + q) * kLpThreads + tid, bits[q]));
+      sums(g, x, bits, std::true_type{});
+    };
+    if (kRagged) edge_group(0);
 #pragma unroll 1
-    for (int g = 1; g + 1 < groups; ++g) group(g, std::false_type{});
-    if (groups > 1) group(groups - 1, std::true_type{});
+    for (int g = now.g0; g < now.g1; ++g) {
+      P x[kLpPacks];
+      const unsigned all[kLpPacks] = {};
+#pragma unroll
+      for (int q = 0; q < kLpPacks; ++q) x[q] = next[q];
+      fetch(now, g + 1);
+      sums(g, x, all, std::false_type{});
+    }
+    if (now.g1 < groups && now.g1 >= now.g0) edge_group(groups - 1);
+    Task then = now;
+    if (more) {  // its first loads are on their way while this row is finished
+      then = task_of(next_row, (int)((task + gridDim.x) % p.n_chunks));
+      fetch(then, then.g0);
+    }
 
-    const float wm = wave_max(best);
-    ss = wave_sum(ss);
-    aa = wave_sum(aa);
+    const float wm = wave_max_dpp(best);
+    ss = wave_sum_dpp(ss);
+    aa = wave_sum_dpp(aa);
     if (lane == 0) {
       s_wave[wid][0] = wm;
       s_wave[wid][1] = ref;
@@ -304,14 +395,78 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
       s_units = 0;
     }
     __syncthreads();
-    if (tid == 0) {
-      Sums t{-INFINITY, 0.0f, 0.0f};
+    Sums t{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kLpWaves; ++w) {
+      t.m = fmaxf(t.m, s_wave[w][0]);
+      t.s += s_wave[w][2];
+    }
+    // (every thread comes to the same answer)
+    const bool odd = (fabsf(t.m) > kHuge && t.m != -INFINITY) || !(t.s < INFINITY);
+    t.s = 0.0f;
+    if (!odd && t.m != -INFINITY) {
+#pragma unroll
+      for (int w = 0; w < kLpWaves; ++w) {
+        const float d = (s_wave[w][1] - t.m) * kLog2e;
+        const float f = exp2f(d);
+        t.s = fmaf(f, s_wave[w][2], t.s);
+        t.a = fmaf(f, fmaf(s_wave[w][2], f == 0.0f ? 0.0f : d, s_wave[w][3]), t.a);
+      }
+    }
+    if (odd) {
+      // against the exact maximum of what are numbers, with differences that
+      // cannot overflow into each other
+      auto each = [&](auto use) {
+#pragma unroll 1
+        for (int i = tid; i < n; i += kLpThreads) {
+          unsigned bits;
+          const int at = span.place(i, bits);
+          P x;
+          span.load(x, at);
+#pragma unroll
+          for (int j = 0; j < kEpv; ++j)
+            if ((bits >> j) & 1u) use(x.get(j));
+        }
+      };
+      best = -INFINITY;
+      each([&](float z) { best = z > best ? z : best; });
+      const float m = wave_max_dpp(best);
+      __syncthreads();
+      if (lane == 0) s_wave[wid][0] = m;
+      if (kTop) s_max[tid] = order_of(best);
+      __syncthreads();
+      t.m = -INFINITY;
+#pragma unroll
       for (int w = 0; w < kLpWaves; ++w) t.m = fmaxf(t.m, s_wave[w][0]);
-      for (int w = 0; w < kLpWaves; ++w) add_part(t, s_wave[w][1], s_wave[w][2], s_wave[w][3]);
+      const float u = t.m == -INFINITY ? 0.0f : t.m;
+      ss = 0.0f;
+      aa = 0.0f;
+      each([&](float z) {
+        const float y = (z - u) * kLog2e;
+        const float e = exp2_fast(y);
+        ss += e;
+        aa = fmaf(e, fmaxf(y, kFloor), aa);
+      });
+      ss = wave_sum_dpp(ss);
+      aa = wave_sum_dpp(aa);
+      if (lane == 0) {
+        s_wave[wid][2] = ss;
+        s_wave[wid][3] = aa;
+      }
+      __syncthreads();
+      t.s = 0.0f;
+      t.a = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kLpWaves; ++w) {
+        t.s += s_wave[w][2];
+        t.a += s_wave[w][3];
+      }
+    }
+    if (tid == 0) {
       if (p.n_chunks == 1) {
-        write_row(p, row, t.m, t.s, t.a, s_row);
+        write_row(p, row, t.m, t.s, t.a, given);
       } else {
-        float* const out = p.part + task * kLogprobPart;
+        float* const out = p.part + (row * p.n_chunks + c) * kLogprobPart;
         out[0] = t.m;
         out[1] = t.s;
         out[2] = t.a;
@@ -323,62 +478,111 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
         unsigned v[kLpWaves];
 #pragma unroll
         for (int q = 0; q < kLpWaves; ++q) v[q] = s_max[q * kWave + lane];
-        const unsigned t = kth_largest(v, p.k);
-        if (lane == 0) s_floor = (unsigned long long)t << 32;
+        // (a bf16's order is in its upper half)
+        const unsigned k_th = kth_largest<kBf16 ? 16 : 8>(v, p.k);
+        if (lane == 0) s_floor = (unsigned long long)k_th << 32;
       }
       __syncthreads();
-      Best list{s_cand, &s_n, &s_floor};
-      const unsigned bound = (unsigned)(s_floor >> 32) & 0xFFFF0000u;
-      for (int w = 0; w < groups * kWords; ++w) {
-        const unsigned x = s_unit[w * kLpThreads + tid];
-        const int first = w * 2 * kUnitPacks * kLpThreads + tid;  // the unit's first pack
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if ((h ? x & 0xFFFF0000u : x << 16) < bound) continue;
-          const int i = atomicAdd(&s_units, 1);
-          if (i < kList) s_list[i] = first + h * kUnitPacks * kLpThreads;
+      // units whose largest reaches the bound (by its upper half, which orders
+      // halves as it orders floats)
+      const float bound = __uint_as_float(__float_as_uint(logit_of((unsigned)(s_floor >> 32))) & 0xFFFF0000u);
+      if (!odd) {
+        unsigned long long reach = 0;  // bit 2 g + h: unit h of group g
+#pragma unroll 4
+        for (int g = 0; g < groups; ++g) {
+          const unsigned x = s_unit[g * kLpThreads + tid];
+          const unsigned two = (__uint_as_float(x << 16) >= bound ? 1u : 0u) |
+                               (__uint_as_float(x & 0xFFFF0000u) >= bound ? 2u : 0u);
+          reach |= (unsigned long long)two << (2 * g);
+        }
+        // (one atomic a wave: of lanes with numbers of their own it takes a turn for each)
+        int wave_units;
+        int i = wave_exclusive_dpp(__popcll(reach), &wave_units);
+        if (wave_units) {
+          int first = 0;
+          if (lane == 0) first = atomicAdd(&s_units, wave_units);
+          i += __builtin_amdgcn_readfirstlane(first);
+          for (; reach && i < kList; reach &= reach - 1, ++i)  // the unit's first pack
+            s_list[i] = (__ffsll((long long)reach) - 1) * (kUnitPacks * kLpThreads) + tid;
         }
       }
       __syncthreads();
-      // the units' packs, or all of the chunk's where there are too many
-      const bool listed = s_units <= kList;
-      const int total = listed ? s_units * kUnitPacks : n;
-      for (int base = 0; base < total; base += kStep) {
-        const int j = base + tid;
-        if (tid < kStep && j < total) {
-          const int i = listed ? s_list[j / kUnitPacks] + j % kUnitPacks * kLpThreads : j;
-          unsigned bits;
-          const int at = span.place(i, bits);
-          P x;
+      // Elements of pack i that reach the floor join the candidates where there is room
+      // (i < 0: no pack).  All threads call it.
+      auto gather = [&](int i, unsigned long long least) {
+        unsigned bits = 0, in = 0;
+        int at = 0;
+        P x;
+        if (i >= 0) {
+          at = span.place(i, bits);
           span.load(x, at);
-          const unsigned long long least = s_floor;
 #pragma unroll
-          for (int q = 0; q < kEpv; ++q) {
-            const unsigned long long y = ranked(order_of(x.get(q)), at + q);
-            if (((bits >> q) & 1u) && y >= least) s_cand[atomicAdd(&s_n, 1)] = y;
-          }
+          for (int q = 0; q < kEpv; ++q)
+            if (ranked(order_of(x.get(q)), at + q) >= least) in |= 1u << q;
+          in &= bits;
+        }
+        int wave_in;
+        int to = wave_exclusive_dpp(__popc(in), &wave_in);
+        if (!wave_in) return;
+        int first = 0;
+        if (lane == 0) first = atomicAdd(&s_n, wave_in);
+        to += __builtin_amdgcn_readfirstlane(first);
+        if (!in) return;
+#pragma unroll
+        for (int q = 0; q < kEpv; ++q)
+          if (((in >> q) & 1u) && to < kCand) s_cand[to++] = ranked(order_of(x.get(q)), at + q);
+      };
+      Best list{s_cand, s_kept, &s_n, &s_floor};
+      int held = kCand + 1;
+      if (!odd && s_units <= kList) {
+        const int total = s_units * kUnitPacks;
+        const unsigned long long least = s_floor;
+        for (int base = 0; base < total; base += kLpThreads) {
+          const int j = base + tid;
+          gather(j < total ? s_list[j / kUnitPacks] + j % kUnitPacks * kLpThreads : -1, least);
         }
         __syncthreads();
-        if (base + kStep < total) {
-          const int held = s_n;
-          __syncthreads();  // every thread has read it before the next step adds to it
-          if (held > kMaxAlternatives) list.cut(p.k);
+        held = s_n;
+      }
+      if (held > kCand) {
+        // More than the lists hold: all packs of the chunk in steps.  (Every thread
+        // has read s_n before it is cleared.)
+        __syncthreads();
+        if (tid == 0) s_n = 0;
+        __syncthreads();
+        held = 0;
+        for (int base = 0; base < n;) {
+          if (kCand - held < 16 * kEpv) {
+            list.cut(held, p.k);
+            held = s_n;
+          }
+          const int room = (kCand - held) / kEpv;
+          const int step = room < kLpThreads ? room : kLpThreads;
+          gather(tid < step && base + tid < n ? base + tid : -1, s_floor);
+          __syncthreads();
+          held = s_n;
+          base += step;
+          if (base < n) __syncthreads();  // all have read it before the next step adds to it
         }
       }
       if (p.n_chunks == 1) {
-        write_top(p, row, list, s_row[0], s_row[1]);
+        const float l = log_sum(t.m, t.s);
+        list.ranks(held, [&](unsigned long long x, int r) {
+          if (r < p.k) write_alternative(p, row, r, x, t.m, l);
+        });
       } else {
-        unsigned long long x[Best::kMine];
-        int r[Best::kMine];
-        list.ranks(s_n, x, r);
-        unsigned long long* const out = p.cand + task * p.k;
-#pragma unroll
-        for (int q = 0; q < Best::kMine; ++q)
-          if (x[q] != 0ull && r[q] < p.k) out[r[q]] = x[q];
-        for (int j = s_n + tid; j < p.k; j += kLpThreads) out[j] = 0ull;  // a chunk shorter than k
+        unsigned long long* const out = p.cand + (row * p.n_chunks + c) * p.k;
+        list.ranks(held, [&](unsigned long long x, int r) {
+          if (r < p.k) out[r] = x;
+        });
+        for (int j = held + tid; j < p.k; j += kLpThreads) out[j] = 0ull;  // a chunk shorter than k
       }
     }
+    if (!more) break;
     __syncthreads();  // LDS is reused by the next task
+    task += gridDim.x;
+    row = next_row;
+    now = then;
   }
 }
 
@@ -386,21 +590,31 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
 __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
   __shared__ float s_row[2];
   __shared__ unsigned s_max[kLpThreads];
-  __shared__ unsigned long long s_cand[kCand];
+  __shared__ unsigned long long s_cand[kCand + kRankPad];
+  __shared__ unsigned long long s_kept[kMaxAlternatives];
   __shared__ unsigned long long s_floor;
   __shared__ int s_n;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   for (long long row = blockIdx.x; row < p.n_rows; row += gridDim.x) {
     if (p.mask && !p.mask[row]) continue;  // written by the row kernel
-    if (tid == 0) {
+    if (tid < kWave) {
+      // a chunk per lane and turn, joined in a fixed tree
       const float* const part = p.part + row * p.n_chunks * kLogprobPart;
+      const Given given = given_of(p, row);
       Sums t{-INFINITY, 0.0f, 0.0f};
-      for (int c = 0; c < p.n_chunks; ++c) t.m = fmaxf(t.m, part[c * kLogprobPart]);
-      for (int c = 0; c < p.n_chunks; ++c)
+      for (int c = lane; c < p.n_chunks; c += kWave) t.m = fmaxf(t.m, part[c * kLogprobPart]);
+      t.m = wave_max_dpp(t.m);
+      for (int c = lane; c < p.n_chunks; c += kWave)
         add_part(t, part[c * kLogprobPart], part[c * kLogprobPart + 1], part[c * kLogprobPart + 2]);
-      write_row(p, row, t.m, t.s, t.a, s_row);
-      s_n = 0;
+      t.s = wave_sum_dpp(t.s);
+      t.a = wave_sum_dpp(t.a);
+      if (tid == 0) {
+        write_row(p, row, t.m, t.s, t.a, given);
+        s_row[0] = t.m;
+        s_row[1] = log_sum(t.m, t.s);
+        s_n = 0;
+      }
     }
     if (p.k > 0) {
       const unsigned long long* const in = p.cand + row * p.n_chunks * p.k;
@@ -413,35 +627,40 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
         unsigned v[kLpWaves];
 #pragma unroll
         for (int q = 0; q < kLpWaves; ++q) v[q] = s_max[q * kWave + lane];
-        const unsigned t = kth_largest(v, p.k);
+        const unsigned t = kth_largest<0>(v, p.k);
         // numbers of 0 stand for no element
         if (lane == 0) s_floor = t ? (unsigned long long)t << 32 : 1ull;
       }
       __syncthreads();
-      Best list{s_cand, &s_n, &s_floor};
-      constexpr int kEach = kStep * 8 / kLpThreads;
-      for (int base = 0; base < total; base += kStep * 8) {
-        const unsigned long long least = s_floor;
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-          const int j = base + q * kLpThreads + tid;
-          const unsigned long long y = j < total ? in[j] : 0ull;
-          if (y >= least) s_cand[atomicAdd(&s_n, 1)] = y;
+      Best list{s_cand, s_kept, &s_n, &s_floor};
+      int held = 0;
+      for (int base = 0; base < total;) {
+        if (kCand - held < kLpThreads) {
+          list.cut(held, p.k);
+          held = s_n;
         }
+        const unsigned long long y = base + tid < total ? in[base + tid] : 0ull;
+        const bool in = y >= s_floor;
+        const unsigned long long who = __ballot(in);
+        int first = 0;
+        if (lane == 0 && who) first = atomicAdd(&s_n, __popcll(who));
+        first = __builtin_amdgcn_readfirstlane(first);
+        if (in) s_cand[first + __popcll(who & ((1ull << lane) - 1ull))] = y;
         __syncthreads();
-        if (base + kStep * 8 < total) {
-          const int held = s_n;
-          __syncthreads();  // every thread has read it before the next step adds to it
-          if (held > kMaxAlternatives) list.cut(p.k);
-        }
+        held = s_n;
+        base += kLpThreads;
+        if (base < total) __syncthreads();  // all have read it before the next step adds to it
       }
-      write_top(p, row, list, s_row[0], s_row[1]);
+      list.ranks(held, [&](unsigned long long x, int r) {
+        if (r < p.k) write_alternative(p, row, r, x, s_row[0], s_row[1]);
+      });
     }
     __syncthreads();
   }
 }
 
-constexpr int kMaxChunkElems = 24 * kLpPacks * kLpThreads * 8;  // 48 KiB of units
+constexpr int kMaxChunkElems = 24 * kGroupElems;  // and one group more for rows of any start: 50 units a lane
+constexpr int kJoinGrid = 1 << 20;  // workgroups; beyond, each takes several rows
 
 }  // namespace
 
@@ -453,17 +672,21 @@ int logprob_chunks(long long n_rows, long long vocab) {
 }
 
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
-  logprob_begin<<<1, 1, 0, s>>>(p.hdr);
+  logprob_begin<<<1, p.rows ? kBeginThreads : kWave, 0, s>>>(p);
   if (p.n_rows == 0) return hipGetLastError();
   const int epv = p.bf16 ? 8 : 4;
   const long long tasks = (long long)p.n_rows * p.n_chunks;
-  const int grid = (int)(tasks < kLpGrid ? tasks : kLpGrid);
   // packs of the widest chunk: chunk_start's boundaries lie within eight packs
   const long long packs = ((long long)p.vocab + 127 / (16 / epv) + epv - 1) / epv;
   const long long widest = p.n_chunks == 1 ? packs : packs / p.n_chunks + 9;
-  const int groups = (int)((widest + kLpThreads * kLpPacks - 1) / (kLpThreads * kLpPacks));
-  const int words = groups * kLpPacks / (2 * (8 / epv)) * kLpThreads;
+  const int group = kLpThreads * group_packs(p.bf16 != 0);
+  const int words = (int)((widest + group - 1) / group) * kLpThreads;
   const size_t lds = p.k > 0 ? (size_t)words * 4 : 0;
+  // as many workgroups as the card holds at once
+  const size_t each = lds + (p.k > 0 ? 11 * 1024 : 0);
+  const int regs = !p.bf16 ? (p.ragged && p.k > 0 ? 3 : 4) : p.k > 0 ? 5 : 6;  // workgroups a CU has registers for
+  const int per_cu = each * regs > 160 * 1024 ? (int)(160 * 1024 / each) : regs;
+  const int grid = (int)(tasks < 256 * per_cu ? tasks : 256 * per_cu);
 #define TURNKL_LP(B, R, K)                                                       \
   if ((p.bf16 != 0) == B && (p.ragged != 0) == R && (p.k > 0) == K)              \
     logprob_rows<B, R, K><<<grid, kLpThreads, lds, s>>>(p);
@@ -473,7 +696,7 @@ hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
 #undef TURNKL_LP
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (p.n_chunks > 1) {
-    logprob_join<<<(int)(p.n_rows < kLpGrid ? p.n_rows : kLpGrid), kLpThreads, 0, s>>>(p);
+    logprob_join<<<(int)(p.n_rows < kJoinGrid ? p.n_rows : kJoinGrid), kLpThreads, 0, s>>>(p);
     return hipGetLastError();
   }
   return hipSuccess;

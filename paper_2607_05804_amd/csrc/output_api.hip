@@ -11,7 +11,7 @@ namespace turnkl {
 namespace {
 
 struct LogprobLayout {
-  size_t part, cand, total;
+  size_t rows, part, cand, total;
   int n_chunks;
 };
 
@@ -25,7 +25,8 @@ LogprobLayout logprob_layout(int64_t n_tokens, int64_t vocab, int32_t k) {
   LogprobLayout L{};
   L.n_chunks = logprob_chunks(n_tokens, vocab);
   const size_t tasks = L.n_chunks > 1 ? (size_t)n_tokens * (size_t)L.n_chunks : 0;
-  L.part = align256(sizeof(Header));
+  L.rows = align256(sizeof(Header));
+  L.part = align256(L.rows + (size_t)n_tokens * sizeof(int));
   L.cand = align256(L.part + tasks * kLogprobPart * sizeof(float));
   L.total = align256(L.cand + tasks * (size_t)k * 8);
   return L;
@@ -116,6 +117,7 @@ int turnkl_token_logprobs(const void* logits, int64_t ld, int dtype, int64_t n_t
   p.top_ids = top_ids_out;
   p.top_logp = top_logp_out;
   p.hdr = reinterpret_cast<Header*>(ws);
+  p.rows = mask ? reinterpret_cast<int*>(ws + L.rows) : nullptr;
   p.part = reinterpret_cast<float*>(ws + L.part);
   p.cand = reinterpret_cast<unsigned long long*>(ws + L.cand);
   p.ld = ld;

@@ -388,6 +388,7 @@ struct LogprobParams {
   int* top_ids;
   float* top_logp;
   Header* hdr;
+  int* rows;                  // with a mask: [n_rows], the rows asked for (hdr->n_sup of them)
   float* part;                // [n_rows][n_chunks][kLogprobPart]
   unsigned long long* cand;   // [n_rows][n_chunks][k]
   long long ld;
