@@ -659,22 +659,194 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
   }
 }
 
+// Short rows: a wave each, the row in registers (kPacks packs a lane), four rows a
+// workgroup and no barriers.  The bound of the alternatives is the k-th largest of the
+// packs' maxima; where more elements reach it than the list holds, the k-th largest
+// element and, among its equals, the largest id that counts are found bit by bit.
+constexpr int kShortPacks = 8;    // of a lane, at most
+constexpr int kShortCand = 256;   // elements held for ranking
+constexpr int kShortGrid = 1 << 20;
+__device__ inline void wave_lds_order() {
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+template <bool kBf16, bool kRagged, int kPacks, bool kTop>
+__global__ __launch_bounds__(kLpThreads) void logprob_short(LogprobParams p) {
+  using Span = RowSpan<kBf16, kRagged>;
+  using P = typename Span::P;
+  constexpr int kEpv = Span::kEpv;
+  constexpr int kEs = Span::kEs;
+  __shared__ unsigned long long s_cand[kLpWaves][kShortCand + kRankTurn];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const long long stride = (long long)gridDim.x * kLpWaves;
+  for (long long row = (long long)blockIdx.x * kLpWaves + wid; row < p.n_rows; row += stride) {
+    if (p.mask && !p.mask[row]) {
+      write_masked_row(p, row, lane, kWave);
+      continue;
+    }
+    const Given given = given_of(p, row);
+    const char* const at_row = static_cast<const char*>(p.z) + row * p.ld * kEs;
+    const int pre = kRagged ? (int)(reinterpret_cast<uintptr_t>(at_row) & 15u) / kEs : 0;
+    const Span span{at_row, chunk_rsrc(at_row), p.vocab, -pre, (pre + p.vocab + kEpv - 1) / kEpv};
+    P x[kPacks];
+    int at[kPacks];
+    unsigned bits[kPacks];
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      at[q] = span.place(q * kWave + lane, bits[q]);
+      span.load(x[q], at[q]);
+    }
+    auto own = [&](int q, int j) { return kRagged ? ((bits[q] >> j) & 1u) != 0 : bits[q] != 0; };
+    float top[kPacks], best = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      top[q] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) top[q] = fmaxf(top[q], own(q, j) ? x[q].get(j) : -INFINITY);
+      best = fmaxf(best, top[q]);
+      x[q].fence();  // unpacked again, rather than kept
+    }
+    const float m = wave_max_dpp(best);
+    const float u = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f, a = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+#pragma unroll
+      for (int j = 0; j < kEpv; ++j) {
+        const float y = own(q, j) ? (x[q].get(j) - u) * kLog2e : kFloor;
+        const float e = exp2_fast(y);
+        s += e;
+        a = fmaf(e, fmaxf(y, kFloor), a);
+      }
+      x[q].fence();
+    }
+    s = wave_sum_dpp(s);
+    a = wave_sum_dpp(a);
+    if (lane == 0) write_row(p, row, m, s, a, given);
+    if constexpr (kTop) {
+      const float l = log_sum(m, s);
+      unsigned v[kPacks];
+#pragma unroll
+      for (int q = 0; q < kPacks; ++q) v[q] = bits[q] ? order_of(top[q]) : 0u;
+      const unsigned bound = kth_largest<kBf16 ? 16 : 8>(v, p.k);
+      unsigned long long* const cand = s_cand[wid];
+      int held = 0;
+      // the elements of which keep(order, id) says so join the list where there is room
+      auto collect = [&](auto keep) {
+        held = 0;
+#pragma unroll
+        for (int q = 0; q < kPacks; ++q) {
+          x[q].fence();  // no element's order is kept from one use to the next
+          unsigned in = 0;
+#pragma unroll
+          for (int j = 0; j < kEpv; ++j)
+            if (own(q, j) && keep(order_of(x[q].get(j)), at[q] + j)) in |= 1u << j;
+          int wave_in;
+          int to = held + wave_exclusive_dpp(__popc(in), &wave_in);
+          held += wave_in;
+          if (!in) continue;
+#pragma unroll
+          for (int j = 0; j < kEpv; ++j)
+            if (((in >> j) & 1u) && to < kShortCand) cand[to++] = ranked(order_of(x[q].get(j)), at[q] + j);
+        }
+      };
+      collect([&](unsigned o, int) { return o >= bound; });
+      if (held > kShortCand) {
+        // how many elements `which` says yes to
+        auto number = [&](auto which) {
+          int n = 0;
+#pragma unroll
+          for (int q = 0; q < kPacks; ++q) {
+            x[q].fence();
+#pragma unroll
+            for (int j = 0; j < kEpv; ++j)
+              n += __popcll(__ballot(own(q, j) && which(order_of(x[q].get(j)), at[q] + j)));
+          }
+          return n;
+        };
+        unsigned k_th = 0;
+#pragma unroll 1
+        for (int b = 31; b >= 0; --b) {
+          const unsigned t = k_th | (1u << b);
+          if (number([&](unsigned o, int) { return o >= t; }) >= p.k) k_th = t;
+        }
+        const int equal = p.k - number([&](unsigned o, int) { return o > k_th; });
+        int last = 0;  // the largest id with fewer than `equal` equals below it
+#pragma unroll 1
+        for (int b = 13; b >= 0; --b) {
+          const int t = last | (1 << b);
+          if (number([&](unsigned o, int id) { return o == k_th && id < t; }) < equal) last = t;
+        }
+        collect([&](unsigned o, int id) { return o > k_th || (o == k_th && id <= last); });
+      }
+      if (lane < kRankTurn) cand[held + lane] = 0ull;
+      wave_lds_order();
+      for (int i = lane; i < held; i += kWave) {
+        const unsigned long long mine = cand[i];
+        int r = 0;
+        for (int j = 0; j < held; j += kRankTurn) {
+          unsigned long long c[kRankTurn];
+#pragma unroll
+          for (int q = 0; q < kRankTurn; ++q) c[q] = cand[j + q];
+#pragma unroll
+          for (int q = 0; q < kRankTurn; ++q) r += c[q] > mine;
+        }
+        if (r < p.k) write_alternative(p, row, r, mine, m, l);
+      }
+      wave_lds_order();  // the list is rewritten for the next row
+    }
+  }
+}
+
 constexpr int kMaxChunkElems = 24 * kGroupElems;  // and one group more for rows of any start: 50 units a lane
+constexpr int kMinChunkElems = 4096;
+constexpr int kFillTasks = 1280;
 constexpr int kJoinGrid = 1 << 20;  // workgroups; beyond, each takes several rows
 
 }  // namespace
 
-// Chunks of a row: as many as its units' LDS asks for.
+// Chunks of a row: as many as its units' LDS asks for, and for few rows so many
+// that they fill the card, of 4,096 elements at least (a depth that depends on sizes
+// only, so that the workspace can be sized for it).
 int logprob_chunks(long long n_rows, long long vocab) {
-  (void)n_rows;
   // ragged rows hold up to 64 elements more, and boundaries move by eight packs
-  return (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);
+  const int by_size = (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);
+  if (n_rows < 1) return by_size;
+  const long long fill = kFillTasks / n_rows, most = vocab / kMinChunkElems;
+  const int by_rows = (int)(fill < most ? fill : most);
+  return by_rows > by_size ? by_rows : by_size;
+}
+
+template <bool kBf16, bool kRagged, bool kTop>
+void launch_short(const LogprobParams& p, int packs, hipStream_t s) {
+  const int blocks = (p.n_rows + kLpWaves - 1) / kLpWaves;
+  const int grid = blocks < kShortGrid ? blocks : kShortGrid;
+  if (packs <= kWave) logprob_short<kBf16, kRagged, 1, kTop><<<grid, kLpThreads, 0, s>>>(p);
+  else if (packs <= 2 * kWave) logprob_short<kBf16, kRagged, 2, kTop><<<grid, kLpThreads, 0, s>>>(p);
+  else if (packs <= 4 * kWave) logprob_short<kBf16, kRagged, 4, kTop><<<grid, kLpThreads, 0, s>>>(p);
+  else logprob_short<kBf16, kRagged, 8, kTop><<<grid, kLpThreads, 0, s>>>(p);
 }
 
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
-  logprob_begin<<<1, p.rows ? kBeginThreads : kWave, 0, s>>>(p);
-  if (p.n_rows == 0) return hipGetLastError();
   const int epv = p.bf16 ? 8 : 4;
+  // packs of a row of any start, on 16-byte boundaries
+  const int short_packs = (p.vocab + (p.ragged ? epv - 1 : 0) + epv - 1) / epv;
+  const bool is_short = short_packs <= kShortPacks * kWave;
+  LogprobParams first = p;
+  if (is_short) first.rows = nullptr;  // their kernel looks at the mask itself
+  logprob_begin<<<1, first.rows ? kBeginThreads : kWave, 0, s>>>(first);
+  if (p.n_rows == 0) return hipGetLastError();
+#define TURNKL_LP(B, R, K) \
+  if ((p.bf16 != 0) == B && (p.ragged != 0) == R && (p.k > 0) == K) launch_short<B, R, K>(p, short_packs, s);
+  if (is_short) {
+    TURNKL_LP(true, false, false) TURNKL_LP(true, false, true) TURNKL_LP(true, true, false)
+    TURNKL_LP(true, true, true) TURNKL_LP(false, false, false) TURNKL_LP(false, false, true)
+    TURNKL_LP(false, true, false) TURNKL_LP(false, true, true)
+    return hipGetLastError();
+  }
+#undef TURNKL_LP
   const long long tasks = (long long)p.n_rows * p.n_chunks;
   // packs of the widest chunk: chunk_start's boundaries lie within eight packs
   const long long packs = ((long long)p.vocab + 127 / (16 / epv) + epv - 1) / epv;
