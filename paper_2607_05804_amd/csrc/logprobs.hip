@@ -255,6 +255,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
   const int lane = tid & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
   const long long count = p.rows ? p.hdr->n_sup : p.n_rows;
+  // (the status of a call without logprob_begin: only the join reports to it)
+  if (p.clear && blockIdx.x == 0 && tid == 0) p.hdr->err_key = kNoError;
 
   if (p.mask)  // the rows that are not asked for
     for (long long base = blockIdx.x; base < p.n_rows; base += (long long)gridDim.x * kWave) {
@@ -264,6 +266,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
         write_masked_row(p, base + (long long)(__ffsll((long long)off) - 1) * gridDim.x, tid, kLpThreads);
     }
 
+  const long long n_tasks = count * p.n_chunks;
   // A task: a chunk of a row, packs [lo, lo + n) of it (of ragged rows on the grid of
   // 128-byte lines); g0 to g1: its groups of whole packs that lie in the row, all but
   // the last, and of ragged rows all but the first.
@@ -284,6 +287,13 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
   auto row_of = [&](long long task) -> long long {
     return p.rows ? p.rows[task / p.n_chunks] : task / p.n_chunks;
   };
+  // The next task of this workgroup from `task` on (without the list, rows that are
+  // not asked for are passed over here), n_tasks or more if there is none.
+  auto next_of = [&](long long task) {
+    if (p.mask && !p.rows)
+      while (task < n_tasks && !p.mask[task / p.n_chunks]) task += gridDim.x;
+    return task;
+  };
   P next[kLpPacks];  // the group that comes next, of this task or the next one
   auto fetch = [&](const Task& of, int g) {
     if (g >= of.g1) return;
@@ -291,16 +301,16 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     for (int q = 0; q < kLpPacks; ++q)
       next[q].load(of.span.rsrc, tid * 16, of.span.col * kEs + (g * kLpPacks + q) * (kLpThreads * 16));
   };
-  const long long n_tasks = count * p.n_chunks;
-  long long task = blockIdx.x;
+  long long task = next_of(blockIdx.x);
   if (task >= n_tasks) return;
   long long row = row_of(task);
   Task now = task_of(row, (int)(task % p.n_chunks));
   fetch(now, now.g0);
   for (;;) {
     const int c = (int)(task % p.n_chunks);
-    const bool more = task + gridDim.x < n_tasks;
-    const long long next_row = more ? row_of(task + gridDim.x) : 0;
+    const long long next_task = next_of(task + gridDim.x);
+    const bool more = next_task < n_tasks;
+    const long long next_row = more ? row_of(next_task) : 0;
     const Given given = p.n_chunks == 1 ? given_of(p, row) : Given{};
     const Span& span = now.span;
     const int n = span.n, groups = now.groups;
@@ -376,7 +386,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     if (now.g1 < groups && now.g1 >= now.g0) edge_group(groups - 1);
     Task then = now;
     if (more) {  // its first loads are on their way while this row is finished
-      then = task_of(next_row, (int)((task + gridDim.x) % p.n_chunks));
+      then = task_of(next_row, (int)(next_task % p.n_chunks));
       fetch(then, then.g0);
     }
 
@@ -580,7 +590,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     }
     if (!more) break;
     __syncthreads();  // LDS is reused by the next task
-    task += gridDim.x;
+    task = next_task;
     row = next_row;
     now = then;
   }
@@ -627,7 +637,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
         unsigned v[kLpWaves];
 #pragma unroll
         for (int q = 0; q < kLpWaves; ++q) v[q] = s_max[q * kWave + lane];
-        const unsigned t = kth_largest<0>(v, p.k);
+        const unsigned t = p.bf16 ? kth_largest<16>(v, p.k) : kth_largest<8>(v, p.k);
         // numbers of 0 stand for no element
         if (lane == 0) s_floor = t ? (unsigned long long)t << 32 : 1ull;
       }
@@ -663,8 +673,9 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
 // workgroup and no barriers.  The bound of the alternatives is the k-th largest of the
 // packs' maxima; where more elements reach it than the list holds, the k-th largest
 // element and, among its equals, the largest id that counts are found bit by bit.
-constexpr int kShortPacks = 8;    // of a lane, at most
+constexpr int kShortPacks = 16;   // of a lane, at most
 constexpr int kShortCand = 256;   // elements held for ranking
+constexpr int kShortList = 256;   // packs held for a second look
 constexpr int kShortGrid = 1 << 20;
 __device__ inline void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
@@ -672,12 +683,13 @@ __device__ inline void wave_lds_order() {
 }
 
 template <bool kBf16, bool kRagged, int kPacks, bool kTop>
-__global__ __launch_bounds__(kLpThreads) void logprob_short(LogprobParams p) {
+__global__ __launch_bounds__(kLpThreads, kPacks > 8 ? 3 : 4) void logprob_short(LogprobParams p) {
   using Span = RowSpan<kBf16, kRagged>;
   using P = typename Span::P;
   constexpr int kEpv = Span::kEpv;
   constexpr int kEs = Span::kEs;
   __shared__ unsigned long long s_cand[kLpWaves][kShortCand + kRankTurn];
+  __shared__ int s_pack[kLpWaves][kShortList];
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const long long stride = (long long)gridDim.x * kLpWaves;
@@ -730,56 +742,108 @@ __global__ __launch_bounds__(kLpThreads) void logprob_short(LogprobParams p) {
       unsigned v[kPacks];
 #pragma unroll
       for (int q = 0; q < kPacks; ++q) v[q] = bits[q] ? order_of(top[q]) : 0u;
-      const unsigned bound = kth_largest<kBf16 ? 16 : 8>(v, p.k);
+      // (of up to 32 the lanes' maxima bound them nearly as well as the packs')
+      constexpr int kLow = kBf16 ? 16 : 8;
+      const unsigned lane_best[1] = {order_of(best)};
+      const unsigned bound = 2 * p.k <= kWave ? kth_largest<kLow>(lane_best, p.k) : kth_largest<kLow>(v, p.k);
       unsigned long long* const cand = s_cand[wid];
       int held = 0;
-      // the elements of which keep(order, id) says so join the list where there is room
-      auto collect = [&](auto keep) {
-        held = 0;
+      // Adds the elements of a pack (`mine`: which of them are the lane's) to the list,
+      // where there is room, that keep(order, id) says yes to.
+      auto add = [&](const P& y, int first, unsigned mine, auto keep) {
+        unsigned in = 0;
+#pragma unroll
+        for (int j = 0; j < kEpv; ++j)
+          if (keep(order_of(y.get(j)), first + j)) in |= 1u << j;
+        in &= mine;
+        int wave_in;
+        int to = held + wave_exclusive_dpp(__popc(in), &wave_in);
+        held += wave_in;
+        if (!in) return;
+#pragma unroll
+        for (int j = 0; j < kEpv; ++j)
+          if (((in >> j) & 1u) && to < kShortCand) cand[to++] = ranked(order_of(y.get(j)), first + j);
+      };
+      if constexpr (kPacks <= 2) {
+#pragma unroll
+        for (int q = 0; q < kPacks; ++q)
+          add(x[q], at[q], bits[q], [&](unsigned o, int) { return o >= bound; });
+      } else {
+        // the packs whose largest reaches the bound, loaded again by a lane each
+        int packs = 0;
 #pragma unroll
         for (int q = 0; q < kPacks; ++q) {
-          x[q].fence();  // no element's order is kept from one use to the next
-          unsigned in = 0;
-#pragma unroll
-          for (int j = 0; j < kEpv; ++j)
-            if (own(q, j) && keep(order_of(x[q].get(j)), at[q] + j)) in |= 1u << j;
-          int wave_in;
-          int to = held + wave_exclusive_dpp(__popc(in), &wave_in);
-          held += wave_in;
-          if (!in) continue;
-#pragma unroll
-          for (int j = 0; j < kEpv; ++j)
-            if (((in >> j) & 1u) && to < kShortCand) cand[to++] = ranked(order_of(x[q].get(j)), at[q] + j);
+          const bool in = v[q] >= bound && v[q] != 0u;
+          const unsigned long long who = __ballot(in);
+          const int i = packs + __popcll(who & ((1ull << lane) - 1ull));
+          if (in && i < kShortList) s_pack[wid][i] = q * kWave + lane;
+          packs += __popcll(who);
         }
-      };
-      collect([&](unsigned o, int) { return o >= bound; });
+        if (packs <= kShortList) {
+          wave_lds_order();
+          for (int base = 0; base < packs; base += kWave) {
+            P y;
+            unsigned mine = 0;
+            int first = 0;
+            if (base + lane < packs) {
+              first = span.place(s_pack[wid][base + lane], mine);
+              span.load(y, first);
+            }
+            add(y, first, mine, [&](unsigned o, int) { return o >= bound; });
+          }
+        } else {
+          held = kShortCand + 1;
+        }
+      }
       if (held > kShortCand) {
+        // Hands every pack to use(pack, its first element, its own elements): up to two a
+        // lane from the registers, more (whose orders would fill them) from memory.
+        auto each = [&](auto use) {
+          if constexpr (kPacks <= 2) {
+#pragma unroll
+            for (int q = 0; q < kPacks; ++q) use(x[q], at[q], bits[q]);
+          } else {
+#pragma unroll 1
+            for (int q = 0; q < kPacks; ++q) {
+              P y;
+              unsigned mine;
+              const int first = span.place(q * kWave + lane, mine);
+              span.load(y, first);
+              use(y, first, mine);
+            }
+          }
+        };
         // how many elements `which` says yes to
         auto number = [&](auto which) {
           int n = 0;
-#pragma unroll
-          for (int q = 0; q < kPacks; ++q) {
-            x[q].fence();
+          each([&](const P& y, int first, unsigned mine) {
 #pragma unroll
             for (int j = 0; j < kEpv; ++j)
-              n += __popcll(__ballot(own(q, j) && which(order_of(x[q].get(j)), at[q] + j)));
-          }
+              n += __popcll(__ballot(((mine >> j) & 1u) && which(order_of(y.get(j)), first + j)));
+          });
           return n;
         };
+        constexpr int kCut = kBf16 ? 16 : 0;  // a bf16's order is in its upper half
         unsigned k_th = 0;
 #pragma unroll 1
-        for (int b = 31; b >= 0; --b) {
+        for (int b = 31; b >= kCut; --b) {
           const unsigned t = k_th | (1u << b);
           if (number([&](unsigned o, int) { return o >= t; }) >= p.k) k_th = t;
         }
-        const int equal = p.k - number([&](unsigned o, int) { return o > k_th; });
+        k_th >>= kCut;
+        const int equal = p.k - number([&](unsigned o, int) { return o >> kCut > k_th; });
         int last = 0;  // the largest id with fewer than `equal` equals below it
 #pragma unroll 1
         for (int b = 13; b >= 0; --b) {
           const int t = last | (1 << b);
-          if (number([&](unsigned o, int id) { return o == k_th && id < t; }) < equal) last = t;
+          if (number([&](unsigned o, int id) { return o >> kCut == k_th && id < t; }) < equal) last = t;
         }
-        collect([&](unsigned o, int id) { return o > k_th || (o == k_th && id <= last); });
+        held = 0;
+        each([&](const P& y, int first, unsigned mine) {
+          add(y, first, mine, [&](unsigned o, int id) {
+            return o >> kCut > k_th || (o >> kCut == k_th && id <= last);
+          });
+        });
       }
       if (lane < kRankTurn) cand[held + lane] = 0ull;
       wave_lds_order();
@@ -826,7 +890,8 @@ void launch_short(const LogprobParams& p, int packs, hipStream_t s) {
   if (packs <= kWave) logprob_short<kBf16, kRagged, 1, kTop><<<grid, kLpThreads, 0, s>>>(p);
   else if (packs <= 2 * kWave) logprob_short<kBf16, kRagged, 2, kTop><<<grid, kLpThreads, 0, s>>>(p);
   else if (packs <= 4 * kWave) logprob_short<kBf16, kRagged, 4, kTop><<<grid, kLpThreads, 0, s>>>(p);
-  else logprob_short<kBf16, kRagged, 8, kTop><<<grid, kLpThreads, 0, s>>>(p);
+  else if (packs <= 8 * kWave) logprob_short<kBf16, kRagged, 8, kTop><<<grid, kLpThreads, 0, s>>>(p);
+  else logprob_short<kBf16, kRagged, 16, kTop><<<grid, kLpThreads, 0, s>>>(p);
 }
 
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
@@ -834,9 +899,14 @@ hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
   // packs of a row of any start, on 16-byte boundaries
   const int short_packs = (p.vocab + (p.ragged ? epv - 1 : 0) + epv - 1) / epv;
   const bool is_short = short_packs <= kShortPacks * kWave;
-  LogprobParams first = p;
-  if (is_short) first.rows = nullptr;  // their kernel looks at the mask itself
-  logprob_begin<<<1, first.rows ? kBeginThreads : kWave, 0, s>>>(first);
+  LogprobParams q = p;
+  // Many rows with a mask are listed, so that every workgroup gets as many of them;
+  // where few are split only the join reports a bad id, and the row kernel can clear
+  // the status itself.
+  if (is_short || p.n_rows < kFillTasks) q.rows = nullptr;
+  q.clear = !is_short && p.n_chunks > 1 && !q.rows;
+  if (!q.clear || p.n_rows == 0)
+    logprob_begin<<<1, q.rows ? kBeginThreads : kWave, 0, s>>>(q);
   if (p.n_rows == 0) return hipGetLastError();
 #define TURNKL_LP(B, R, K) \
   if ((p.bf16 != 0) == B && (p.ragged != 0) == R && (p.k > 0) == K) launch_short<B, R, K>(p, short_packs, s);
@@ -861,7 +931,7 @@ hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
   const int grid = (int)(tasks < 256 * per_cu ? tasks : 256 * per_cu);
 #define TURNKL_LP(B, R, K)                                                       \
   if ((p.bf16 != 0) == B && (p.ragged != 0) == R && (p.k > 0) == K)              \
-    logprob_rows<B, R, K><<<grid, kLpThreads, lds, s>>>(p);
+    logprob_rows<B, R, K><<<grid, kLpThreads, lds, s>>>(q);
   TURNKL_LP(true, false, false) TURNKL_LP(true, false, true) TURNKL_LP(true, true, false)
   TURNKL_LP(true, true, true) TURNKL_LP(false, false, false) TURNKL_LP(false, false, true)
   TURNKL_LP(false, true, false) TURNKL_LP(false, true, true)

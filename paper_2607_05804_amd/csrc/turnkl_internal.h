@@ -388,7 +388,7 @@ struct LogprobParams {
   int* top_ids;
   float* top_logp;
   Header* hdr;
-  int* rows;                  // with a mask: [n_rows], the rows asked for (hdr->n_sup of them)
+  int* rows;                  // [n_rows], the rows asked for (hdr->n_sup of them), or null
   float* part;                // [n_rows][n_chunks][kLogprobPart]
   unsigned long long* cand;   // [n_rows][n_chunks][k]
   long long ld;
@@ -399,6 +399,7 @@ struct LogprobParams {
   int n_chunks;
   int bf16;
   int ragged;  // rows of any start and length (else whole aligned packs)
+  int clear;   // the row kernel clears the status
 };
 
 constexpr int kMaxAlternatives = TURNKL_MAX_ALTERNATIVES;
