@@ -319,23 +319,30 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     float best = -INFINITY;                            // the lane's largest logit
     auto sums = [&](int g, const P (&x)[kLpPacks], const unsigned (&bits)[kLpPacks], auto edge) {
       constexpr bool kEdge = decltype(edge)::value;
-      float z[kLpPacks][kEpv];
+      // (of an edge a wave passes over the packs beyond the chunk)
+      auto live = [&](int q) { return !kEdge || (g * kLpPacks + q) * kLpThreads + wid * kWave < span.n; };
+      float z[kLpPacks][kEpv], most[kLpPacks];
 #pragma unroll
-      for (int q = 0; q < kLpPacks; ++q)
+      for (int q = 0; q < kLpPacks; ++q) {
+        most[q] = -INFINITY;
+        if (!live(q)) continue;
 #pragma unroll
         for (int j = 0; j < kEpv; ++j) {
           z[q][j] = x[q].get(j);
           if constexpr (kEdge)
             if (!((bits[q] >> j) & 1u)) z[q][j] = -INFINITY;
         }
+        most[q] = max3(z[q][0], z[q][1], z[q][2]);
+#pragma unroll
+        for (int j = 3; j + 1 < kEpv; j += 2) most[q] = max3(most[q], z[q][j], z[q][j + 1]);
+        most[q] = max2(most[q], z[q][kEpv - 1]);
+      }
       float top[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        auto e = [&](int i) { return z[u * kUnitPacks + i / kEpv][i % kEpv]; };
-        top[u] = max3(e(0), e(1), e(2));
-#pragma unroll
-        for (int i = 3; i + 1 < kUnitPacks * kEpv; i += 2) top[u] = max3(top[u], e(i), e(i + 1));
-        top[u] = max2(top[u], e(kUnitPacks * kEpv - 1));
+        const int q = u * kUnitPacks;
+        if constexpr (kUnitPacks == 2) top[u] = max2(most[q], most[q + 1]);
+        else top[u] = max2(max3(most[q], most[q + 1], most[q + 2]), most[q + 3]);
       }
       best = max3(best, top[0], top[1]);
       if constexpr (kTop) {
@@ -353,6 +360,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
       }
 #pragma unroll
       for (int q = 0; q < kLpPacks; ++q) {
+        if (!live(q)) continue;
         float ps = 0.0f, pa = 0.0f;
 #pragma unroll
         for (int j = 0; j < kEpv; ++j) {
