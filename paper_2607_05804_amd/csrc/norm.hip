@@ -291,10 +291,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
 #pragma unroll
       for (int q = 0; q < kPacks; ++q) out.store_own(data[q], at[q], bits[q]);
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q) out.store_whole(data[q], at[q], bits[q]);
-      drain_stores();  // their data registers are free for the next row
+      for (int q = 0; q < kPacks; ++q) out.store_whole(data[q], at[q], bits[q]);
     }
   }
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
   if constexpr (!kLean) {
     if (!p.part) return;
     float* const part = p.part + (long long)blockIdx.x * 2 * p.width;
