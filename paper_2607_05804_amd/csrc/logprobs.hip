@@ -8,9 +8,10 @@
 // against M log2 e in the same way when the waves are joined, so that no error of
 // r enters.  The reference moves (and the sums with it) when a lane meets a logit
 // more than kSlack above it, so that no sum overflows and no second pass is needed;
-// A / S then cancels a few units at most.  A is summed over max(x, kFloor): a
-// forbidden token (-inf) gives 0 * kFloor, not 0 * -inf.  Rows beyond the reach of
-// that (|M| > kHuge, NaN, +inf) are summed again against their exact maximum.
+// A / S then cancels a few units at most.  A forbidden token (-inf) makes A NaN: its
+// group is summed again, and all that follow, over max(x, kFloor), which gives
+// 0 * kFloor, not 0 * -inf.  Rows beyond the reach of that (|M| > kHuge, NaN, +inf)
+// are summed again against their exact maximum.
 //
 // Alternatives.  Ranking works on 64-bit numbers that order logits and ids at
 // once: the logit's bits, made monotone, above the complement of its id.  While
@@ -130,19 +131,18 @@ struct Best {
   }
 };
 
-// The given token of a row and its logit, read while the row streams by.
+// Whether a wave's row has a given token, and its logit, read while the row streams by.
 struct Given {
-  int id;
   bool in;
   float z;
 };
 __device__ inline Given given_of(const LogprobParams& p, long long row) {
-  Given g{0, false, __builtin_nanf("")};
+  Given g{false, __builtin_nanf("")};
   if (!p.ids) return g;
-  g.id = p.ids[row];
-  g.in = g.id >= 0 && g.id < p.vocab;
+  const int id = __builtin_amdgcn_readfirstlane(p.ids[row]);
+  g.in = id >= 0 && id < p.vocab;
   if (g.in && p.logp) {
-    const long long at = row * p.ld + g.id;
+    const long long at = row * p.ld + id;
     g.z = p.bf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
                  : static_cast<const float*>(p.z)[at];
   }
@@ -234,8 +234,15 @@ __global__ __launch_bounds__(kBeginThreads) void logprob_begin(LogprobParams p) 
 
 // One chunk of a row after the other (task = row of the list x chunk), by workgroups
 // that fill the card.
+// Workgroups of a variant that a CU has registers for.  (The one of bf16 rows on packs
+// with alternatives has five without being held to it; held to it, it spills.)
+__host__ __device__ constexpr int rows_a_cu(bool bf16, bool ragged, bool top) {
+  return bf16 ? (top ? 5 : 6) : (ragged && top ? 3 : 4);
+}
+
 template <bool kBf16, bool kRagged, bool kTop>
-__global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
+__global__ __launch_bounds__(kLpThreads, kBf16 && kTop && !kRagged ? 4 : rows_a_cu(kBf16, kRagged, kTop))
+    void logprob_rows(LogprobParams p) {
   constexpr int kLpPacks = group_packs(kBf16);
   using Span = RowSpan<kBf16, kRagged>;
   using P = typename Span::P;
@@ -294,6 +301,9 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
       while (task < n_tasks && !p.mask[task / p.n_chunks]) task += gridDim.x;
     return task;
   };
+  // Whether this wave has met a forbidden token: from then on A is summed over
+  // max(x, kFloor), which changes no bit of rows without one.
+  bool floored = false;
   P next[kLpPacks];  // the group that comes next, of this task or the next one
   auto fetch = [&](const Task& of, int g) {
     if (g >= of.g1) return;
@@ -315,7 +325,8 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     const Span& span = now.span;
     const int n = span.n, groups = now.groups;
 
-    float ref = -kHuge, ss = 0.0f, aa = 0.0f;  // the wave's reference and lane sums
+    float ref = -kHuge, ref2 = ref * kLog2e;           // the wave's reference, in log2 units too
+    float ss = 0.0f, aa = 0.0f;                        // the lane's sums
     float best = -INFINITY;                            // the lane's largest logit
     auto sums = [&](int g, const P (&x)[kLpPacks], const unsigned (&bits)[kLpPacks], auto edge) {
       constexpr bool kEdge = decltype(edge)::value;
@@ -351,27 +362,42 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
             __builtin_amdgcn_perm(__float_as_uint(top[1]), __float_as_uint(top[0]), 0x07060302u);
       }
       if (__any(best > ref + kSlack)) {
-        const float to = wave_max_dpp(best);
-        const float d = (ref - to) * kLog2e;
+        ref = wave_max_dpp(best);
+        const float to = ref * kLog2e, d = ref2 - to;
         const float f = exp2f(d);
         aa = f == 0.0f ? 0.0f : fmaf(ss, d, aa) * f;
         ss *= f;
-        ref = to;
+        ref2 = to;
       }
+      float gs = 0.0f, ga = 0.0f;
+      auto add = [&](auto floored) {
+        gs = 0.0f;
+        ga = 0.0f;
 #pragma unroll
-      for (int q = 0; q < kLpPacks; ++q) {
-        if (!live(q)) continue;
-        float ps = 0.0f, pa = 0.0f;
+        for (int q = 0; q < kLpPacks; ++q) {
+          if (!live(q)) continue;
+          float ps = 0.0f, pa = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kEpv; ++j) {
-          const float y = (z[q][j] - ref) * kLog2e;
-          const float e = exp2_fast(y);
-          ps = j ? ps + e : e;
-          pa = j ? fmaf(e, fmaxf(y, kFloor), pa) : e * fmaxf(y, kFloor);
+          for (int j = 0; j < kEpv; ++j) {
+            const float y = fmaf(z[q][j], kLog2e, -ref2);
+            const float e = exp2_fast(y);
+            const float x = decltype(floored)::value ? fmaxf(y, kFloor) : y;
+            ps = j ? ps + e : e;
+            pa = j ? fmaf(e, x, pa) : e * x;
+          }
+          gs += ps;
+          ga += pa;
         }
-        ss += ps;
-        aa += pa;
+      };
+      if constexpr (!kEdge) {
+        if (!floored) {
+          add(std::false_type{});
+          floored = __any(ga != ga);
+        }
       }
+      if (kEdge || floored) add(std::true_type{});
+      ss += gs;
+      aa += ga;
     };
     auto edge_group = [&](int g) {
       P x[kLpPacks];
@@ -403,7 +429,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     aa = wave_sum_dpp(aa);
     if (lane == 0) {
       s_wave[wid][0] = wm;
-      s_wave[wid][1] = ref;
+      s_wave[wid][1] = ref2;
       s_wave[wid][2] = ss;
       s_wave[wid][3] = aa;
     }
@@ -425,7 +451,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows(LogprobParams p) {
     if (!odd && t.m != -INFINITY) {
 #pragma unroll
       for (int w = 0; w < kLpWaves; ++w) {
-        const float d = (s_wave[w][1] - t.m) * kLog2e;
+        const float d = -fmaf(t.m, kLog2e, -s_wave[w][1]);
         const float f = exp2f(d);
         t.s = fmaf(f, s_wave[w][2], t.s);
         t.a = fmaf(f, fmaf(s_wave[w][2], f == 0.0f ? 0.0f : d, s_wave[w][3]), t.a);
@@ -934,7 +960,7 @@ hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s) {
   const size_t lds = p.k > 0 ? (size_t)words * 4 : 0;
   // as many workgroups as the card holds at once
   const size_t each = lds + (p.k > 0 ? 11 * 1024 : 0);
-  const int regs = !p.bf16 ? (p.ragged && p.k > 0 ? 3 : 4) : p.k > 0 ? 5 : 6;  // workgroups a CU has registers for
+  const int regs = rows_a_cu(p.bf16 != 0, p.ragged != 0, p.k > 0);
   const int per_cu = each * regs > 160 * 1024 ? (int)(160 * 1024 / each) : regs;
   const int grid = (int)(tasks < 256 * per_cu ? tasks : 256 * per_cu);
 #define TURNKL_LP(B, R, K)                                                       \
