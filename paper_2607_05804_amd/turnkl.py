@@ -260,12 +260,14 @@ def _options(n: int, support_floor: int, support_frac: float, success, outcome_s
                                 _ptr(outcome_stats), _ptr(token_weights), _ptr(token_lse)))
 
 
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise TypeError(f"logits must be bfloat16 or float32, got {t.dtype}")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"logits must be bfloat16 or float32, got {t.dtype}")
+    return code
 
 
 def _row_stride(t: torch.Tensor) -> int:
@@ -578,10 +580,72 @@ def fwd_bwd_topk(student: torch.Tensor, teacher_ids: torch.Tensor, teacher_vals:
     return loss, grad_t, gk, turn_stats, kl_t, workspace
 
 
-def _stream(device) -> int:
-    """Address of the device's current HIP stream.  (The raw getter: building a
-    torch Stream object takes 1.8 us, a fifth of a small call.)"""
-    return torch._C._cuda_getCurrentRawStream(device.index)
+# The calls of the operators around the logits are small next to the fused loss: what
+# their arguments are checked with costs as much as a small kernel.  Each tensor is
+# therefore asked once for what is needed of it, devices are compared by index, and
+# addresses are passed as they are.
+
+
+def _gpu(t: torch.Tensor) -> int:
+    """The index of a tensor's device."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"tensors must be on the GPU, not {t.device}")
+    return index
+
+
+def _stream(index: int) -> int:
+    """Address of a device's current HIP stream.  (The raw getter: building a torch
+    Stream object takes 1.8 us, a fifth of a small call.)"""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _matrix(t: torch.Tensor, n: int, cols: int):
+    """Address and row stride of n rows of cols elements."""
+    if n == 0:
+        return t.data_ptr(), cols
+    ld, step = t.stride()
+    if step != 1:
+        raise ValueError("rows must be 2-D with unit column stride")
+    return t.data_ptr(), ld if n > 1 else max(ld, cols)
+
+
+def _vector(t: torch.Tensor | None, count: int, name: str, index: int, dtype=torch.float32):
+    """Address of a caller buffer of `count` elements at least (None: no buffer)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}, not {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < count:
+        raise ValueError(f"{name} holds {t.numel()} elements; the call needs {count}")
+    return t.data_ptr()
+
+
+def _per_row(t: torch.Tensor | None, n: int, name: str, index: int, dtype):
+    """Address of a contiguous vector with one entry per row (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} with one entry per row")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}, not {t.device}")
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, code: int, index: int, shape, name: str) -> None:
+    if t.get_device() != index or _DTYPES.get(t.dtype) != code or t.shape != shape:
+        raise ValueError(f"{name} must match the rows' device, dtype and shape")
+
+
+def _scratch(workspace, index: int):
+    """Address and size of a workspace."""
+    if workspace.tensor.get_device() != index:
+        raise ValueError(f"workspace must be on cuda:{index}, not {workspace.tensor.device}")
+    return workspace.tensor.data_ptr(), workspace.nbytes
 
 
 class TokenLogprobs(NamedTuple):
@@ -615,21 +679,13 @@ class LogprobsWorkspace(Workspace):
         self.n_tokens = n_tokens
 
 
-def _check_token_rows(logits, token_ids, mask):
-    """dtype code, n_tokens and vocab of a call on rows of logits, after checking
-    the given tokens and the mask against them."""
-    dt = _dtype_code(logits)
-    if logits.dim() != 2:
-        raise ValueError("logits must be 2-D with unit column stride")
-    n, v = int(logits.shape[0]), int(logits.shape[1])
-    for t, dtype, name in ((token_ids, torch.int32, "token_ids"), (mask, torch.uint8, "mask")):
-        if t is None:
-            continue
-        if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous {dtype} with one entry per row")
-        if t.device != logits.device:
-            raise ValueError(f"{name} must be on {logits.device}, not {t.device}")
-    return dt, n, v
+def _check_rows(t: torch.Tensor, what: str):
+    """dtype code, shape and device index of a matrix of rows."""
+    dt = _dtype_code(t)
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be 2-D with unit column stride")
+    return dt, shape, _gpu(t)
 
 
 def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, *, k: int = 0,
@@ -645,30 +701,34 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
     but the alternatives may be None; check: read the device status once at the
     end and raise on an id outside [0, V).  Returns out.
     """
-    dt, n, v = _check_token_rows(logits, token_ids, mask)
-    dev = logits.device
+    dt, shape, index = _check_rows(logits, "logits")
+    n, v = shape
+    ids_at = _per_row(token_ids, n, "token_ids", index, torch.int32)
+    mask_at = _per_row(mask, n, "mask", index, torch.uint8)
     if not 0 <= k <= min(MAX_ALTERNATIVES, v):
         raise ValueError(f"k must be in 0 .. min({MAX_ALTERNATIVES}, vocab), not {k}")
     if out is None:
-        out = new_token_logprobs(n, k, device=dev, logp=token_ids is not None)
-    for t, need, name in ((out.logp, 4 * n, "logp"), (out.entropy, 4 * n, "entropy"),
-                          (out.log_z, 8 * n, "log_z")):
-        _need(t, need, name, dev, torch.float32)
+        out = new_token_logprobs(n, k, device=logits.device, logp=token_ids is not None)
+    top_ids = top_logp = None
+    ld_top = 0
     if k:
-        for t, dtype, name in ((out.top_ids, torch.int32, "top_ids"),
-                               (out.top_logp, torch.float32, "top_logp")):
-            if t is None or t.device != dev or t.dtype != dtype or t.dim() != 2 or \
-                    t.shape != (n, k) or (n and t.stride(1) != 1):
-                raise ValueError(f"{name} must be {dtype} [n_tokens, k] on {dev} with unit column stride")
-        if out.top_ids.stride() != out.top_logp.stride():
+        top_ids, top_logp = out.top_ids, out.top_logp
+        for t, dtype, name in ((top_ids, torch.int32, "top_ids"), (top_logp, torch.float32, "top_logp")):
+            if t is None or t.dtype is not dtype or t.shape != (n, k) or t.get_device() != index or \
+                    (n and t.stride()[1] != 1):
+                raise ValueError(f"{name} must be {dtype} [n_tokens, k] on cuda:{index} with unit "
+                                 "column stride")
+        strides = top_ids.stride()
+        if strides != top_logp.stride():
             raise ValueError("top_ids and top_logp must share a row stride")
+        ld_top = max(strides[0], k)
+        top_ids, top_logp = top_ids.data_ptr(), top_logp.data_ptr()
     if workspace is None:
-        workspace = LogprobsWorkspace(n, v, k, device=dev)
+        workspace = LogprobsWorkspace(n, v, k, device=logits.device)
     rc = lib().turnkl_token_logprobs(
-        _ptr(logits), _row_stride(logits) if n else v, dt, n, v, _ptr(token_ids), _ptr(mask), k,
-        _ptr(out.logp), _ptr(out.entropy), _ptr(out.log_z), _ptr(out.top_ids) if k else None,
-        _ptr(out.top_logp) if k else None, (max(int(out.top_ids.stride(0)), k) if k else 0),
-        _ptr(workspace.tensor), workspace.nbytes, _stream(dev))
+        *_matrix(logits, n, v), dt, n, v, ids_at, mask_at, k, _vector(out.logp, n, "logp", index),
+        _vector(out.entropy, n, "entropy", index), _vector(out.log_z, 2 * n, "log_z", index), top_ids,
+        top_logp, ld_top, *_scratch(workspace, index), _stream(index))
     if rc != OK:
         raise TurnKLError(rc, "turnkl_token_logprobs")
     if check:
@@ -690,21 +750,19 @@ def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log
     (entropy is needed with grad_entropy only); grad: "new" allocates it,
     "inplace" writes it over the logits, a tensor of their shape receives it.
     """
-    dt, n, v = _check_token_rows(logits, token_ids, mask)
-    dev = logits.device
-    for t, size, name in ((log_z, 8 * n, "log_z"), (entropy, 4 * n, "entropy"),
-                          (grad_logp, 4 * n, "grad_logp"), (grad_entropy, 4 * n, "grad_entropy")):
-        _need(t, size, name, dev, torch.float32)
+    dt, shape, index = _check_rows(logits, "logits")
+    n, v = shape
     if isinstance(grad, str):
         if grad not in ("new", "inplace"):
             raise ValueError(grad)
         grad = torch.empty_like(logits) if grad == "new" else logits
-    elif grad.device != dev or grad.dtype != logits.dtype or grad.shape != logits.shape:
-        raise ValueError("grad must match the logits' device, dtype and shape")
+    else:
+        _like(grad, dt, index, shape, "grad")
     rc = lib().turnkl_token_logprobs_bwd(
-        _ptr(logits), _row_stride(logits) if n else v, dt, n, v, _ptr(token_ids), _ptr(mask),
-        _ptr(log_z), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad),
-        _row_stride(grad) if n else v, _stream(dev))
+        *_matrix(logits, n, v), dt, n, v, _per_row(token_ids, n, "token_ids", index, torch.int32),
+        _per_row(mask, n, "mask", index, torch.uint8), _vector(log_z, 2 * n, "log_z", index),
+        _vector(entropy, n, "entropy", index), _vector(grad_logp, n, "grad_logp", index),
+        _vector(grad_entropy, n, "grad_entropy", index), *_matrix(grad, n, v), _stream(index))
     if rc != OK:
         raise TurnKLError(rc, "turnkl_token_logprobs_bwd")
     return grad
@@ -721,27 +779,13 @@ class NormWorkspace(Workspace):
         self.nbytes = nbytes
 
 
-def _rows_like(t: torch.Tensor | None, x: torch.Tensor, name: str) -> None:
-    if t is not None and (t.device != x.device or t.dtype != x.dtype or t.shape != x.shape):
-        raise ValueError(f"{name} must match the rows' device, dtype and shape")
-
-
-def _check_norm(x, params):
-    """dtype code, rows, width and the parameters' dtype code of a normalisation."""
-    dt = _dtype_code(x)
-    if x.dim() != 2:
-        raise ValueError("rows must be 2-D with unit column stride")
-    pt = None
-    for t, name in params:
-        if t is None:
-            continue
-        if t.dim() != 1 or t.numel() != x.shape[1] or t.device != x.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous with one entry per column, on {x.device}")
-        code = _dtype_code(t)
-        if pt is not None and code != pt:
-            raise TypeError("weight and bias must share a dtype")
-        pt = code
-    return dt, int(x.shape[0]), int(x.shape[1]), dt if pt is None else pt
+def _parameter(t: torch.Tensor | None, d: int, name: str, index: int):
+    """Address of a vector of parameters (None: not given)."""
+    if t is None:
+        return None
+    if t.dim() != 1 or t.numel() != d or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with one entry per column, on cuda:{index}")
+    return t.data_ptr()
 
 
 def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None,
@@ -755,20 +799,26 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None,
     allocates, or a float32 [N, 2] tensor receives, each row's (mean, 1 / standard
     deviation), which norm_bwd takes.  Returns (y, stats or None).
     """
-    dt, n, d, pt = _check_norm(x, ((weight, "weight"), (bias, "bias")))
-    dev = x.device
+    dt, shape, index = _check_rows(x, "rows")
+    n, d = shape
+    w_at = _parameter(weight, d, "weight", index)
+    b_at = _parameter(bias, d, "bias", index)
+    pt = dt if weight is None else _dtype_code(weight)
+    if bias is not None:
+        if weight is not None and bias.dtype != weight.dtype:
+            raise TypeError("weight and bias must share a dtype")
+        pt = _dtype_code(bias)
     if isinstance(y, str):
         if y not in ("new", "inplace"):
             raise ValueError(y)
         y = torch.empty_like(x) if y == "new" else x
-    _rows_like(y, x, "y")
+    else:
+        _like(y, dt, index, shape, "y")
     if isinstance(stats, bool):
-        stats = torch.empty((n, 2), dtype=torch.float32, device=dev) if stats else None
-    _need(stats, 8 * n, "stats", dev, torch.float32)
+        stats = torch.empty((n, 2), dtype=torch.float32, device=x.device) if stats else None
     rc = lib().turnkl_norm_fwd(
-        _ptr(x), _row_stride(x) if n else d, dt, n, d, _ptr(weight), _ptr(bias), pt,
-        NORM_RMS if rms else NORM_LAYER, eps, _ptr(y), _row_stride(y) if n else d, _ptr(stats),
-        _stream(dev))
+        *_matrix(x, n, d), dt, n, d, w_at, b_at, pt, NORM_RMS if rms else NORM_LAYER, eps,
+        *_matrix(y, n, d), _vector(stats, 2 * n, "stats", index), _stream(index))
     if rc != OK:
         raise TurnKLError(rc, "turnkl_norm_fwd")
     return y, stats
@@ -787,34 +837,36 @@ def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
     tensor receives, the sums over all rows (accumulate: is added to).  Returns
     (grad_x, grad_weight, grad_bias), None where not asked for.
     """
-    dt, n, d, pt = _check_norm(x, ((weight, "weight"),))
-    dev = x.device
-    _rows_like(grad_y, x, "grad_y")
+    dt, shape, index = _check_rows(x, "rows")
+    n, d = shape
+    w_at = _parameter(weight, d, "weight", index)
+    pt = dt if weight is None else _dtype_code(weight)
+    _like(grad_y, dt, index, shape, "grad_y")
     if isinstance(grad_x, str):
         if grad_x not in ("new", "inplace"):
             raise ValueError(grad_x)
         grad_x = torch.empty_like(x) if grad_x == "new" else grad_y
-    _rows_like(grad_x, x, "grad_x")
-    sums = []
-    for t, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")):
-        if t is None or isinstance(t, bool):
-            if t and accumulate:
-                raise ValueError(f"accumulate needs a tensor for {name}")
-            t = torch.empty(d, dtype=torch.float32, device=dev) if t else None
-        _need(t, 4 * d, name, dev, torch.float32)
-        sums.append(t)
-    _need(stats, 8 * n, "stats", dev, torch.float32)
-    if workspace is None and (sums[0] is not None or sums[1] is not None):
-        workspace = NormWorkspace(n, d, device=dev)
+    elif grad_x is not None:
+        _like(grad_x, dt, index, shape, "grad_x")
+    if isinstance(grad_weight, bool) or isinstance(grad_bias, bool):
+        new = lambda: torch.empty(d, dtype=torch.float32, device=x.device)  # noqa: E731
+        if accumulate and (grad_weight is True or grad_bias is True):
+            raise ValueError("accumulate needs a tensor for each sum that is asked for")
+        grad_weight = new() if grad_weight is True else grad_weight if grad_weight is not False else None
+        grad_bias = new() if grad_bias is True else grad_bias if grad_bias is not False else None
+    gx_at, ld_gx = (None, 0) if grad_x is None else _matrix(grad_x, n, d)
+    ws_at, ws_bytes = None, 0
+    if grad_weight is not None or grad_bias is not None:
+        if workspace is None:
+            workspace = NormWorkspace(n, d, device=x.device)
+        ws_at, ws_bytes = _scratch(workspace, index)
     rc = lib().turnkl_norm_bwd(
-        _ptr(grad_y), _row_stride(grad_y) if n else d, _ptr(x), _row_stride(x) if n else d, dt, n, d,
-        _ptr(weight), pt, NORM_RMS if rms else NORM_LAYER, _ptr(stats), _ptr(grad_x),
-        (_row_stride(grad_x) if n else d) if grad_x is not None else 0, _ptr(sums[0]), _ptr(sums[1]),
-        int(bool(accumulate)), _ptr(workspace.tensor) if workspace is not None else None,
-        workspace.nbytes if workspace is not None else 0, _stream(dev))
+        *_matrix(grad_y, n, d), *_matrix(x, n, d), dt, n, d, w_at, pt, NORM_RMS if rms else NORM_LAYER,
+        _vector(stats, 2 * n, "stats", index), gx_at, ld_gx, _vector(grad_weight, d, "grad_weight", index),
+        _vector(grad_bias, d, "grad_bias", index), 1 if accumulate else 0, ws_at, ws_bytes, _stream(index))
     if rc != OK:
         raise TurnKLError(rc, "turnkl_norm_bwd")
-    return grad_x, sums[0], sums[1]
+    return grad_x, grad_weight, grad_bias
 
 
 def new_turn_stats(max_turns: int, device="cuda") -> torch.Tensor:
