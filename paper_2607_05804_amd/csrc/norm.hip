@@ -5,7 +5,9 @@
 // squared differences from it are taken one after the other.  Every workgroup goes
 // from row to row and keeps its columns' weights (and, backward, the columns' sums
 // over its rows) in registers; the next row is on its way while one is reduced.
-// Backward a second kernel adds the workgroups' sums in their order.  Bound: HBM.
+// Backward a second kernel adds the workgroups' sums in their order.  Bound: HBM; small
+// batches by latency.  65,536 bf16 rows of 4,096: 191 us forward (5.6 TB/s), 275
+// backward (5.85 TB/s), where a copy of 2 GiB reaches 5.2; 64 rows of 2,048 forward 4 us.
 
 #include "row_span.h"
 
@@ -38,43 +40,65 @@ __device__ inline void row_sums(float (&v)[kN], float* lds, int waves, int& turn
   }
 }
 
-// A pack's own elements of a vector of parameters (`fill` where there is none, and
-// for elements that are another thread's).
-template <int kEpv>
-__device__ inline void load_params(const void* v, bool bf16, float fill, int at, unsigned bits,
-                                   float (&out)[kEpv]) {
+// Whether element j of a pack is its own (of rows of whole packs all are, or none).
+template <bool kRagged>
+__device__ inline bool own_element(unsigned bits, int j) {
+  return kRagged ? ((bits >> j) & 1u) != 0 : bits != 0;
+}
+
+// A thread's packs of a vector of parameters: their own elements, `fill` for the others
+// and where there is no vector.  All loads go out before one is waited for, here as for
+// the rows: a branch around each makes every pack wait for the one before it (100 bf16
+// rows of 2,048 backward took 12.0 us with such branches).
+template <int kEpv, bool kRagged, int kPacks>
+__device__ inline void load_params(const void* v, bool bf16, float fill, int width, const int* at,
+                                   const unsigned* bits, float (&out)[kPacks][kEpv]) {
 #pragma unroll
-  for (int j = 0; j < kEpv; ++j) out[j] = fill;
-  if (!v || !bits) return;
+  for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+    for (int j = 0; j < kEpv; ++j) out[q][j] = fill;
+  if (!v) return;
   const auto r = chunk_rsrc(v);
-  const bool whole = bits == (1u << kEpv) - 1u;
-  if (bf16 && whole) {
-    unsigned u[kEpv / 2];
-    if constexpr (kEpv == 8) {
-      const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at * 2, 0, 0);
-      u[0] = x[0]; u[1] = x[1]; u[2] = x[2]; u[3] = x[3];
-    } else {
-      const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, at * 2, 0, 0);
-      u[0] = x[0]; u[1] = x[1];
-    }
+  if (kRagged && width < kEpv) {  // a vector shorter than a pack: element by element
 #pragma unroll
     for (int j = 0; j < kEpv; ++j)
-      out[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xFFFF0000u : u[j >> 1] << 16);
-  } else if (whole) {
+      if ((bits[0] >> j) & 1u)
+        out[0][j] = bf16 ? __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, j * 2, 0, 0) << 16)
+                         : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, j * 4, 0, 0));
+    return;
+  }
+  unsigned u[kPacks][kEpv];
+  if (bf16) {
 #pragma unroll
-    for (int k = 0; k < kEpv / 4; ++k) {
-      const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 16 * k, 0);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) out[4 * k + j] = __uint_as_float(x[j]);
+    for (int q = 0; q < kPacks; ++q) {
+      if constexpr (kEpv == 8) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at[q] * 2, 0, 0);
+        u[q][0] = x[0]; u[q][1] = x[1]; u[q][2] = x[2]; u[q][3] = x[3];
+      } else {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, at[q] * 2, 0, 0);
+        u[q][0] = x[0]; u[q][1] = x[1];
+      }
     }
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+      for (int j = kEpv - 1; j >= 0; --j)
+        u[q][j] = j & 1 ? u[q][j >> 1] & 0xFFFF0000u : u[q][j >> 1] << 16;
   } else {
 #pragma unroll
-    for (int j = 0; j < kEpv; ++j) {
-      if (!((bits >> j) & 1u)) continue;
-      out[j] = bf16 ? __uint_as_float((unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, (at + j) * 2, 0, 0) << 16)
-                    : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (at + j) * 4, 0, 0));
-    }
+    for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+      for (int k = 0; k < kEpv / 4; ++k) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, at[q] * 4, 16 * k, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[q][4 * k + j] = x[j];
+      }
   }
+#pragma unroll
+  for (int q = 0; q < kPacks; ++q)
+#pragma unroll
+    for (int j = 0; j < kEpv; ++j)
+      if (own_element<kRagged>(bits[q], j)) out[q][j] = __uint_as_float(u[q][j]);
 }
 
 template <bool kBf16, bool kRagged>
@@ -105,17 +129,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_rows(NormParams p) {
     for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * threads + tid, bits[q]);
   }
   float w[kPacks][kEpv], b[kPacks][kEpv];
-#pragma unroll
-  for (int q = 0; q < kPacks; ++q) {
-    load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[q]);
-    load_params(p.bias, p.param_bf16, 0.0f, at[q], bits[q], b[q]);
-  }
+  load_params<kEpv, kRagged>(p.weight, p.param_bf16, 1.0f, p.width, at, bits, w);
+  load_params<kEpv, kRagged>(p.bias, p.param_bf16, 0.0f, p.width, at, bits, b);
   P next[kPacks];
   auto fetch = [&](long long row) {
     const Span s = row_of<kBf16, kRagged>(p.x, p.ld_x, row, p.width, packs);
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q)
-      if (bits[q]) s.load(next[q], at[q]);
+    for (int q = 0; q < kPacks; ++q) s.load(next[q], at[q]);
   };
   // The stores of a row may read their data while the next row is summed: it stays
   // in registers of its own until then.
@@ -135,7 +155,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_rows(NormParams p) {
 #pragma unroll
       for (int q = 0; q < kPacks; ++q)
 #pragma unroll
-        for (int j = 0; j < kEpv; ++j) v[0] += (bits[q] >> j) & 1u ? x[q].get(j) : 0.0f;
+        for (int j = 0; j < kEpv; ++j) v[0] += own_element<kRagged>(bits[q], j) ? x[q].get(j) : 0.0f;
 #pragma unroll
       for (int q = 0; q < kPacks; ++q) x[q].fence();  // unpacked again, rather than kept
       row_sums<kOneWave>(v, s_sum, waves, turn);
@@ -146,7 +166,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_rows(NormParams p) {
     for (int q = 0; q < kPacks; ++q)
 #pragma unroll
       for (int j = 0; j < kEpv; ++j) {
-        const float d = (bits[q] >> j) & 1u ? x[q].get(j) - mean : 0.0f;
+        const float d = own_element<kRagged>(bits[q], j) ? x[q].get(j) - mean : 0.0f;
         v[0] = fmaf(d, d, v[0]);
       }
 #pragma unroll
@@ -178,6 +198,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_rows(NormParams p) {
   for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
 }
 
+// Packs of a thread whose columns' sums go through LDS at a time: 32 KB at most.
+constexpr int col_packs(bool one_wave, int packs) { return one_wave || packs < 2 ? packs : 2; }
+
 template <bool kBf16, bool kRagged, bool kRms, bool kOneWave, int kPacks>
 __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
   using Span = RowSpan<kBf16, kRagged>;
@@ -202,11 +225,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
     for (int q = 0; q < kPacks; ++q) at[q] = s.place(q * threads + tid, bits[q]);
   }
   float w[kLean ? 1 : kPacks][kEpv], gw[kLean ? 1 : kPacks][kEpv], gb[kLean ? 1 : kPacks][kEpv];
-  if constexpr (!kLean)
-#pragma unroll
-    for (int q = 0; q < kPacks; ++q) load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[q]);
+  if constexpr (!kLean) load_params<kEpv, kRagged>(p.weight, p.param_bf16, 1.0f, p.width, at, bits, w);
   auto weights = [&](int q) -> const float* {
-    if constexpr (kLean) load_params(p.weight, p.param_bf16, 1.0f, at[q], bits[q], w[0]);
+    if constexpr (kLean)
+      load_params<kEpv, kRagged>(p.weight, p.param_bf16, 1.0f, p.width, at + q, bits + q, w);
     return w[kLean ? 0 : q];
   };
 #pragma unroll
@@ -223,7 +245,6 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
     const Span sg = row_of<kBf16, kRagged>(p.gy, p.ld_gy, row, p.width, packs);
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) {
-      if (!bits[q]) continue;
       sx.load(next_x[q], at[q]);
       sg.load(next_g[q], at[q]);
     }
@@ -251,9 +272,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
       const float* const wq = weights(q);
 #pragma unroll
       for (int j = 0; j < kEpv; ++j) {
-        if (!((bits[q] >> j) & 1u)) continue;
-        const float gy = g[q].get(j);
-        const float xh = (x[q].get(j) - mean) * rstd;
+        const bool own = own_element<kRagged>(bits[q], j);
+        const float gy = own ? g[q].get(j) : 0.0f;
+        const float xh = own ? (x[q].get(j) - mean) * rstd : 0.0f;
         const float qq = gy * wq[j];
         v[0] = fmaf(qq, xh, v[0]);
         if constexpr (!kRms) v[1] += qq;
@@ -262,10 +283,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
           gb[q][j] += gy;
         }
       }
-    }
+      if constexpr (!kLean)  // added here, and not at the end of the row
 #pragma unroll
-    for (int q = 0; q < kPacks; ++q) {  // unpacked again, rather than kept
-      x[q].fence();
+        for (int j = 0; j < kEpv; ++j) asm volatile("" : "+v"(gw[q][j]), "+v"(gb[q][j]));
+      x[q].fence();                       // unpacked again, rather than kept
       g[q].fence();
     }
     row_sums<kOneWave>(v, s_sum, waves, turn);
@@ -298,43 +319,37 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_rows(NormParams p) {
   for (int q = 0; q < kPacks; ++q) keep_alive(data[q]);
   if constexpr (!kLean) {
     if (!p.part) return;
+    // The rows' sums side by side through LDS, where columns lie in order, so that they
+    // are stored in order: added over the waves that have rows of their own, one after
+    // the other.
+    extern __shared__ float s_col[];
+    constexpr int kTurn = col_packs(kOneWave, kPacks);
+    const int cols = threads * kTurn * kEpv;
+    const int side = kOneWave ? waves : 1;
+    float* const mine = s_col + slot * cols;
     float* const part = p.part + (long long)blockIdx.x * 2 * p.width;
-    if constexpr (kOneWave) {
-      // the waves' sums one after the other
-      __shared__ float s_col[kWave * kPacks * kEpv];
 #pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        if (!(which ? p.gb : p.gw)) continue;
-        for (int w = 0; w < waves; ++w) {
-          if (w == slot)
+    for (int which = 0; which < 2; ++which) {
+      if (!(which ? p.gb : p.gw)) continue;
 #pragma unroll
-            for (int q = 0; q < kPacks; ++q)
+      for (int q0 = 0; q0 < kPacks; q0 += kTurn) {
 #pragma unroll
-              for (int j = 0; j < kEpv; ++j) {
-                const int i = (q * kEpv + j) * kWave + tid;
-                const float v = which ? gb[q][j] : gw[q][j];
-                s_col[i] = w ? s_col[i] + v : v;
-              }
-          __syncthreads();
+        for (int q = 0; q < kTurn; ++q)
+#pragma unroll
+          for (int j = 0; j < kEpv; ++j)
+            mine[(q * threads + tid) * kEpv + j] = which ? gb[q0 + q][j] : gw[q0 + q][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < cols; i += blockDim.x) {
+          // element i % kEpv of the pack at e, which lies further left where it sticks out
+          const int e = q0 * threads * kEpv + i / kEpv * kEpv;
+          const int col = (kRagged ? inside_row(e, p.width > kEpv ? p.width - kEpv : 0) : e) + i % kEpv;
+          if (e >= p.width || col < e || col >= p.width) continue;
+          float v = s_col[i];
+          for (int w = 1; w < side; ++w) v += s_col[w * cols + i];
+          part[which * p.width + col] = v;
         }
-        if (slot == 0)
-#pragma unroll
-          for (int q = 0; q < kPacks; ++q)
-#pragma unroll
-            for (int j = 0; j < kEpv; ++j)
-              if ((bits[q] >> j) & 1u)
-                part[which * p.width + at[q] + j] = s_col[(q * kEpv + j) * kWave + tid];
         __syncthreads();
       }
-    } else {
-#pragma unroll
-      for (int q = 0; q < kPacks; ++q)
-#pragma unroll
-        for (int j = 0; j < kEpv; ++j) {
-          if (!((bits[q] >> j) & 1u)) continue;
-          if (p.gw) part[at[q] + j] = gw[q][j];
-          if (p.gb) part[p.width + at[q] + j] = gb[q][j];
-        }
     }
   }
 }
@@ -399,16 +414,21 @@ struct NormShape {
 };
 
 // Rows of up to 128 packs (backward 256) take one wave, which needs no barrier:
-// 65,536 bf16 rows of 2,048 backward (root mean square) take 144 us with four packs
-// a lane and four rows a workgroup, 145 to 153 with two or four waves to a row; of
-// 512, 45 us with eight rows a workgroup, 48 with four, 54 with two.  Wider rows take
-// two packs a thread while 512 threads suffice (65,536 of 4,096 backward: 300 us, with
-// four packs 310, with one 320), then four, and eight for fp32 rows past 8,192.
-// The workgroups are those that the registers let the card hold at once, 16 waves a
-// CU up to two packs and eight beyond: more would wait for the first to end, and
-// backward would leave more partial sums (8,192 rows of 16,384: 228 us with 256, 247
-// with 512, 292 with 1,024; 65,536 of 4,096: 322 with 512, 300 with 1,024, 315 with
-// 2,048).
+// backward, 12,000 bf16 rows of 2,048 (root mean square) take 32 us with four packs a
+// lane and four rows a workgroup, 34 to 38 with two waves to a row, and 65,536 of 1,500
+// 149 against 163 to 183 (of 2,048 149 against 141 to 155); with one pack, eight rows a
+// workgroup: 65,536 of 512 took 45 us, with four rows 48, with two 54.  Wider rows take
+// two packs a thread while 512 threads suffice (65,536 of 4,096 backward, layer form:
+// 275 us; in one sweep 302, with four packs 327, with one 312), then four, and eight for fp32 rows past 8,192.
+// The workgroups go from row to row, so they are no more than the registers let the
+// card hold at once, and backward fewer: what reads two streams and writes a third
+// slows down with more of them in flight, and each leaves partial sums.  Forward 16
+// waves a CU up to two packs (65,536 of 4,096: 192 us, with 8 waves 250, with 24 214).
+// Backward, two packs a thread: two workgroups of four waves or more (65,536 of 4,096:
+// 302 us, with three 324, with four 337; 50,000 of 5,000: 314, with three 343), smaller
+// ones up to 12 waves (65,536 of 2,056: 193, with 8 waves 234); a wave per row: 16 waves
+// of one pack (65,536 of 512: 40, with 8 waves 44), 8 of two (of 1,000: 73, with 16 82).
+// Beyond two packs 8 waves.
 NormShape norm_shape(long long width, int epv, bool bwd) {
   const int packs = (int)((width + epv - 1) / epv);
   NormShape s{};
@@ -422,7 +442,9 @@ NormShape norm_shape(long long width, int epv, bool bwd) {
     s.rows = 1;
     s.threads = ((packs + s.packs - 1) / s.packs + kWave - 1) / kWave * kWave;
   }
-  const int per_cu = (s.packs <= 2 ? 16 : 8) / (s.threads / kWave);
+  const int waves = s.threads / kWave;
+  int per_cu = (s.packs <= 2 ? 16 : 8) / waves;
+  if (bwd && s.packs == 2) per_cu = s.one_wave ? 1 : waves >= 4 ? 2 : 12 / waves;
   s.groups = 256 * (per_cu < 1 ? 1 : per_cu);
   return s;
 }
@@ -437,8 +459,11 @@ int groups_of(const NormShape& s, long long n_rows, bool bwd) {
 
 template <bool kBwd, bool kBf16, bool kRagged, bool kRms, bool kOneWave, int kPacks>
 void launch_one(const NormParams& p, const NormShape& n, hipStream_t s) {
+  constexpr int kEpv = kBf16 ? 8 : 4;
+  const size_t lds =
+      kPacks <= 4 && p.part ? (size_t)n.threads * col_packs(kOneWave, kPacks) * kEpv * sizeof(float) : 0;
   if constexpr (kBwd)
-    norm_bwd_rows<kBf16, kRagged, kRms, kOneWave, kPacks><<<p.n_groups, n.threads, 0, s>>>(p);
+    norm_bwd_rows<kBf16, kRagged, kRms, kOneWave, kPacks><<<p.n_groups, n.threads, lds, s>>>(p);
   else
     norm_fwd_rows<kBf16, kRagged, kRms, kOneWave, kPacks>
         <<<groups_of(n, p.n_rows, false), n.threads, 0, s>>>(p);
