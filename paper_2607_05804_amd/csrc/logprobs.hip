@@ -630,7 +630,10 @@ __global__ __launch_bounds__(kLpThreads, kBf16 && kTop && !kRagged ? 4 : rows_a_
   }
 }
 
-// Joins the chunks of a row: one workgroup per row.
+// Joins the chunks of a row: one workgroup per row.  The first candidates are loaded
+// before anything is waited for, and one wave adds the sums while another looks for the
+// bound: few rows wait for nothing but this chain (64 bf16 rows of 151,936, k = 5: 4.5 us).
+constexpr int kJoinEach = 3;  // candidates that a thread keeps
 __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
   __shared__ float s_row[2];
   __shared__ unsigned s_max[kLpThreads];
@@ -640,60 +643,99 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
   __shared__ int s_n;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
+  const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int total = p.n_chunks * p.k;
   for (long long row = blockIdx.x; row < p.n_rows; row += gridDim.x) {
     if (p.mask && !p.mask[row]) continue;  // written by the row kernel
-    if (tid < kWave) {
-      // a chunk per lane and turn, joined in a fixed tree
-      const float* const part = p.part + row * p.n_chunks * kLogprobPart;
-      const Given given = given_of(p, row);
-      Sums t{-INFINITY, 0.0f, 0.0f};
-      for (int c = lane; c < p.n_chunks; c += kWave) t.m = fmaxf(t.m, part[c * kLogprobPart]);
+    const unsigned long long* const in = p.cand + row * total;
+    unsigned long long got[kJoinEach];
+#pragma unroll
+    for (int q = 0; q < kJoinEach; ++q) got[q] = q * kLpThreads + tid < total ? in[q * kLpThreads + tid] : 0ull;
+    // a chunk per lane and turn, joined in a fixed tree
+    const float* const part = p.part + row * p.n_chunks * kLogprobPart;
+    Given given{};
+    float m = -INFINITY, s = 0.0f, a = 0.0f;
+    if (wid == 0) {
+      given = given_of(p, row);
+      if (lane < p.n_chunks) {
+        m = part[lane * kLogprobPart];
+        s = part[lane * kLogprobPart + 1];
+        a = part[lane * kLogprobPart + 2];
+      }
+    }
+    if (tid == 0) s_n = 0;
+    if (p.k > 0) {
+      // The chunks' lists are sorted: the first of each, by as many threads as there are
+      // (by chunk, then rank), bound the k-th largest of all closely.
+      const int rank = tid / p.n_chunks, c0 = tid - rank * p.n_chunks;
+      unsigned long long best = 0;
+      if (rank < p.k)
+        for (int c = c0; c < p.n_chunks; c += kLpThreads) {
+          const unsigned long long x = in[(long long)c * p.k + rank];
+          best = x > best ? x : best;
+        }
+      s_max[tid] = (unsigned)(best >> 32);
+    }
+    __syncthreads();
+    if (wid == 0) {
+      Sums t{m, 0.0f, 0.0f};
+      for (int c = lane + kWave; c < p.n_chunks; c += kWave) t.m = fmaxf(t.m, part[c * kLogprobPart]);
       t.m = wave_max_dpp(t.m);
-      for (int c = lane; c < p.n_chunks; c += kWave)
+      if (lane < p.n_chunks) add_part(t, m, s, a);
+      for (int c = lane + kWave; c < p.n_chunks; c += kWave)
         add_part(t, part[c * kLogprobPart], part[c * kLogprobPart + 1], part[c * kLogprobPart + 2]);
       t.s = wave_sum_dpp(t.s);
       t.a = wave_sum_dpp(t.a);
-      if (tid == 0) {
+      if (lane == 0) {
         write_row(p, row, t.m, t.s, t.a, given);
         s_row[0] = t.m;
         s_row[1] = log_sum(t.m, t.s);
-        s_n = 0;
       }
-    }
-    if (p.k > 0) {
-      const unsigned long long* const in = p.cand + row * p.n_chunks * p.k;
-      const int total = p.n_chunks * p.k;
-      unsigned long long best = 0;
-      for (int j = tid; j < total; j += kLpThreads) best = in[j] > best ? in[j] : best;
-      s_max[tid] = (unsigned)(best >> 32);
-      __syncthreads();
-      if (tid < kWave) {
-        unsigned v[kLpWaves];
+    } else if (wid == 1 && p.k > 0) {
+      unsigned v[kLpWaves];
 #pragma unroll
-        for (int q = 0; q < kLpWaves; ++q) v[q] = s_max[q * kWave + lane];
-        const unsigned t = p.bf16 ? kth_largest<16>(v, p.k) : kth_largest<8>(v, p.k);
-        // numbers of 0 stand for no element
-        if (lane == 0) s_floor = t ? (unsigned long long)t << 32 : 1ull;
-      }
-      __syncthreads();
+      for (int q = 0; q < kLpWaves; ++q) v[q] = s_max[q * kWave + lane];
+      const unsigned t = p.bf16 ? kth_largest<16>(v, p.k) : kth_largest<8>(v, p.k);
+      // numbers of 0 stand for no element
+      if (lane == 0) s_floor = t ? (unsigned long long)t << 32 : 1ull;
+    }
+    __syncthreads();
+    if (p.k > 0) {
       Best list{s_cand, s_kept, &s_n, &s_floor};
-      int held = 0;
-      for (int base = 0; base < total;) {
-        if (kCand - held < kLpThreads) {
-          list.cut(held, p.k);
-          held = s_n;
-        }
-        const unsigned long long y = base + tid < total ? in[base + tid] : 0ull;
-        const bool in = y >= s_floor;
-        const unsigned long long who = __ballot(in);
+      auto add = [&](unsigned long long y, unsigned long long least) {
+        const bool reaches = y >= least;
+        const unsigned long long who = __ballot(reaches);
         int first = 0;
         if (lane == 0 && who) first = atomicAdd(&s_n, __popcll(who));
         first = __builtin_amdgcn_readfirstlane(first);
-        if (in) s_cand[first + __popcll(who & ((1ull << lane) - 1ull))] = y;
+        const int to = first + __popcll(who & ((1ull << lane) - 1ull));
+        if (reaches && to < kCand) s_cand[to] = y;
+      };
+      const unsigned long long least = s_floor;
+#pragma unroll
+      for (int q = 0; q < kJoinEach; ++q) add(got[q], least);
+#pragma unroll 4
+      for (int base = kJoinEach * kLpThreads; base < total; base += kLpThreads)
+        add(base + tid < total ? in[base + tid] : 0ull, least);
+      __syncthreads();
+      int held = s_n;
+      if (held > kCand) {  // in steps, as in the row kernel
         __syncthreads();
-        held = s_n;
-        base += kLpThreads;
-        if (base < total) __syncthreads();  // all have read it before the next step adds to it
+        if (tid == 0) s_n = 0;
+        __syncthreads();
+        held = 0;
+        for (int base = 0; base < total;) {
+          if (kCand - held < kLpThreads) {
+            list.cut(held, p.k);
+            held = s_n;
+            __syncthreads();  // all have read it before the next step adds to it
+          }
+          add(base + tid < total ? in[base + tid] : 0ull, s_floor);
+          __syncthreads();
+          held = s_n;
+          base += kLpThreads;
+          if (base < total) __syncthreads();
+        }
       }
       list.ranks(held, [&](unsigned long long x, int r) {
         if (r < p.k) write_alternative(p, row, r, x, s_row[0], s_row[1]);
@@ -744,13 +786,19 @@ __global__ __launch_bounds__(kLpThreads, kPacks > 8 ? 3 : 4) void logprob_short(
       at[q] = span.place(q * kWave + lane, bits[q]);
       span.load(x[q], at[q]);
     }
-    auto own = [&](int q, int j) { return kRagged ? ((bits[q] >> j) & 1u) != 0 : bits[q] != 0; };
+    // Others' elements count as -inf.  Of rows of any start whole packs are passed over
+    // and only the packs at the ends are made so (4,500 rows of 2,136, k = 26: 23 to 18
+    // us); of rows of whole packs, whose loops then spill, every lane's pack is asked.
+    auto live = [&](int q) { return !kRagged || q * kWave < span.n; };
+    auto value = [&](int q, int j) { return kRagged || bits[q] ? x[q].get(j) : -INFINITY; };
     float top[kPacks], best = -INFINITY;
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) {
       top[q] = -INFINITY;
+      if (!live(q)) continue;
+      if (kRagged && __any(bits[q] != (1u << kEpv) - 1u)) forbid(x[q], bits[q]);
 #pragma unroll
-      for (int j = 0; j < kEpv; ++j) top[q] = fmaxf(top[q], own(q, j) ? x[q].get(j) : -INFINITY);
+      for (int j = 0; j < kEpv; ++j) top[q] = fmaxf(top[q], value(q, j));
       best = fmaxf(best, top[q]);
       x[q].fence();  // unpacked again, rather than kept
     }
@@ -759,9 +807,10 @@ __global__ __launch_bounds__(kLpThreads, kPacks > 8 ? 3 : 4) void logprob_short(
     float s = 0.0f, a = 0.0f;
 #pragma unroll
     for (int q = 0; q < kPacks; ++q) {
+      if (!live(q)) continue;
 #pragma unroll
       for (int j = 0; j < kEpv; ++j) {
-        const float y = own(q, j) ? (x[q].get(j) - u) * kLog2e : kFloor;
+        const float y = (value(q, j) - u) * kLog2e;
         const float e = exp2_fast(y);
         s += e;
         a = fmaf(e, fmaxf(y, kFloor), a);
@@ -900,14 +949,16 @@ __global__ __launch_bounds__(kLpThreads, kPacks > 8 ? 3 : 4) void logprob_short(
 
 constexpr int kMaxChunkElems = 24 * kGroupElems;  // and one group more for rows of any start: 50 units a lane
 constexpr int kMinChunkElems = 4096;
-constexpr int kFillTasks = 1280;
+constexpr int kFillTasks = 768;  // three workgroups a CU, which every variant has room for
 constexpr int kJoinGrid = 1 << 20;  // workgroups; beyond, each takes several rows
 
 }  // namespace
 
 // Chunks of a row: as many as its units' LDS asks for, and for few rows so many
 // that they fill the card, of 4,096 elements at least (a depth that depends on sizes
-// only, so that the workspace can be sized for it).
+// only, so that the workspace can be sized for it; with 1,280 tasks 173 fp32 rows of
+// 45,230, k = 3, took 25.5 us instead of 20.6, 64 bf16 rows of 151,936, k = 128, 29.1
+// instead of 25.9, but k = 0 11.3 instead of 12.2).
 int logprob_chunks(long long n_rows, long long vocab) {
   // ragged rows hold up to 64 elements more, and boundaries move by eight packs
   const int by_size = (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);

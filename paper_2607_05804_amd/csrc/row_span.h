@@ -7,6 +7,19 @@
 namespace turnkl {
 namespace {
 
+// A pack with -inf in place of the elements outside `bits`.
+__device__ inline void forbid(Pack<true, 8>& x, unsigned bits) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const unsigned keep = ((bits >> (2 * k)) & 1u ? 0xFFFFu : 0u) | ((bits >> (2 * k + 1)) & 1u ? 0xFFFF0000u : 0u);
+    x.w[k] = (x.w[k] & keep) | (0xFF80FF80u & ~keep);
+  }
+}
+__device__ inline void forbid(Pack<false, 4>& x, unsigned bits) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x.f[j] = (bits >> j) & 1u ? x.f[j] : -INFINITY;
+}
+
 // Computes the data of a store here, before any of the stores (whose own data must
 // not be rewritten closely behind them), and not where it is stored.
 __device__ inline void settle(u32x4& x) { asm volatile("" : "+v"(x)); }
