@@ -416,7 +416,8 @@ struct NormShape {
 // Rows of up to 128 packs (backward 256) take one wave, which needs no barrier:
 // backward, 12,000 bf16 rows of 2,048 (root mean square) take 32 us with four packs a
 // lane and four rows a workgroup, 34 to 38 with two waves to a row, and 65,536 of 1,500
-// 149 against 163 to 183 (of 2,048 149 against 141 to 155); with one pack, eight rows a
+// 149 against 163 to 183 (112 with the three packs that such a row fills; of 2,048 149
+// against 141 to 155); with one pack, eight rows a
 // workgroup: 65,536 of 512 took 45 us, with four rows 48, with two 54.  Wider rows take
 // two packs a thread while 512 threads suffice (65,536 of 4,096 backward, layer form:
 // 275 us; in one sweep 302, with four packs 327, with one 312), then four, and eight for fp32 rows past 8,192.
@@ -434,8 +435,8 @@ NormShape norm_shape(long long width, int epv, bool bwd) {
   NormShape s{};
   s.one_wave = packs <= (bwd ? 256 : 128);
   if (s.one_wave) {
-    s.packs = packs <= 64 ? 1 : packs <= 128 ? 2 : 4;
-    s.rows = bwd && s.packs < 4 ? 8 : 4;
+    s.packs = (packs + 63) / 64;
+    s.rows = bwd && s.packs <= 2 ? 8 : 4;
     s.threads = s.rows * kWave;
   } else {
     s.packs = packs <= 2 * kNormThreads ? 2 : packs <= kSumPacks ? 4 : 8;
@@ -477,7 +478,8 @@ void launch_sized(const NormParams& p, hipStream_t s) {
   else if (n.packs == 2) launch_one<kBwd, kBf16, kRagged, kRms, false, 2>(p, n, s);
   else if (!n.one_wave && n.packs == 4) launch_one<kBwd, kBf16, kRagged, kRms, false, 4>(p, n, s);
   else if constexpr (kBwd) {
-    if (n.one_wave) launch_one<kBwd, kBf16, kRagged, kRms, true, 4>(p, n, s);
+    if (n.one_wave && n.packs == 3) launch_one<kBwd, kBf16, kRagged, kRms, true, 3>(p, n, s);
+    else if (n.one_wave) launch_one<kBwd, kBf16, kRagged, kRms, true, 4>(p, n, s);
     else if constexpr (!kBf16) launch_one<kBwd, kBf16, kRagged, kRms, false, 8>(p, n, s);
   } else if constexpr (!kBf16) {
     launch_one<kBwd, kBf16, kRagged, kRms, false, 8>(p, n, s);
