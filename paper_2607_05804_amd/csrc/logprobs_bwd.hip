@@ -3,7 +3,8 @@
 //   G = gl ([v = t] - p) - gh p (x + H) = gl [v = t] - p (gl + gh (x + H)),
 // element by element from the row's saved (M, L) and H; no row waits for another.
 // x is held above kLogFloor in the product, so that a forbidden token (p = 0)
-// gives 0 and not 0 * inf.
+// gives 0 and not 0 * inf.  Bound: HBM (16,384 bf16 rows of 151,936, 60% asked for, the
+// others written as zeros without being read: 1,426 us, 5.6 TB/s).
 
 #include "row_span.h"
 

@@ -417,19 +417,21 @@ struct NormShape {
 // backward, 12,000 bf16 rows of 2,048 (root mean square) take 32 us with four packs a
 // lane and four rows a workgroup, 34 to 38 with two waves to a row, and 65,536 of 1,500
 // 149 against 163 to 183 (112 with the three packs that such a row fills; of 2,048 149
-// against 141 to 155); with one pack, eight rows a
-// workgroup: 65,536 of 512 took 45 us, with four rows 48, with two 54.  Wider rows take
-// two packs a thread while 512 threads suffice (65,536 of 4,096 backward, layer form:
-// 275 us; in one sweep 302, with four packs 327, with one 312), then four, and eight for fp32 rows past 8,192.
+// against 141 to 155); with one pack, eight rows a workgroup: 65,536 of 512 took 45 us,
+// with four rows 48, with two 54.  Wider rows take two packs a thread while 512 threads
+// suffice (65,536 of 4,096 backward, layer form: 275 us, with four packs 327, with one
+// 312), then four, and eight for fp32 rows past 8,192.
 // The workgroups go from row to row, so they are no more than the registers let the
 // card hold at once, and backward fewer: what reads two streams and writes a third
 // slows down with more of them in flight, and each leaves partial sums.  Forward 16
 // waves a CU up to two packs (65,536 of 4,096: 192 us, with 8 waves 250, with 24 214).
-// Backward, two packs a thread: two workgroups of four waves or more (65,536 of 4,096:
-// 302 us, with three 324, with four 337; 50,000 of 5,000: 314, with three 343), smaller
-// ones up to 12 waves (65,536 of 2,056: 193, with 8 waves 234); a wave per row: 16 waves
-// of one pack (65,536 of 512: 40, with 8 waves 44), 8 of two (of 1,000: 73, with 16 82).
-// Beyond two packs 8 waves.
+// Backward by measurement, workgroups a CU for 65,536 bf16 rows: with a row to a
+// workgroup and two packs a thread two (of 4,096: 279 us, with three 307, with four 338;
+// of 3,800 284, 316, 325), of shorter rows three (of 3,500: 306, with two 366) or four (of
+// 2,500: 232, with two 338); with a wave per row two (of 512: 40, with one 44; of 1,500:
+// 122, with one 177, with three 153), but one where eight rows of more than 85 packs lie
+// side by side (of 1,000: 73, with two 82; of 600 two again: 55, with one 65).
+// With a row to a workgroup and more packs a thread 8 waves.
 NormShape norm_shape(long long width, int epv, bool bwd) {
   const int packs = (int)((width + epv - 1) / epv);
   NormShape s{};
@@ -445,7 +447,9 @@ NormShape norm_shape(long long width, int epv, bool bwd) {
   }
   const int waves = s.threads / kWave;
   int per_cu = (s.packs <= 2 ? 16 : 8) / waves;
-  if (bwd && s.packs == 2) per_cu = s.one_wave ? 1 : waves >= 4 ? 2 : 12 / waves;
+  const int pieces = (packs + kWave - 1) / kWave;
+  if (bwd && s.one_wave) per_cu = pieces == 2 && packs > 85 ? 1 : 2;
+  else if (bwd && s.packs == 2) per_cu = pieces < 8 ? 24 / pieces : 2;
   s.groups = 256 * (per_cu < 1 ? 1 : per_cu);
   return s;
 }
