@@ -26,6 +26,7 @@
 
 #include <type_traits>
 
+#include "candidate_walk.h"
 #include "row_span.h"
 
 namespace turnkl {
@@ -600,20 +601,10 @@ __global__ __launch_bounds__(kLpThreads, kBf16 && kTop && !kRagged ? 4 : rows_a_
         __syncthreads();
         if (tid == 0) s_n = 0;
         __syncthreads();
-        held = 0;
-        for (int base = 0; base < n;) {
-          if (kCand - held < 16 * kEpv) {
-            list.cut(held, p.k);
-            held = s_n;
-          }
-          const int room = (kCand - held) / kEpv;
-          const int step = room < kLpThreads ? room : kLpThreads;
-          gather(tid < step && base + tid < n ? base + tid : -1, s_floor);
-          __syncthreads();
-          held = s_n;
-          base += step;
-          if (base < n) __syncthreads();  // all have read it before the next step adds to it
-        }
+        held = walk_candidates(
+            n, kEpv, 16 * kEpv, kLpThreads, kCand, p.k, [&](int all) { list.cut(all, p.k); },
+            [&](int base, int step) { gather(tid < step && base + tid < n ? base + tid : -1, s_floor); },
+            [&] { return s_n; }, [] { __syncthreads(); });
       }
       if (p.n_chunks == 1) {
         const float l = log_sum(t.m, t.s);
@@ -729,19 +720,10 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
         __syncthreads();
         if (tid == 0) s_n = 0;
         __syncthreads();
-        held = 0;
-        for (int base = 0; base < total;) {
-          if (kCand - held < kLpThreads) {
-            list.cut(held, p.k);
-            held = s_n;
-            __syncthreads();  // all have read it before the next step adds to it
-          }
-          add(base + tid < total ? in[base + tid] : 0ull, s_floor);
-          __syncthreads();
-          held = s_n;
-          base += kLpThreads;
-          if (base < total) __syncthreads();
-        }
+        held = walk_candidates(
+            total, 1, kLpThreads, kLpThreads, kCand, p.k, [&](int all) { list.cut(all, p.k); },
+            [&](int base, int) { add(base + tid < total ? in[base + tid] : 0ull, s_floor); },
+            [&] { return s_n; }, [] { __syncthreads(); });
       }
       list.ranks(held, [&](unsigned long long x, int r) {
         if (r < p.k) write_alternative(p, row, r, x, s_row[0], s_row[1]);
