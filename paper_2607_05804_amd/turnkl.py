@@ -718,11 +718,10 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
                     (n and t.stride()[1] != 1):
                 raise ValueError(f"{name} must be {dtype} [n_tokens, k] on cuda:{index} with unit "
                                  "column stride")
-        strides = top_ids.stride()
-        if strides != top_logp.stride():
+        if top_ids.stride() != top_logp.stride():
             raise ValueError("top_ids and top_logp must share a row stride")
-        ld_top = max(strides[0], k)
-        top_ids, top_logp = top_ids.data_ptr(), top_logp.data_ptr()
+        top_ids, ld_top = _matrix(top_ids, n, k)
+        top_logp = top_logp.data_ptr()
     if workspace is None:
         workspace = LogprobsWorkspace(n, v, k, device=logits.device)
     rc = lib().turnkl_token_logprobs(
