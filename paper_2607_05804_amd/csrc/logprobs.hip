@@ -38,7 +38,10 @@ constexpr int kGroupElems = 32 * kLpThreads;  // elements of a group: 32 a lane
 __host__ __device__ constexpr int group_packs(bool bf16) { return bf16 ? 4 : 8; }  // a lane's packs of it
 constexpr float kSlack = 8.0f;           // logit units
 constexpr float kFloor = -256.0f;        // log2 units: 2^kFloor is zero
-constexpr float kHuge = 1e38f;           // log2 e times it is a float still
+// Rows with a larger |M| are summed again: log2 e times the reference is rounded, here by
+// up to eight, which x then carries until the waves are joined, and A's sum with it; from
+// 1.5e9 on the rounding alone takes every 2^x out of a float's range.
+constexpr float kHuge = 1e8f;
 constexpr int kCand = 896;        // elements held for ranking: k and a step's, at least
 constexpr int kList = 384;         // units held for a second look
 
