@@ -392,8 +392,10 @@ int turnkl_fwd_bwd_topk(const void* student_logits, int64_t ld_student, int dtyp
 /*
  * Bytes of device workspace turnkl_token_logprobs needs (host; a pure function
  * of its arguments), 0 when they are invalid (n_tokens < 0, vocab < 1 or above
- * 2^24, k outside 0 .. min(TURNKL_MAX_ALTERNATIVES, vocab)).  The workspace
- * needs no initialisation; it must be 256-byte aligned.
+ * 2^24, k outside 0 .. min(TURNKL_MAX_ALTERNATIVES, vocab)).  It does not fall
+ * as an argument grows: a workspace for the largest batch serves smaller ones,
+ * smaller vocabularies and fewer alternatives.  The workspace needs no
+ * initialisation; it must be 256-byte aligned.
  */
 size_t turnkl_token_logprobs_workspace_bytes(int64_t n_tokens, int64_t vocab, int32_t k);
 

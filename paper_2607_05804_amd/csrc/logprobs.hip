@@ -952,13 +952,26 @@ constexpr int kJoinGrid = 1 << 20;  // workgroups; beyond, each takes several ro
 // only, so that the workspace can be sized for it; with 1,280 tasks 173 fp32 rows of
 // 45,230, k = 3, took 25.5 us instead of 20.6, 64 bf16 rows of 151,936, k = 128, 29.1
 // instead of 25.9, but k = 0 11.3 instead of 12.2).
-int logprob_chunks(long long n_rows, long long vocab) {
+static int chunks_by_size(long long vocab) {
   // ragged rows hold up to 64 elements more, and boundaries move by eight packs
-  const int by_size = (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);
+  return (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);
+}
+int logprob_chunks(long long n_rows, long long vocab) {
+  const int by_size = chunks_by_size(vocab);
   if (n_rows < 1) return by_size;
   const long long fill = kFillTasks / n_rows, most = vocab / kMinChunkElems;
   const int by_rows = (int)(fill < most ? fill : most);
   return by_rows > by_size ? by_rows : by_size;
+}
+
+// Chunks of all rows together of any batch up to n_rows rows, where they are joined:
+// the workspace has room for as many, so that one for n_rows rows serves fewer too, of
+// which each is split into more.
+long long logprob_room(long long n_rows, long long vocab) {
+  const long long by_size = chunks_by_size(vocab), most = vocab / kMinChunkElems;
+  const long long split = most > 1 ? (n_rows * most < kFillTasks ? n_rows * most : kFillTasks) : 0;
+  const long long whole = by_size > 1 ? n_rows * by_size : 0;
+  return split > whole ? split : whole;
 }
 
 template <bool kBf16, bool kRagged, bool kTop>

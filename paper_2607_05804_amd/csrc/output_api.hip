@@ -24,7 +24,7 @@ bool logprob_sizes_ok(int64_t n_tokens, int64_t vocab, int32_t k) {
 LogprobLayout logprob_layout(int64_t n_tokens, int64_t vocab, int32_t k) {
   LogprobLayout L{};
   L.n_chunks = logprob_chunks(n_tokens, vocab);
-  const size_t tasks = L.n_chunks > 1 ? (size_t)n_tokens * (size_t)L.n_chunks : 0;
+  const size_t tasks = (size_t)logprob_room(n_tokens, vocab);
   L.rows = align256(sizeof(Header));
   L.part = align256(L.rows + (size_t)n_tokens * sizeof(int));
   L.cand = align256(L.part + tasks * kLogprobPart * sizeof(float));

@@ -425,6 +425,7 @@ struct LogprobGradParams {
 };
 
 int logprob_chunks(long long n_rows, long long vocab);
+long long logprob_room(long long n_rows, long long vocab);
 hipError_t launch_logprobs(const LogprobParams& p, hipStream_t s);
 hipError_t launch_logprobs_bwd(const LogprobGradParams& p, hipStream_t s);
 

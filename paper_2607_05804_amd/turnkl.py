@@ -668,7 +668,8 @@ def new_token_logprobs(n_tokens: int, k: int = 0, device="cuda", logp: bool = Tr
 
 
 class LogprobsWorkspace(Workspace):
-    """Caller-owned device scratch for turnkl_token_logprobs."""
+    """Caller-owned device scratch for turnkl_token_logprobs of up to n_tokens rows, vocab
+    columns and k alternatives."""
 
     def __init__(self, n_tokens: int, vocab: int, k: int = 0, device="cuda"):
         nbytes = int(lib().turnkl_token_logprobs_workspace_bytes(n_tokens, vocab, k))
