@@ -976,8 +976,8 @@ long long logprob_room(long long n_rows, long long vocab) {
 
 template <bool kBf16, bool kRagged, bool kTop>
 void launch_short(const LogprobParams& p, int packs, hipStream_t s) {
-  const int blocks = (p.n_rows + kLpWaves - 1) / kLpWaves;
-  const int grid = blocks < kShortGrid ? blocks : kShortGrid;
+  const long long blocks = ((long long)p.n_rows + kLpWaves - 1) / kLpWaves;
+  const int grid = (int)(blocks < kShortGrid ? blocks : kShortGrid);
   if (packs <= kWave) logprob_short<kBf16, kRagged, 1, kTop><<<grid, kLpThreads, 0, s>>>(p);
   else if (packs <= 2 * kWave) logprob_short<kBf16, kRagged, 2, kTop><<<grid, kLpThreads, 0, s>>>(p);
   else if (packs <= 4 * kWave) logprob_short<kBf16, kRagged, 4, kTop><<<grid, kLpThreads, 0, s>>>(p);
