@@ -321,7 +321,26 @@ def _rows_aligned(*tensors) -> bool:
     return True
 
 
-class Workspace:
+class _Scratch:
+    """Caller-owned device memory of a call (a uint8 torch tensor) of the size that the
+    library's function `sizes` gave, which is 0 for invalid arguments."""
+
+    def __init__(self, nbytes: int, sizes: str, device):
+        if nbytes == 0:
+            raise TurnKLError(ERR_INVALID_ARG, sizes)
+        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.nbytes = nbytes
+
+
+class _StatusScratch(_Scratch):
+    """Scratch of a call that leaves a status there."""
+
+    def status(self) -> int:
+        stream = torch.cuda.current_stream().cuda_stream
+        return int(lib().turnkl_get_status(_ptr(self.tensor), ctypes.c_void_p(stream)))
+
+
+class Workspace(_StatusScratch):
     """Caller-owned device scratch for turnkl_fwd_bwd (a uint8 torch tensor).
 
     aligned_rows: the calls it serves pass logit and gradient rows that start
@@ -330,16 +349,9 @@ class Workspace:
 
     def __init__(self, n_tokens: int, vocab: int, dtype: int, max_turns: int, device="cuda",
                  aligned_rows: bool = True):
-        nbytes = workspace_bytes(n_tokens, vocab, dtype, max_turns, aligned_rows)
-        if nbytes == 0:
-            raise TurnKLError(ERR_INVALID_ARG, "turnkl_workspace_bytes")
-        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.nbytes = nbytes
+        super().__init__(workspace_bytes(n_tokens, vocab, dtype, max_turns, aligned_rows),
+                         "turnkl_workspace_bytes", device)
         self.n_tokens = n_tokens
-
-    def status(self) -> int:
-        stream = torch.cuda.current_stream().cuda_stream
-        return int(lib().turnkl_get_status(_ptr(self.tensor), ctypes.c_void_p(stream)))
 
     def segments(self, device="cuda") -> dict:
         n = self.n_tokens
@@ -487,11 +499,8 @@ class TopkWorkspace(Workspace):
     """Caller-owned device scratch for turnkl_fwd_bwd_topk."""
 
     def __init__(self, n_tokens: int, k: int, max_turns: int, device="cuda"):
-        nbytes = int(lib().turnkl_topk_workspace_bytes(n_tokens, k, max_turns))
-        if nbytes == 0:
-            raise TurnKLError(ERR_INVALID_ARG, "turnkl_topk_workspace_bytes")
-        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.nbytes = nbytes
+        _Scratch.__init__(self, int(lib().turnkl_topk_workspace_bytes(n_tokens, k, max_turns)),
+                          "turnkl_topk_workspace_bytes", device)
         self.n_tokens = n_tokens
 
 
@@ -667,16 +676,13 @@ def new_token_logprobs(n_tokens: int, k: int = 0, device="cuda", logp: bool = Tr
         torch.empty((n_tokens, k), **f) if k else None)
 
 
-class LogprobsWorkspace(Workspace):
+class LogprobsWorkspace(_StatusScratch):
     """Caller-owned device scratch for turnkl_token_logprobs of up to n_tokens rows, vocab
     columns and k alternatives."""
 
     def __init__(self, n_tokens: int, vocab: int, k: int = 0, device="cuda"):
-        nbytes = int(lib().turnkl_token_logprobs_workspace_bytes(n_tokens, vocab, k))
-        if nbytes == 0:
-            raise TurnKLError(ERR_INVALID_ARG, "turnkl_token_logprobs_workspace_bytes")
-        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.nbytes = nbytes
+        super().__init__(int(lib().turnkl_token_logprobs_workspace_bytes(n_tokens, vocab, k)),
+                         "turnkl_token_logprobs_workspace_bytes", device)
         self.n_tokens = n_tokens
 
 
@@ -768,15 +774,12 @@ def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log
     return grad
 
 
-class NormWorkspace(Workspace):
-    """Caller-owned device scratch for turnkl_norm_bwd."""
+class NormWorkspace(_Scratch):
+    """Caller-owned device scratch for turnkl_norm_bwd of up to n_rows rows."""
 
     def __init__(self, n_rows: int, width: int, device="cuda"):
-        nbytes = int(lib().turnkl_norm_workspace_bytes(n_rows, width))
-        if nbytes == 0:
-            raise TurnKLError(ERR_INVALID_ARG, "turnkl_norm_workspace_bytes")
-        self.tensor = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.nbytes = nbytes
+        super().__init__(int(lib().turnkl_norm_workspace_bytes(n_rows, width)),
+                         "turnkl_norm_workspace_bytes", device)
 
 
 def _parameter(t: torch.Tensor | None, d: int, name: str, index: int):

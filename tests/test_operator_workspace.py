@@ -30,3 +30,19 @@ def test_norm_workspace_does_not_shrink():
     for d in (1, 64, 1000, 2048, 4097, 16384):
         sizes = [f(n, d) for n in range(0, 3000)]
         assert sizes == sorted(sizes), d
+
+
+def test_only_workspaces_that_hold_a_status_or_segments_are_asked_for_them():
+    """A norm's holds sums alone, that of log probabilities no segments."""
+    fused = T.Workspace(8, 64, T.F32, 4, device="cpu")
+    topk = T.TopkWorkspace(8, 4, 4, device="cpu")
+    logprobs = T.LogprobsWorkspace(8, 64, 4, device="cpu")
+    norm = T.NormWorkspace(8, 64, device="cpu")
+    for ws, status, segments in ((fused, True, True), (topk, True, True), (logprobs, True, False),
+                                 (norm, False, False)):
+        assert (hasattr(ws, "status"), hasattr(ws, "segments")) == (status, segments), ws
+        assert ws.tensor.numel() == ws.nbytes > 0
+    for bad in (lambda: T.Workspace(-1, 64, T.F32, 4, device="cpu"), lambda: T.TopkWorkspace(8, 0, 4, device="cpu"),
+                lambda: T.LogprobsWorkspace(8, 64, 65, device="cpu"), lambda: T.NormWorkspace(8, 0, device="cpu")):
+        with pytest.raises(T.TurnKLError):
+            bad()
