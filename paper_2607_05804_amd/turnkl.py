@@ -321,6 +321,16 @@ def _rows_aligned(*tensors) -> bool:
     return True
 
 
+def _on(index: int, call, *args) -> int:
+    """call(*args) with a device current: the address of the default stream is the same
+    on every device, and work on it goes to the current one.  (Asked for directly, which
+    takes 0.1 us: entering a device that is current already takes 0.5.)"""
+    if torch._C._cuda_getDevice() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
+
+
 class _Scratch:
     """Caller-owned device memory of a call (a uint8 torch tensor) of the size that the
     library's function `sizes` gave, which is 0 for invalid arguments."""
@@ -336,8 +346,10 @@ class _StatusScratch(_Scratch):
     """Scratch of a call that leaves a status there."""
 
     def status(self) -> int:
-        stream = torch.cuda.current_stream().cuda_stream
-        return int(lib().turnkl_get_status(_ptr(self.tensor), ctypes.c_void_p(stream)))
+        """The status that the last call left, read on the current stream of the workspace's
+        device, where that call went."""
+        index = self.tensor.get_device()
+        return int(_on(index, lib().turnkl_get_status, self.tensor.data_ptr(), _stream(index)))
 
 
 class Workspace(_StatusScratch):
@@ -353,13 +365,14 @@ class Workspace(_StatusScratch):
                          "turnkl_workspace_bytes", device)
         self.n_tokens = n_tokens
 
-    def segments(self, device="cuda") -> dict:
+    def segments(self, device=None) -> dict:
         n = self.n_tokens
-        bufs = [torch.empty(max(n, 1), dtype=torch.int32, device=device) for _ in range(5)]
+        bufs = [torch.empty(max(n, 1), dtype=torch.int32, device=device or self.tensor.device)
+                for _ in range(5)]
         n_seg = ctypes.c_int32(0)
-        stream = torch.cuda.current_stream().cuda_stream
-        rc = lib().turnkl_get_segments(_ptr(self.tensor), n, ctypes.c_void_p(stream),
-                                       ctypes.byref(n_seg), *[_ptr(b) for b in bufs])
+        index = self.tensor.get_device()
+        rc = _on(index, lib().turnkl_get_segments, self.tensor.data_ptr(), n, _stream(index),
+                 ctypes.byref(n_seg), *[_ptr(b) for b in bufs])
         if rc != OK:
             raise TurnKLError(rc, "turnkl_get_segments")
         k = n_seg.value
@@ -441,7 +454,8 @@ def fwd_bwd(student: torch.Tensor, teacher: torch.Tensor, turn_id: torch.Tensor,
     stream = torch.cuda.current_stream(dev).cuda_stream
     opts = _options(n, support_floor, support_frac, success, outcome_stats, token_weights,
                     token_lse, dev)
-    rc = lib().turnkl_fwd_bwd(
+    rc = _on(
+        student.get_device(), lib().turnkl_fwd_bwd,
         *_fused_args(student, teacher, dt, n, v, turn_id, traj_id, loss_mask, alpha, grad_scale,
                      loss, grad_t, turn_stats, max_turns, accumulate_stats, kl_t, opts),
         _ptr(workspace.tensor), workspace.nbytes, ctypes.c_void_p(stream))
@@ -487,7 +501,8 @@ def fwd_bwd_noalloc(student: torch.Tensor, teacher: torch.Tensor, turn_id: torch
     stream = torch.cuda.current_stream(dev).cuda_stream
     opts = _options(n, support_floor, support_frac, success, outcome_stats, token_weights,
                     token_lse, dev)
-    rc = lib().turnkl_fwd_bwd_noalloc(
+    rc = _on(
+        student.get_device(), lib().turnkl_fwd_bwd_noalloc,
         *_fused_args(student, teacher, dt, n, v, turn_id, traj_id, loss_mask, alpha, grad_scale,
                      loss, grad_t, turn_stats, max_turns, accumulate_stats, token_kl, opts),
         _ptr(status), ctypes.c_void_p(stream))
@@ -569,7 +584,8 @@ def fwd_bwd_topk(student: torch.Tensor, teacher_ids: torch.Tensor, teacher_vals:
         raise ValueError("grad_topk must be float32 [n_tokens, K] with unit column stride")
     stream = torch.cuda.current_stream(dev).cuda_stream
     ld_k = int(teacher_ids.stride(0)) if n else k
-    rc = lib().turnkl_fwd_bwd_topk(
+    rc = _on(
+        student.get_device(), lib().turnkl_fwd_bwd_topk,
         _ptr(student), _row_stride(student) if n else v, dt, n, v, _ptr(teacher_ids),
         _ptr(teacher_vals), ld_k, k, _ptr(turn_id), _ptr(traj_id), _ptr(loss_mask), float(alpha),
         float(grad_scale), _ptr(loss), _ptr(grad_t),
@@ -731,7 +747,8 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
         top_logp = top_logp.data_ptr()
     if workspace is None:
         workspace = LogprobsWorkspace(n, v, k, device=logits.device)
-    rc = lib().turnkl_token_logprobs(
+    rc = _on(
+        index, lib().turnkl_token_logprobs,
         *_matrix(logits, n, v), dt, n, v, ids_at, mask_at, k, _vector(out.logp, n, "logp", index),
         _vector(out.entropy, n, "entropy", index), _vector(out.log_z, 2 * n, "log_z", index), top_ids,
         top_logp, ld_top, *_scratch(workspace, index), _stream(index))
@@ -764,7 +781,8 @@ def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log
         grad = torch.empty_like(logits) if grad == "new" else logits
     else:
         _like(grad, dt, index, shape, "grad")
-    rc = lib().turnkl_token_logprobs_bwd(
+    rc = _on(
+        index, lib().turnkl_token_logprobs_bwd,
         *_matrix(logits, n, v), dt, n, v, _per_row(token_ids, n, "token_ids", index, torch.int32),
         _per_row(mask, n, "mask", index, torch.uint8), _vector(log_z, 2 * n, "log_z", index),
         _vector(entropy, n, "entropy", index), _vector(grad_logp, n, "grad_logp", index),
@@ -819,7 +837,8 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None,
         _like(y, dt, index, shape, "y")
     if isinstance(stats, bool):
         stats = torch.empty((n, 2), dtype=torch.float32, device=x.device) if stats else None
-    rc = lib().turnkl_norm_fwd(
+    rc = _on(
+        index, lib().turnkl_norm_fwd,
         *_matrix(x, n, d), dt, n, d, w_at, b_at, pt, NORM_RMS if rms else NORM_LAYER, eps,
         *_matrix(y, n, d), _vector(stats, 2 * n, "stats", index), _stream(index))
     if rc != OK:
@@ -863,7 +882,8 @@ def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
         if workspace is None:
             workspace = NormWorkspace(n, d, device=x.device)
         ws_at, ws_bytes = _scratch(workspace, index)
-    rc = lib().turnkl_norm_bwd(
+    rc = _on(
+        index, lib().turnkl_norm_bwd,
         *_matrix(grad_y, n, d), *_matrix(x, n, d), dt, n, d, w_at, pt, NORM_RMS if rms else NORM_LAYER,
         _vector(stats, 2 * n, "stats", index), gx_at, ld_gx, _vector(grad_weight, d, "grad_weight", index),
         _vector(grad_bias, d, "grad_bias", index), 1 if accumulate else 0, ws_at, ws_bytes, _stream(index))
