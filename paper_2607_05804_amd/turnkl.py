@@ -741,10 +741,10 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
                     (n and t.stride()[1] != 1):
                 raise ValueError(f"{name} must be {dtype} [n_tokens, k] on cuda:{index} with unit "
                                  "column stride")
-        if top_ids.stride() != top_logp.stride():
-            raise ValueError("top_ids and top_logp must share a row stride")
         top_ids, ld_top = _matrix(top_ids, n, k)
-        top_logp = top_logp.data_ptr()
+        top_logp, ld = _matrix(top_logp, n, k)
+        if n > 1 and ld != ld_top:
+            raise ValueError("top_ids and top_logp must share a row stride")
     if workspace is None:
         workspace = LogprobsWorkspace(n, v, k, device=logits.device)
     rc = _on(

@@ -57,3 +57,13 @@ def test_strides_of_alternatives(n, k, ld, library):
     ids, logp = (torch.empty((n, ld), dtype=d)[:, :k] for d in (torch.int32, torch.float32))
     call(alternatives(n, k, ids, logp), n, k)
     assert library.n == n and library.ld_top >= k and (n < 2 or library.ld_top == ld)
+
+
+def test_a_single_row_of_alternatives_has_no_stride_to_share(library):
+    """One row may lie in two buffers of their own widths; rows at two strides may not."""
+    ids, logp = torch.empty((1, 9), dtype=torch.int32)[:, :3], torch.empty((1, 3))
+    call(alternatives(1, 3, ids, logp), 1, 3)
+    assert library.ld_top >= 3
+    ids, logp = torch.empty((2, 9), dtype=torch.int32)[:, :3], torch.empty((2, 3))
+    with pytest.raises(ValueError, match="share a row stride"):
+        call(alternatives(2, 3, ids, logp), 2, 3)
