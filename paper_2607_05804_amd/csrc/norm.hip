@@ -515,12 +515,13 @@ hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s) {
 
 hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s) {
   const bool sums = p.gw || p.gb;
-  if (sums && !p.bf16 && (p.width + 3) / 4 > kSumPacks) {  // before the rows: they may be in place
+  const bool columns = !p.bf16 && (p.width + 3) / 4 > kSumPacks;  // whose rows leave no sums
+  if (sums && columns) {  // before the rows: they may be in place
     const dim3 grid((p.width + kColumnThreads - 1) / kColumnThreads, p.n_groups);
     norm_bwd_columns<<<grid, kColumnThreads, 0, s>>>(p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  launch_norm<true>(p, s);
+  if (p.out || !columns) launch_norm<true>(p, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (!sums) return hipSuccess;
   norm_bwd_join<<<dim3((p.width + kWave - 1) / kWave, p.gb ? 2 : 1), kJoinThreads, 0, s>>>(p);
