@@ -321,14 +321,24 @@ def _rows_aligned(*tensors) -> bool:
     return True
 
 
-def _on(index: int, call, *args) -> int:
-    """call(*args) with a device current: the address of the default stream is the same
-    on every device, and work on it goes to the current one.  (Asked for directly, which
-    takes 0.1 us: entering a device that is current already takes 0.5.)"""
-    if torch._C._cuda_getDevice() == index:
-        return call(*args)
-    with torch.cuda.device(index):
-        return call(*args)
+# The current device, and the address of a device's current stream, without the objects
+# that torch builds around them: a Stream takes 1.8 us, a fifth of a small call, entering a
+# device that is current already 0.5 us.
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _on(index: int, call):
+    """`call` with a device current: the address of the default stream is the same on
+    every device, and work on it goes to the current one."""
+    if _current_device() == index:
+        return call
+
+    def there(*args):
+        with torch.cuda.device(index):
+            return call(*args)
+
+    return there
 
 
 class _Scratch:
@@ -349,7 +359,7 @@ class _StatusScratch(_Scratch):
         """The status that the last call left, read on the current stream of the workspace's
         device, where that call went."""
         index = self.tensor.get_device()
-        return int(_on(index, lib().turnkl_get_status, self.tensor.data_ptr(), _stream(index)))
+        return int(_on(index, lib().turnkl_get_status)(self.tensor.data_ptr(), _stream(index)))
 
 
 class Workspace(_StatusScratch):
@@ -371,8 +381,8 @@ class Workspace(_StatusScratch):
                 for _ in range(5)]
         n_seg = ctypes.c_int32(0)
         index = self.tensor.get_device()
-        rc = _on(index, lib().turnkl_get_segments, self.tensor.data_ptr(), n, _stream(index),
-                 ctypes.byref(n_seg), *[_ptr(b) for b in bufs])
+        rc = _on(index, lib().turnkl_get_segments)(self.tensor.data_ptr(), n, _stream(index),
+                                                   ctypes.byref(n_seg), *[_ptr(b) for b in bufs])
         if rc != OK:
             raise TurnKLError(rc, "turnkl_get_segments")
         k = n_seg.value
@@ -454,8 +464,7 @@ def fwd_bwd(student: torch.Tensor, teacher: torch.Tensor, turn_id: torch.Tensor,
     stream = torch.cuda.current_stream(dev).cuda_stream
     opts = _options(n, support_floor, support_frac, success, outcome_stats, token_weights,
                     token_lse, dev)
-    rc = _on(
-        student.get_device(), lib().turnkl_fwd_bwd,
+    rc = _on(student.get_device(), lib().turnkl_fwd_bwd)(
         *_fused_args(student, teacher, dt, n, v, turn_id, traj_id, loss_mask, alpha, grad_scale,
                      loss, grad_t, turn_stats, max_turns, accumulate_stats, kl_t, opts),
         _ptr(workspace.tensor), workspace.nbytes, ctypes.c_void_p(stream))
@@ -501,8 +510,7 @@ def fwd_bwd_noalloc(student: torch.Tensor, teacher: torch.Tensor, turn_id: torch
     stream = torch.cuda.current_stream(dev).cuda_stream
     opts = _options(n, support_floor, support_frac, success, outcome_stats, token_weights,
                     token_lse, dev)
-    rc = _on(
-        student.get_device(), lib().turnkl_fwd_bwd_noalloc,
+    rc = _on(student.get_device(), lib().turnkl_fwd_bwd_noalloc)(
         *_fused_args(student, teacher, dt, n, v, turn_id, traj_id, loss_mask, alpha, grad_scale,
                      loss, grad_t, turn_stats, max_turns, accumulate_stats, token_kl, opts),
         _ptr(status), ctypes.c_void_p(stream))
@@ -584,8 +592,7 @@ def fwd_bwd_topk(student: torch.Tensor, teacher_ids: torch.Tensor, teacher_vals:
         raise ValueError("grad_topk must be float32 [n_tokens, K] with unit column stride")
     stream = torch.cuda.current_stream(dev).cuda_stream
     ld_k = int(teacher_ids.stride(0)) if n else k
-    rc = _on(
-        student.get_device(), lib().turnkl_fwd_bwd_topk,
+    rc = _on(student.get_device(), lib().turnkl_fwd_bwd_topk)(
         _ptr(student), _row_stride(student) if n else v, dt, n, v, _ptr(teacher_ids),
         _ptr(teacher_vals), ld_k, k, _ptr(turn_id), _ptr(traj_id), _ptr(loss_mask), float(alpha),
         float(grad_scale), _ptr(loss), _ptr(grad_t),
@@ -617,12 +624,6 @@ def _gpu(t: torch.Tensor) -> int:
     if index < 0:
         raise ValueError(f"tensors must be on the GPU, not {t.device}")
     return index
-
-
-def _stream(index: int) -> int:
-    """Address of a device's current HIP stream.  (The raw getter: building a torch
-    Stream object takes 1.8 us, a fifth of a small call.)"""
-    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _matrix(t: torch.Tensor, n: int, cols: int):
@@ -747,8 +748,7 @@ def token_logprobs(logits: torch.Tensor, token_ids: torch.Tensor | None = None, 
             raise ValueError("top_ids and top_logp must share a row stride")
     if workspace is None:
         workspace = LogprobsWorkspace(n, v, k, device=logits.device)
-    rc = _on(
-        index, lib().turnkl_token_logprobs,
+    rc = _on(index, lib().turnkl_token_logprobs)(
         *_matrix(logits, n, v), dt, n, v, ids_at, mask_at, k, _vector(out.logp, n, "logp", index),
         _vector(out.entropy, n, "entropy", index), _vector(out.log_z, 2 * n, "log_z", index), top_ids,
         top_logp, ld_top, *_scratch(workspace, index), _stream(index))
@@ -781,8 +781,7 @@ def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log
         grad = torch.empty_like(logits) if grad == "new" else logits
     else:
         _like(grad, dt, index, shape, "grad")
-    rc = _on(
-        index, lib().turnkl_token_logprobs_bwd,
+    rc = _on(index, lib().turnkl_token_logprobs_bwd)(
         *_matrix(logits, n, v), dt, n, v, _per_row(token_ids, n, "token_ids", index, torch.int32),
         _per_row(mask, n, "mask", index, torch.uint8), _vector(log_z, 2 * n, "log_z", index),
         _vector(entropy, n, "entropy", index), _vector(grad_logp, n, "grad_logp", index),
@@ -837,8 +836,7 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None,
         _like(y, dt, index, shape, "y")
     if isinstance(stats, bool):
         stats = torch.empty((n, 2), dtype=torch.float32, device=x.device) if stats else None
-    rc = _on(
-        index, lib().turnkl_norm_fwd,
+    rc = _on(index, lib().turnkl_norm_fwd)(
         *_matrix(x, n, d), dt, n, d, w_at, b_at, pt, NORM_RMS if rms else NORM_LAYER, eps,
         *_matrix(y, n, d), _vector(stats, 2 * n, "stats", index), _stream(index))
     if rc != OK:
@@ -882,8 +880,7 @@ def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
         if workspace is None:
             workspace = NormWorkspace(n, d, device=x.device)
         ws_at, ws_bytes = _scratch(workspace, index)
-    rc = _on(
-        index, lib().turnkl_norm_bwd,
+    rc = _on(index, lib().turnkl_norm_bwd)(
         *_matrix(grad_y, n, d), *_matrix(x, n, d), dt, n, d, w_at, pt, NORM_RMS if rms else NORM_LAYER,
         _vector(stats, 2 * n, "stats", index), gx_at, ld_gx, _vector(grad_weight, d, "grad_weight", index),
         _vector(grad_bias, d, "grad_bias", index), 1 if accumulate else 0, ws_at, ws_bytes, _stream(index))

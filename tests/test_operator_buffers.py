@@ -25,7 +25,7 @@ def library(monkeypatch):
     monkeypatch.setattr(T, "lib", lambda: stub)
     monkeypatch.setattr(T, "_gpu", lambda t: t.get_device())
     monkeypatch.setattr(T, "_stream", lambda index: 0)
-    monkeypatch.setattr(T, "_on", lambda index, call, *args: call(*args))
+    monkeypatch.setattr(T, "_on", lambda index, call: call)
     monkeypatch.setattr(T, "status_string", lambda code: real.turnkl_status_string(code).decode())
     return stub
 

@@ -50,8 +50,8 @@ def library(monkeypatch):
     stub = Recorder(current)
     monkeypatch.setattr(T, "lib", lambda: stub)
     monkeypatch.setattr(T, "_gpu", lambda t: t.get_device())
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0])
-    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: STREAMS[index])
+    monkeypatch.setattr(T, "_current_device", lambda: current[0])
+    monkeypatch.setattr(T, "_stream", lambda index: STREAMS[index])
     monkeypatch.setattr(torch.cuda, "device", Device)
     monkeypatch.setattr(torch.cuda, "current_stream", Stream)
     monkeypatch.setattr(T.ctypes, "c_void_p", lambda x: x)
