@@ -240,10 +240,11 @@ __global__ __launch_bounds__(kBeginThreads) void logprob_begin(LogprobParams p) 
 // that fill the card.  Bound: HBM; the arithmetic (a fused multiply-add, an exponential,
 // two sums and half a maximum an element) keeps the vector units busy for three quarters
 // of that time, so nothing may be added to it, and what a row's end takes is hidden by
-// the other workgroups' loads only in part.  9,830 bf16 rows of 151,936: 468 us without
-// alternatives (6.4 TB/s), 492 with 5, 528 with 50; 3,000 fp32 rows of 50,257 94 us
-// (6.4 TB/s).  Two groups ahead instead of one, in four workgroups a CU instead of five,
-// gave 527; as few workgroups as take no more turns 539.
+// the other workgroups' loads only in part.  9,830 bf16 rows of 151,936 out of 16,384:
+// 463 us without alternatives (6.5 TB/s), 492 with 5, 523 to 529 with 50 (side by side 444,
+// 462 and 490); 3,000 fp32 rows of 50,257 94 us (6.4 TB/s), 104 with 20; 4,900 of 151,936
+// 441 (6.8 TB/s), 480 with 50.  Two groups ahead instead of one, in four workgroups a CU
+// instead of five, or as few workgroups as take no more turns gave nothing or 2% less.
 // Workgroups of a variant that a CU has registers for.  (The one of bf16 rows on packs
 // with alternatives has five without being held to it; held to it, it spills.)
 __host__ __device__ constexpr int rows_a_cu(bool bf16, bool ragged, bool top) {
@@ -714,7 +715,6 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
       const unsigned long long least = s_floor;
 #pragma unroll
       for (int q = 0; q < kJoinEach; ++q) add(got[q], least);
-#pragma unroll 4
       for (int base = kJoinEach * kLpThreads; base < total; base += kLpThreads)
         add(base + tid < total ? in[base + tid] : 0ull, least);
       __syncthreads();
@@ -738,10 +738,11 @@ __global__ __launch_bounds__(kLpThreads) void logprob_join(LogprobParams p) {
 
 // Short rows: a wave each, the row in registers (kPacks packs a lane), four rows a
 // workgroup and no barriers.  Bound: the arithmetic and, with alternatives, the chain of
-// steps that finds them (20,000 bf16 rows of 8,192, no alternatives: 65 to 71 us, 4.6 to
-// 5.0 TB/s; of 4,000 with 20: 50 us; 65,536 of 1,000 with 50: 116 us).  The bound of the alternatives is the k-th largest of the
-// packs' maxima; where more elements reach it than the list holds, the k-th largest
-// element and, among its equals, the largest id that counts are found bit by bit.
+// steps that finds them (20,000 bf16 rows of 8,192: 60 us, 5.5 TB/s, with 20 alternatives
+// 89; of 4,000 32 and 50 us; 65,536 of 1,000 37 us, with 50 alternatives 118).  The bound of
+// the alternatives is the k-th largest of the packs' maxima; where more elements reach it
+// than the list holds, the k-th largest element and, among its equals, the largest id that
+// counts are found bit by bit (20,000 rows of 4,000 with ten allowed tokens, k = 20: 1.2 ms).
 constexpr int kShortPacks = 16;   // of a lane, at most
 constexpr int kShortCand = 256;   // elements held for ranking
 constexpr int kShortList = 256;   // packs held for a second look
@@ -947,11 +948,14 @@ constexpr int kJoinGrid = 1 << 20;  // workgroups; beyond, each takes several ro
 
 }  // namespace
 
-// Chunks of a row: as many as its units' LDS asks for, and for few rows so many
-// that they fill the card, of 4,096 elements at least (a depth that depends on sizes
-// only, so that the workspace can be sized for it; with 1,280 tasks 173 fp32 rows of
-// 45,230, k = 3, took 25.5 us instead of 20.6, 64 bf16 rows of 151,936, k = 128, 29.1
-// instead of 25.9, but k = 0 11.3 instead of 12.2).
+// Chunks of a row: as many as its units' LDS asks for, and for few rows so many that
+// they fill the card, of 4,096 elements at least (a depth that depends on sizes only, so
+// that the workspace can be sized for it; with 1,280 tasks 173 fp32 rows of 45,230, k = 3,
+// took 25 us instead of 20, 64 bf16 rows of 151,936, k = 128, 29 instead of 25, but k = 0
+// a microsecond less).  From 385 rows on a row is one chunk: bf16 rows of 151,936
+// without alternatives take, whole, in two chunks and in three, 200 of them 19.1, 16.6 and
+// 17.4 us, 300 22.6, 22.5 and 22.2, 384 23.9, 24.8 and 27.0, 512 28.7, 31.2 and 30.3, 1,280
+// 62.4, 65.6 and 66.2; with 20 alternatives whole rows win from 256 on (23.7, 24.4, 24.7).
 static int chunks_by_size(long long vocab) {
   // ragged rows hold up to 64 elements more, and boundaries move by eight packs
   return (int)((vocab + 192 + kMaxChunkElems - 1) / kMaxChunkElems);

@@ -6,8 +6,8 @@
 // from row to row and keeps its columns' weights (and, backward, the columns' sums
 // over its rows) in registers; the next row is on its way while one is reduced.
 // Backward a second kernel adds the workgroups' sums in their order.  Bound: HBM; small
-// batches by latency.  65,536 bf16 rows of 4,096: 191 us forward (5.6 TB/s), 275
-// backward (5.85 TB/s), where a copy of 2 GiB reaches 5.2; 64 rows of 2,048 forward 4 us.
+// batches by latency.  65,536 bf16 rows of 4,096: 192 us forward (5.6 TB/s), 278
+// backward (5.8 TB/s), where a copy of 2 GiB reaches 5.2; 64 rows of 2,048 forward 3 us.
 
 #include "row_span.h"
 
@@ -413,24 +413,32 @@ struct NormShape {
   int groups;     // workgroups that fill the card
 };
 
-// Rows of up to 128 packs (backward 256) take one wave, which needs no barrier:
-// backward, 12,000 bf16 rows of 2,048 (root mean square) take 32 us with four packs a
-// lane and four rows a workgroup, 34 to 38 with two waves to a row, and 65,536 of 1,500
-// 149 against 163 to 183 (112 with the three packs that such a row fills; of 2,048 149
-// against 141 to 155); with one pack, eight rows a workgroup: 65,536 of 512 took 45 us,
-// with four rows 48, with two 54.  Wider rows take two packs a thread while 512 threads
-// suffice (65,536 of 4,096 backward, layer form: 275 us, with four packs 327, with one
-// 312), then four, and eight for fp32 rows past 8,192.
+// Rows of up to 128 packs (backward 256) take one wave, which needs no barrier: backward,
+// 12,000 bf16 rows of 2,048 (root mean square) take 33 us with four packs a lane and four
+// rows a workgroup, 35 to 42 with two waves to a row (65,536 of them, layer form, 150
+// against 145 to 162); 65,536 of 1,500, with the three packs that such a row fills, 122, with
+// four 148, with two waves to a row 146.  Up to two packs a lane backward eight rows a
+// workgroup: 65,536 of 512 take 40 us, with four rows 45, with two 70.  Wider rows take two
+// packs a thread while 512 threads suffice (65,536 of 4,096 backward, layer form: 278 us,
+// with four packs 329, with one 309), then four, and eight for fp32 rows past 8,192, whose
+// column sums are a kernel of their own: it reads both matrices again (8,000 rows of 16,384
+// 527 us, of 8,192 142).
 // The workgroups go from row to row, so they are no more than the registers let the
 // card hold at once, and backward fewer: what reads two streams and writes a third
 // slows down with more of them in flight, and each leaves partial sums.  Forward 16
-// waves a CU up to two packs (65,536 of 4,096: 192 us, with 8 waves 250, with 24 214).
-// Backward by measurement, workgroups a CU for 65,536 bf16 rows: with a row to a
-// workgroup and two packs a thread two (of 4,096: 279 us, with three 307, with four 338;
-// of 3,800 284, 316, 325), of shorter rows three (of 3,500: 306, with two 366) or four (of
-// 2,500: 232, with two 338); with a wave per row two (of 512: 40, with one 44; of 1,500:
-// 122, with one 177, with three 153), but one where eight rows of more than 85 packs lie
-// side by side (of 1,000: 73, with two 82; of 600 two again: 55, with one 65).
+// waves a CU up to two packs (65,536 of 4,096: with 8 waves 231 us, with 24 213).
+// Backward by measurement, us by workgroups a CU (1 / 2 / 3 / 4).
+// A row to a workgroup and two packs a thread: two for eight waves of packs and more, fewer
+// waves 24 in all.  65,536 bf16 rows of 4,096: 367 / 278 / 321 / 335, of 3,800: - / 280 / 314
+// / 320; of 3,500 (seven waves): - / 364 / 304 / 305; of 2,500 (five): - / 339 / 268 / 228.
+// 92 million fp32 elements in rows of 2,048: - / 188 / 201 / 215, of 1,537 (seven): - / 239 /
+// 202 / 230, of 1,028 (five): - / 216 / 229 / 212; of whole packs two would do as well or
+// better (of 1,792: - / 202 / 199 / 215, of 1,280: - / 186 / 199 / 193, of 1,536: - / 179 /
+// 183 / 203).
+// A wave to a row: two (65,536 of 512: 43 / 40 / 42; of 1,500: 176 / 122 / 153), but one where
+// eight rows of more than 85 packs lie side by side, which is where the two cross: bf16 rows
+// of 600: 62 / 54, of 680 (85 packs): 61.4 / 60.1, of 720: 62.7 / 63.2, of 1,000: 73 / 83;
+// fp32 rows of 300: 51.2 / 50.6, of 340 (85): 56.5 / 56.8, of 400: 60.9 / 62.8.
 // With a row to a workgroup and more packs a thread 8 waves.
 NormShape norm_shape(long long width, int epv, bool bwd) {
   const int packs = (int)((width + epv - 1) / epv);
