@@ -473,7 +473,8 @@ typedef enum {
  * x              [n_rows x width] of `dtype`, row stride ld_x (elements, >= width),
  *                rows of any start.
  * weight, bias   [width] of param_dtype, or NULL (ones, zeros).
- * eps            finite, >= 0.
+ * eps            >= 0 and at most the largest float; used as a float, as the smallest
+ *                one where it is less and not 0.
  * y              [n_rows x width] of `dtype`, row stride ld_y; may equal x with
  *                ld_y == ld_x (in place).
  * stats_out      [n_rows x 2] float (mu, r), or NULL.

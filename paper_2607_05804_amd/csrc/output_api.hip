@@ -3,6 +3,7 @@
 // workspace carve-up and launches, all on the caller's stream with no host
 // synchronisation.
 
+#include <float.h>
 #include <math.h>
 
 #include "turnkl_internal.h"
@@ -178,7 +179,7 @@ int turnkl_norm_fwd(const void* x, int64_t ld_x, int dtype, int64_t n_rows, int6
                     const void* weight, const void* bias, int param_dtype, int kind, double eps,
                     void* y, int64_t ld_y, float* stats_out, hipStream_t stream) {
   if (!norm_sizes_ok(dtype, param_dtype, kind, n_rows, width)) return TURNKL_ERR_INVALID_ARG;
-  if (!(eps >= 0.0) || !isfinite(eps)) return TURNKL_ERR_INVALID_ARG;
+  if (!(eps >= 0.0) || eps > FLT_MAX) return TURNKL_ERR_INVALID_ARG;
   if (n_rows == 0) return TURNKL_OK;
   const size_t es = elem_size(dtype), ps = elem_size(param_dtype), w = (size_t)width;
   if (!rows_ok(x, ld_x, width, es) || !rows_ok(y, ld_y, width, es)) return TURNKL_ERR_INVALID_ARG;
@@ -199,7 +200,8 @@ int turnkl_norm_fwd(const void* x, int64_t ld_x, int dtype, int64_t n_rows, int6
   p.ld_out = ld_y;
   p.n_rows = (int)n_rows;
   p.width = (int)width;
-  p.eps = (float)eps;
+  // (rows without variance have an r for every eps but 0)
+  p.eps = eps > 0.0 && (float)eps == 0.0f ? FLT_TRUE_MIN : (float)eps;
   p.bf16 = dtype == TURNKL_BF16;
   p.param_bf16 = param_dtype == TURNKL_BF16;
   p.rms = kind == TURNKL_NORM_RMS;
