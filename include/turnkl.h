@@ -508,6 +508,54 @@ int turnkl_norm_bwd(const void* grad_y, int64_t ld_gy, const void* x, int64_t ld
                     hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Rows of an embedding table for tokens, and the table's gradient:
+ *   y_i  = s E[t_i],      dE[v] (+)= s sum over the tokens i with t_i = v of g_i.
+ * Products and sums are float; y and dE are rounded to nearest even once.
+ * ------------------------------------------------------------------------ */
+
+/* The widest table row, in elements. */
+#define TURNKL_MAX_EMBED_WIDTH 65536
+
+/*
+ * table          [vocab x width] of table_dtype, row stride ld_table (elements, >=
+ *                width), rows of any start; vocab is at most 2^24.
+ * token_ids      [n_tokens] t.  The row of an id outside [0, vocab) is NaN.
+ * mask           [n_tokens] nonzero: the token is asked for; NULL: every token is.
+ *                Rows of others are zeros, and their ids are not looked at.
+ * scale          s, finite, used as a float.
+ * out            [n_tokens x width] of out_dtype, row stride ld_out; may not overlap
+ *                an input.
+ * No workspace, no device-detected errors.
+ */
+int turnkl_embed_fwd(const void* table, int64_t ld_table, int table_dtype, int64_t vocab,
+                     int64_t width, const int32_t* token_ids, const uint8_t* mask,
+                     int64_t n_tokens, double scale, void* out, int64_t ld_out, int out_dtype,
+                     hipStream_t stream);
+
+/* Bytes of device workspace for turnkl_embed_bwd (host; a pure function of its
+ * arguments, which does not fall as one of them grows), 0 for invalid ones.  No
+ * initialisation; 256-byte aligned. */
+size_t turnkl_embed_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width);
+
+/*
+ * grad_out       [n_tokens x width] of grad_dtype, the gradient g of y, row stride
+ *                ld_grad.
+ * token_ids, mask, vocab, scale   those of turnkl_embed_fwd.  A token that is not asked
+ *                for, or whose id is outside [0, vocab), adds nothing; such an id is
+ *                recorded as TURNKL_ERR_TOKEN_ID (turnkl_get_status).
+ * grad_table     [vocab x width] of table_dtype, row stride ld_table.  accumulate == 0
+ *                overwrites all of it (rows that no token has with zeros); otherwise
+ *                the rows that occur are added to, once each, and the others are not
+ *                touched.  Elements between width and ld_table are never written.
+ * A row's gradients are summed in the order of its tokens in a tree that depends on the
+ * ids alone: the same bits from call to call.
+ */
+int turnkl_embed_bwd(const void* grad_out, int64_t ld_grad, int grad_dtype, int64_t n_tokens,
+                     int64_t width, const int32_t* token_ids, const uint8_t* mask, int64_t vocab,
+                     double scale, void* grad_table, int64_t ld_table, int table_dtype,
+                     int accumulate, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Adaptive rollout-depth controller (Sec. 5.1; App. D, Algorithm 1 and the
  * full-configuration table).  HOST functions: all pointers are host memory,
  * nothing touches the GPU.  They consume the per-turn statistics that

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["turnkl_api.hip", "segment.hip", "rowkl.hip", "rowkl_ragged.hip", "rowkl_whole.hip",
            "rowfwd.hip", "reduce.hip", "topk.hip", "logprobs.hip",
-           "logprobs_bwd.hip", "norm.hip", "output_api.hip", "controller.cpp", "diagnostics.cpp"]
+           "logprobs_bwd.hip", "norm.hip", "output_api.hip", "embed.hip", "boundary_api.hip", "controller.cpp", "diagnostics.cpp"]
 LIB = os.path.join(HERE, "libturnkl.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -6,7 +6,7 @@
 #include <float.h>
 #include <math.h>
 
-#include "turnkl_internal.h"
+#include "api_checks.h"
 
 namespace turnkl {
 namespace {
@@ -33,36 +33,11 @@ LogprobLayout logprob_layout(int64_t n_tokens, int64_t vocab, int32_t k) {
   return L;
 }
 
-bool misaligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
-
-// Whether any of the outputs overlaps an input or another output.
-bool any_overlap(std::initializer_list<Region> in, std::initializer_list<Region> out) {
-  for (const Region* a = out.begin(); a != out.end(); ++a) {
-    if (!a->p || !a->n) continue;
-    if (overlaps_any(a->p, a->n, in)) return true;
-    for (const Region* b = a + 1; b != out.end(); ++b)
-      if (b->p && b->n && overlaps(a->p, a->n, b->p, b->n)) return true;
-  }
-  return false;
-}
-
-bool known_dtype(int dtype) { return dtype == TURNKL_BF16 || dtype == TURNKL_F32; }
-size_t elem_size(int dtype) { return dtype == TURNKL_BF16 ? 2 : 4; }
-
 // The arguments that both directions of the normalisation share.
 bool norm_sizes_ok(int dtype, int param_dtype, int kind, int64_t n_rows, int64_t width) {
   return known_dtype(dtype) && known_dtype(param_dtype) &&
          (kind == TURNKL_NORM_LAYER || kind == TURNKL_NORM_RMS) && n_rows >= 0 &&
          n_rows <= 0x7FFFFFFFll && width >= 1 && width <= TURNKL_MAX_NORM_WIDTH;
-}
-
-bool rows_ok(const void* p, int64_t ld, int64_t width, size_t es) {
-  return p && ld >= width && ld <= 0x7FFFFFFFll && !misaligned(p, es);
-}
-
-// Whether every row of the matrix is whole 16-byte packs.
-bool whole_packs(const void* p, int64_t ld, int64_t n_rows, int64_t width, size_t es) {
-  return !misaligned(p, 16) && (width * es) % 16 == 0 && (n_rows <= 1 || (ld * es) % 16 == 0);
 }
 
 }  // namespace

@@ -458,6 +458,81 @@ int norm_groups(long long n_rows, long long width, bool bf16);
 hipError_t launch_norm_fwd(const NormParams& p, hipStream_t s);
 hipError_t launch_norm_bwd(const NormParams& p, hipStream_t s);
 
+// Rows of an embedding table for tokens, and its gradient (embed.hip).
+struct EmbedParams {
+  const void* table;
+  const int* ids;
+  const unsigned char* mask;  // or null: every token
+  void* out;
+  long long ld_table;
+  long long ld_out;
+  long long n_blocks;  // set at launch, like the next two
+  int lanes;           // of a row, a power of two
+  int parts;           // that a row is cut into
+  int n_rows;
+  int vocab;
+  int width;
+  float scale;
+  int table_bf16;
+  int out_bf16;
+};
+
+constexpr int kEmbedSmallSort = 4096;  // tokens that one workgroup sorts
+constexpr int kEmbedDigitBits = 9;     // of a turn of the sort of more
+constexpr int kEmbedTileCols = 512;    // columns that a wave sums
+constexpr int kEmbedWaves = 4096;      // that sum at once, at least where there is work for them
+constexpr int kEmbedFillRows = 1024;   // table rows that a workgroup looks after, at most
+
+struct EmbedShape {
+  int run;           // sorted tokens that a wave sums
+  int col_tiles;     // of kEmbedTileCols columns
+  int key_bits;
+  long long n_runs;
+  long long part_ld;  // floats of a piece of a table row
+  long long room;     // floats of all pieces
+  long long tile;     // tokens of a workgroup of the sort
+  long long n_tiles;
+};
+
+struct EmbedGradParams {
+  const void* grad;
+  const int* ids;
+  const unsigned char* mask;  // or null: every token
+  void* table;                // the table's gradient
+  Header* hdr;
+  int* key[2];   // [n_rows] each, of the sort: ids and their tokens
+  int* tok[2];
+  const int* key_in;  // set at launch: those in the order so far, in the end sorted
+  const int* tok_in;
+  int* key_out;
+  int* tok_out;
+  int* count;    // [n_tiles][2^kEmbedDigitBits]
+  float* part;   // [n_runs][2][part_ld]
+  long long ld_grad;
+  long long ld_table;
+  long long part_ld;
+  long long tile;
+  int n_rows;
+  int vocab;
+  int width;
+  int run;
+  int n_runs;
+  int col_tiles;
+  int n_tiles;
+  int key_bits;
+  int turn;        // set at launch, like the next two
+  int sum_blocks;  // workgroups that sum, before those that zero
+  int fill_rows;   // table rows of one of those
+  float scale;
+  int grad_bf16;
+  int table_bf16;
+  int accumulate;
+};
+
+EmbedShape embed_shape(long long n, long long vocab, long long width);
+hipError_t launch_embed(const EmbedParams& p, hipStream_t s);
+hipError_t launch_embed_bwd(const EmbedGradParams& p, hipStream_t s);
+
 // status_out: optional device int32 that receives the call's status
 // (TURNKL_OK or the device-detected error) once the loss is written.
 hipError_t launch_reduce(const SegParams& p, const Ws& ws, const float* kl, double alpha,

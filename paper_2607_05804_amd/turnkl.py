@@ -52,7 +52,8 @@ EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
            "turnkl_depth_update", "turnkl_loss_share", "turnkl_budget_report",
            "turnkl_outcome_gap", "turnkl_token_logprobs_workspace_bytes",
            "turnkl_token_logprobs", "turnkl_token_logprobs_bwd", "turnkl_norm_fwd",
-           "turnkl_norm_workspace_bytes", "turnkl_norm_bwd")
+           "turnkl_norm_workspace_bytes", "turnkl_norm_bwd", "turnkl_embed_fwd",
+           "turnkl_embed_workspace_bytes", "turnkl_embed_bwd")
 # ... and every entry point include/turnkl_testing.h declares (measurement and
 # test hooks).
 TESTING_EXPORTS = ("turnkl_profile_row_kernel", "turnkl_set_row_tiling",
@@ -194,6 +195,16 @@ def lib() -> ctypes.CDLL:
             c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p,
             c.c_int, c.c_int, c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p, c.c_int,
             c.c_void_p, c.c_size_t, c.c_void_p]
+        l.turnkl_embed_fwd.restype = c.c_int
+        l.turnkl_embed_fwd.argtypes = [
+            c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int64,
+            c.c_double, c.c_void_p, c.c_int64, c.c_int, c.c_void_p]
+        l.turnkl_embed_workspace_bytes.restype = c.c_size_t
+        l.turnkl_embed_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int64]
+        l.turnkl_embed_bwd.restype = c.c_int
+        l.turnkl_embed_bwd.argtypes = [
+            c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int64,
+            c.c_double, c.c_void_p, c.c_int64, c.c_int, c.c_int, c.c_void_p, c.c_size_t, c.c_void_p]
         _lib = l
     return _lib
 
@@ -887,6 +898,71 @@ def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
     if rc != OK:
         raise TurnKLError(rc, "turnkl_norm_bwd")
     return grad_x, grad_weight, grad_bias
+
+
+def embed_fwd(table: torch.Tensor, token_ids: torch.Tensor, *, scale: float = 1.0,
+              mask: torch.Tensor | None = None, out: torch.Tensor | None = None,
+              dtype: torch.dtype | None = None) -> torch.Tensor:
+    """turnkl_embed_fwd on the current stream: scale times the table's row of every token.
+
+    table: [V, D] bf16 or float32 of any row stride; token_ids: int32 [N]; mask: uint8
+    [N] or None (tokens with 0 get a row of zeros); out: a [N, D] tensor to write, or
+    None for a new one of `dtype` (the table's).  The row of an id outside [0, V) is
+    NaN.  Returns out.
+    """
+    tt, (v, d), index = _check_rows(table, "table")
+    n = token_ids.numel()
+    if out is None:
+        out = torch.empty((n, d), dtype=dtype or table.dtype, device=table.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out is {out.dtype}, not {dtype}")
+    ot = _dtype_code(out)
+    _like(out, ot, index, (n, d), "out")
+    rc = _on(index, lib().turnkl_embed_fwd)(
+        *_matrix(table, v, d), tt, v, d, _per_row(token_ids, n, "token_ids", index, torch.int32),
+        _per_row(mask, n, "mask", index, torch.uint8), n, scale, *_matrix(out, n, d), ot, _stream(index))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_embed_fwd")
+    return out
+
+
+class EmbedWorkspace(_StatusScratch):
+    """Caller-owned device scratch for turnkl_embed_bwd of up to n_tokens tokens, vocab table
+    rows and width columns."""
+
+    def __init__(self, n_tokens: int, vocab: int, width: int, device="cuda"):
+        super().__init__(int(lib().turnkl_embed_workspace_bytes(n_tokens, vocab, width)),
+                         "turnkl_embed_workspace_bytes", device)
+
+
+def embed_bwd(grad: torch.Tensor, token_ids: torch.Tensor, grad_table: torch.Tensor, *,
+              scale: float = 1.0, mask: torch.Tensor | None = None, accumulate: bool = False,
+              workspace: EmbedWorkspace | None = None, check: bool = True) -> torch.Tensor:
+    """turnkl_embed_bwd on the current stream: the gradient of embed_fwd's table from that
+    of its rows.
+
+    grad: [N, D] bf16 or float32 of any row stride; token_ids, scale, mask: embed_fwd's;
+    grad_table: a [V, D] tensor of either type that receives the gradient of every table
+    row (accumulate: that the tokens' sums are added to); check: read the device status
+    once at the end and raise on an id outside [0, V).  Returns grad_table.
+    """
+    gt, (n, d), index = _check_rows(grad, "grad")
+    tt, (v, width), table_index = _check_rows(grad_table, "grad_table")
+    if table_index != index or width != d:
+        raise ValueError("grad_table must be on the rows' device and have their width")
+    if workspace is None:
+        workspace = EmbedWorkspace(n, v, d, device=grad.device)
+    rc = _on(index, lib().turnkl_embed_bwd)(
+        *_matrix(grad, n, d), gt, n, d, _per_row(token_ids, n, "token_ids", index, torch.int32),
+        _per_row(mask, n, "mask", index, torch.uint8), v, scale, *_matrix(grad_table, v, d), tt,
+        1 if accumulate else 0, *_scratch(workspace, index), _stream(index))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_embed_bwd")
+    if check:
+        st = workspace.status()
+        if st != OK:
+            raise TurnKLError(st, "turnkl_embed_bwd (device)")
+    return grad_table
 
 
 def new_turn_stats(max_turns: int, device="cuda") -> torch.Tensor:

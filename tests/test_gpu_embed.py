@@ -1,0 +1,328 @@
+"""turnkl_embed_fwd and turnkl_embed_bwd against their formulas in 64 bits.
+
+Tolerances (u = 2^-24).  Forward: one product rounded to float, 1 u relative, and bf16
+output half a step more, 2^-8.  Backward: a row's sum of m terms adds at most 64 in
+sequence in a run, then the runs' pieces in at most m / 256 + 4 further steps, so that
+|d| <= (64 + m / 256 + 8) u sum|terms|, at most 300 u for the sizes here; the scale, one
+product, and accumulating, one sum, add a unit each of their results: 2 u (|old| + |dE|).
+bf16 output adds 2^-8 of the result.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2607_05804_amd import turnkl as T
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def rows(n, d, dtype, seed, pad=0, start=0):
+    """[n, d] at a stride of d + pad, `start` elements into an allocation of NaN."""
+    buf = torch.full((start + n * (d + pad) + 8,), math.nan, dtype=DT[dtype], device="cuda")
+    x = buf[start:start + n * (d + pad)].view(n, d + pad)[:, :d]
+    x.copy_(torch.randn((n, d), generator=gen(seed), device="cuda"))
+    return x
+
+
+def tokens(n, v, seed, skew=2.0):
+    """Ids of which low ones are likelier (skew 1: all alike)."""
+    u = torch.rand(n, generator=gen(seed + 5), device="cuda", dtype=torch.float64)
+    return (u.pow(skew) * v).long().clamp_(0, v - 1).int()
+
+
+def check_fwd(table, ids, scale=1.0, mask=None, out=None, dtype=None):
+    y = T.embed_fwd(table, ids, scale=scale, mask=mask, out=out, dtype=dtype)
+    v = table.shape[0]
+    inside = (ids >= 0) & (ids < v)
+    ref = table[ids.long().clamp(0, v - 1)].double() * float(torch.tensor(scale, dtype=torch.float32))
+    ref = torch.where(inside[:, None], ref, math.nan)
+    if mask is not None:
+        ref = torch.where(mask[:, None] != 0, ref, 0.0)
+    nan = ref.isnan()
+    assert torch.equal(y.isnan(), nan)
+    tol = U if y.dtype == torch.float32 else 2.0 ** -8
+    assert bool(((y.double() - ref).abs() <= tol * ref.abs() + 1e-44)[~nan].all())
+    return y
+
+
+def check_bwd(g, ids, v, scale=1.0, mask=None, dtype="f32", accumulate=False, pad=0, check=True):
+    n, d = g.shape
+    table = rows(v, d, dtype, 99, pad=pad)
+    old = table.clone()
+    T.embed_bwd(g, ids, table, scale=scale, mask=mask, accumulate=accumulate, check=check)
+    take = (ids >= 0) & (ids < v)
+    if mask is not None:
+        take &= mask != 0
+    at = ids[take].long()
+    terms = g[take].double() * float(torch.tensor(scale, dtype=torch.float32))
+    ref = torch.zeros((v, d), dtype=torch.float64, device="cuda").index_add_(0, at, terms)
+    size = torch.zeros_like(ref).index_add_(0, at, terms.abs())
+    bound = 300 * U * size + 2 * U * ref.abs() + 1e-44
+    if accumulate:
+        touched = torch.zeros(v, dtype=torch.bool, device="cuda").index_fill_(0, at, True)
+        assert torch.equal(table[~touched], old[~touched])
+        ref = ref + old.double()
+        bound = bound + 2 * U * (old.double().abs() + ref.abs())
+    if dtype == "bf16":
+        bound = bound + 2.0 ** -8 * ref.abs()
+    err = (table.double() - ref).abs()
+    assert bool((err <= bound).all()), (float((err - bound).max()), (err > bound).nonzero()[:5].tolist())
+    return table
+
+
+WIDTHS = [1, 2, 3, 7, 8, 9, 15, 16, 31, 64, 100, 511, 512, 513, 1000, 1537, 2048, 2056, 4096, 5001]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_widths(d, dtype, gpu):
+    for n, v in ((1, 1), (37, 11), (300, 257)):
+        ids = tokens(n, v, d + n)
+        check_fwd(rows(v, d, dtype, d), ids, scale=1.7)
+        check_bwd(rows(n, d, dtype, d + 1), ids, v, scale=1.7)
+
+
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 511, 513, 4095, 4096, 4097, 6145, 20000, 70001])
+@pytest.mark.parametrize("v", [1, 2, 500, 151936])
+def test_batches(n, v, gpu):
+    """Both sorts and their edges, tables with a row for most tokens and for few."""
+    ids = tokens(n, v, n, skew=6.0)
+    check_bwd(rows(n, 24, "bf16", n), ids, v)
+    check_fwd(rows(v, 24, "bf16", v), ids)
+
+
+@pytest.mark.parametrize("v", [511, 512, 513, 255, 256, 257, 2 ** 18 - 1, 2 ** 18, 2 ** 18 + 1, 2 ** 24])
+def test_vocabularies_at_the_edges_of_the_sorts_digits(v, gpu):
+    for n in (1000, 9000):
+        ids = tokens(n, v, v, skew=1.0)
+        ids[0], ids[-1], ids[n // 2] = v - 1, v - 1, 0
+        check_bwd(rows(n, 8, "f32", n), ids, v)
+
+
+@pytest.mark.parametrize("n", [4000, 30000])
+def test_one_token_takes_everything(n, gpu):
+    """A segment over all runs; one over nearly all of them, with others on both sides."""
+    g = rows(n, 520, "bf16", n)
+    ids = torch.full((n,), 3, dtype=torch.int32, device="cuda")
+    check_bwd(g, ids, 7)
+    ids[5], ids[n - 9], ids[100:164] = 1, 6, 2
+    check_bwd(g, ids, 7)
+
+
+@pytest.mark.parametrize("pad,start", [(1, 0), (5, 3), (0, 1), (8, 8)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_and_starts(pad, start, dtype, gpu):
+    for d in (5, 64, 777):
+        n, v = 200, 90
+        ids = tokens(n, v, d)
+        table = rows(v, d, dtype, d, pad=pad, start=start)
+        out = rows(n, d, dtype, 1, pad=pad, start=start)
+        behind = out.untyped_storage().nbytes()
+        check_fwd(table, ids, out=out)
+        whole = torch.empty(0, dtype=DT[dtype], device="cuda").set_(out.untyped_storage())
+        left = torch.ones(behind // out.element_size(), dtype=torch.bool, device="cuda")
+        for i in range(n):
+            left[start + i * (d + pad):start + i * (d + pad) + d] = False
+        assert bool(whole[left].isnan().all())  # nothing outside the rows is written
+        grad_table = check_bwd(rows(n, d, dtype, d, pad=pad, start=start), ids, v, dtype=dtype, pad=pad)
+        if pad:
+            whole = torch.as_strided(grad_table, (v - 1, pad), (d + pad, 1), grad_table.storage_offset() + d)
+            assert bool(whole.isnan().all())
+
+
+def test_types(gpu):
+    ids = tokens(500, 300, 1)
+    for table, out in (("bf16", "f32"), ("f32", "bf16")):
+        check_fwd(rows(300, 136, table, 2), ids, scale=3.3, dtype=DT[out])
+        check_fwd(rows(300, 5, table, 2), ids, scale=3.3, dtype=DT[out])
+        check_bwd(rows(500, 136, table, 3), ids, 300, scale=3.3, dtype=out)
+        check_bwd(rows(500, 5, table, 3), ids, 300, scale=3.3, dtype=out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [700, 9000])
+def test_accumulate(n, dtype, gpu):
+    check_bwd(rows(n, 100, "bf16", n), tokens(n, 1000, n), 1000, dtype=dtype, accumulate=True, scale=0.3)
+
+
+@pytest.mark.parametrize("n", [1, 700, 9000])
+def test_masks(n, gpu):
+    g = rows(n, 40, "bf16", n)
+    ids = tokens(n, 50, n)
+    mask = (torch.rand(n, generator=gen(n), device="cuda") < 0.6).to(torch.uint8)
+    ids[mask == 0] = 12345678  # not looked at
+    g[mask == 0] = math.nan
+    check_fwd(rows(50, 40, "bf16", 2), ids, mask=mask)
+    none = torch.zeros_like(mask)
+    check_fwd(rows(50, 40, "bf16", 2), ids, mask=none)
+    safe = torch.where(g.isnan(), torch.zeros_like(g), g)
+    want = check_bwd(safe, ids, 50, mask=mask)
+    got = torch.empty_like(want)
+    T.embed_bwd(g, ids, got, mask=mask)
+    assert torch.equal(got, want)
+    assert not bool(T.embed_bwd(g, ids, got, mask=none).any())
+
+
+@pytest.mark.parametrize("n", [600, 9000])
+def test_ids_outside_the_table(n, gpu):
+    ids = tokens(n, 50, n)
+    ids[7], ids[n - 3], ids[200] = -1, 50, 2 ** 31 - 1
+    g = rows(n, 16, "f32", n)
+    check_fwd(rows(50, 16, "f32", 2), ids)
+    check_bwd(g, ids, 50, check=False)
+    ws = T.EmbedWorkspace(n, 50, 16)
+    table = torch.empty((50, 16), device="cuda")
+    with pytest.raises(T.TurnKLError) as e:
+        T.embed_bwd(g, ids, table, workspace=ws)
+    assert e.value.code == T.ERR_TOKEN_ID
+    ids[7], ids[n - 3], ids[200] = 1, 2, 3
+    T.embed_bwd(g, ids, table, workspace=ws)  # the status is that of the last call
+    assert ws.status() == T.OK
+
+
+def test_no_tokens(gpu):
+    ids = torch.empty(0, dtype=torch.int32, device="cuda")
+    g = torch.empty((0, 33), device="cuda")
+    assert T.embed_fwd(rows(5, 33, "f32", 1), ids).shape == (0, 33)
+    table = rows(70, 33, "f32", 1)
+    old = table.clone()
+    T.embed_bwd(g, ids, table, accumulate=True)
+    assert torch.equal(table, old)
+    assert not bool(T.embed_bwd(g, ids, table).any())
+
+
+def test_values_that_are_no_numbers(gpu):
+    table = rows(9, 24, "f32", 1)
+    table[3], table[4, 5] = math.inf, math.nan
+    ids = torch.tensor([3, 4, 2, 3], dtype=torch.int32, device="cuda")
+    y = T.embed_fwd(table, ids, scale=2.0)
+    assert bool((y[0] == math.inf).all()) and bool(y[1, 5].isnan()) and bool(y[2].isfinite().all())
+    g = torch.ones((4, 24), device="cuda")
+    g[1] = math.inf
+    got = T.embed_bwd(g, ids, torch.empty((9, 24), device="cuda"))
+    assert bool((got[4] == math.inf).all()) and bool((got[3] == 2).all()) and not bool(got[2:3].eq(0).any())
+    assert not bool(got[5:].any())
+
+
+def test_the_same_bits_from_call_to_call(gpu):
+    n = 30000
+    g, ids = rows(n, 300, "bf16", 3), tokens(n, 5000, 3, skew=8.0)
+    first = T.embed_bwd(g, ids, torch.empty((5000, 300), device="cuda"))
+    ws = T.EmbedWorkspace(70000, 9000, 600)  # one for a larger batch
+    for _ in range(3):
+        ws.tensor.random_(0, 255)
+        assert torch.equal(T.embed_bwd(g, ids, torch.empty_like(first), workspace=ws), first)
+
+
+def test_differences(gpu):
+    """dL/dE of L = sum(c * y) by central differences, which are exact up to rounding for a
+    linear map: c has few bits."""
+    v, d, n = 6, 10, 40
+    ids = tokens(n, v, 1, skew=1.0)
+    table = torch.randint(-8, 8, (v, d), generator=gen(1), device="cuda").float()
+    c = torch.randint(-8, 8, (n, d), generator=gen(2), device="cuda").float()
+    got = T.embed_bwd(c, ids, torch.empty_like(table), scale=0.5)
+    for at in ((0, 0), (3, 9), (5, 4)):
+        step = torch.zeros_like(table)
+        step[at] = 1.0
+        up = (c * T.embed_fwd(table + step, ids, scale=0.5)).sum()
+        down = (c * T.embed_fwd(table - step, ids, scale=0.5)).sum()
+        assert float(got[at]) == float(up - down) / 2
+
+
+def test_graph_replays(gpu):
+    """Both calls captured together, replayed with other ids, eager work between."""
+    for n in (900, 9000):
+        v, d = 3000, 64
+        table, g = rows(v, d, "bf16", 1), rows(n, d, "bf16", 2)
+        ids = tokens(n, v, 1)
+        y, gt = torch.empty_like(g), torch.empty((v, d), device="cuda")
+        ws = T.EmbedWorkspace(n, v, d)
+        call = lambda: (T.embed_fwd(table, ids, scale=2.0, out=y),  # noqa: E731
+                        T.embed_bwd(g, ids, gt, scale=2.0, workspace=ws, check=False))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        for r in range(4):
+            ids.copy_(tokens(n, v, 10 + r))
+            graph.replay()
+            got = y.clone(), gt.clone()
+            gt.fill_(math.nan)
+            torch.cuda.synchronize()
+            call()
+            assert torch.equal(got[0], y) and torch.equal(got[1], gt)
+            assert ws.status() == T.OK
+
+
+def test_streams(gpu):
+    """Two calls at once on streams and workspaces of their own."""
+    n, v, d = 20000, 9000, 256
+    made = []
+    for i in range(2):
+        made.append((rows(n, d, "bf16", i), tokens(n, v, i), torch.empty((v, d), device="cuda"),
+                     T.EmbedWorkspace(n, v, d), torch.cuda.Stream()))
+    want = [T.embed_bwd(g, ids, torch.empty((v, d), device="cuda")) for g, ids, *_ in made]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, ids, gt, ws, stream in made:
+            with torch.cuda.stream(stream):
+                T.embed_bwd(g, ids, gt, workspace=ws, check=False)
+    torch.cuda.synchronize()
+    for w, (_, _, gt, _, _) in zip(want, made):
+        assert torch.equal(gt, w)
+
+
+def test_offsets_past_32_bits(gpu):
+    """A table of 5 GiB and rows of 4.4 GB: the last rows of each."""
+    v, d = 160000, 16384
+    table = torch.empty((v, d), dtype=torch.bfloat16, device="cuda")
+    table[-1] = 1.5
+    table[0] = -2.0
+    ids = torch.full((140000,), v - 1, dtype=torch.int32, device="cuda")
+    ids[0] = 0
+    y = T.embed_fwd(table, ids)
+    assert bool((y[0] == -2).all()) and bool((y[-3:] == 1.5).all()) and bool((y[70000] == 1.5).all())
+    del y
+    g = torch.zeros((140000, d), dtype=torch.bfloat16, device="cuda")
+    g[-1], g[-2], g[0] = 1.0, 2.0, 4.0
+    T.embed_bwd(g, ids, table)
+    assert bool((table[-1] == 3).all()) and bool((table[0] == 4).all())
+    assert not bool(table[1:3].any()) and not bool(table[v - 3:v - 1].any())
+
+
+def test_refusals(gpu):
+    table, ids = rows(9, 8, "f32", 1), tokens(4, 9, 1)
+    g = rows(4, 8, "f32", 1)
+    for call in (lambda: T.embed_fwd(table, ids.long()), lambda: T.embed_fwd(table, ids.cpu()),
+                 lambda: T.embed_fwd(table, ids, mask=torch.ones(3, dtype=torch.uint8, device="cuda")),
+                 lambda: T.embed_fwd(table, ids, out=g[:3]), lambda: T.embed_fwd(table.t(), ids),
+                 lambda: T.embed_bwd(g, ids, table[:, :7]), lambda: T.embed_bwd(g[:3], ids, table)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        T.embed_fwd(table.half(), ids)
+    with pytest.raises(TypeError):
+        T.embed_fwd(table, ids, out=g, dtype=torch.bfloat16)
+    with pytest.raises(T.TurnKLError) as e:
+        T.embed_fwd(table, ids, scale=math.inf)
+    assert e.value.code == T.ERR_INVALID_ARG
+    with pytest.raises(T.TurnKLError) as e:
+        T.embed_fwd(table, ids, out=table[:4])
+    assert e.value.code == T.ERR_ALIAS
+    with pytest.raises(T.TurnKLError) as e:
+        T.embed_bwd(rows(900, 8, "f32", 1), tokens(900, 9, 1), torch.empty((9, 8), device="cuda"),
+                    workspace=T.EmbedWorkspace(1, 1, 1))
+    assert e.value.code == T.ERR_WORKSPACE
