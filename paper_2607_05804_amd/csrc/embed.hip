@@ -27,7 +27,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(EmbedParams p) {
   const int lane = threadIdx.x & (p.lanes - 1);
   const int slot = threadIdx.x / p.lanes;
   const int side = kEmbThreads / p.lanes;  // rows side by side in a workgroup
-  const int units = (p.width + kUnit - 1) / kUnit;
+  constexpr int kEl = unit_elements(kTab16, kOut16);
+  const int units = (p.width + kEl - 1) / kEl;
   for (long long block = blockIdx.x; block < p.n_blocks; block += gridDim.x) {
     const long long row = block / p.parts * side + slot;
     const int first = (int)(block % p.parts) * (p.lanes * kEmbUnits) + lane;
@@ -37,13 +38,13 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(EmbedParams p) {
     const bool in = id >= 0 && id < p.vocab;
     const char* const from = static_cast<const char*>(p.table) + (in ? (long long)id * p.ld_table : 0) * (kTab16 ? 2 : 4);
     char* const to = static_cast<char*>(p.out) + row * p.ld_out * (kOut16 ? 2 : 4);
-    Place at[kEmbUnits];
-    Unit<kTab16, true> x[kEmbUnits];
-    Unit<kOut16> y[kEmbUnits];
+    Place<kEl> at[kEmbUnits];
+    Unit<kTab16, kEl, true> x[kEmbUnits];
+    Unit<kOut16, kEl> y[kEmbUnits];
 #pragma unroll
     for (int q = 0; q < kEmbUnits; ++q) {
       const int u = first + q * p.lanes;
-      at[q] = u < units ? place_unit(u, p.width) : Place{0, 0u};
+      at[q] = u < units ? place_unit<kEl>(u, p.width) : Place<kEl>{0, 0u};
       x[q].clear();
       if (in) load_unit(x[q], from, at[q], p.width);
     }
@@ -51,13 +52,13 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(EmbedParams p) {
     const float none = on ? __builtin_nanf("") : 0.0f;
 #pragma unroll
     for (int q = 0; q < kEmbUnits; ++q) {
-      float v[kUnit];
+      float v[kEl];
 #pragma unroll
-      for (int j = 0; j < kUnit; ++j) v[j] = in ? x[q].get(j) * p.scale : none;
+      for (int j = 0; j < kEl; ++j) v[j] = in ? x[q].get(j) * p.scale : none;
       y[q].set(v);
     }
 #pragma unroll
-    for (int q = 0; q < kEmbUnits; ++q) y[q].settle();
+    for (int q = 0; q < kEmbUnits; ++q) y[q].fence();
 #pragma unroll
     for (int q = 0; q < kEmbUnits; ++q) store_edge(y[q], to, at[q]);
 #pragma unroll
@@ -66,6 +67,49 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(EmbedParams p) {
     for (int q = 0; q < kEmbUnits; ++q) y[q].keep();
     if (block + gridDim.x < p.n_blocks) drain_stores();  // before their data is rewritten
   }
+}
+
+// ---------------------------------------------------------------------------
+// zeroing the table beside the sort
+
+constexpr int kSortThreads = 512;
+
+// The share of one of the sort's launches in zeroing the whole table, by the workgroups
+// behind the p.n_tiles that sort: 16 bytes a thread, in address order, and nothing loaded
+// before (2.5 GB: 6.9 TB/s; longer-lived workgroups write 5.7).
+template <int kEs>
+__device__ inline void zero_share(const EmbedGradParams& p) {
+  const unsigned per_row = p.fill_per_row;
+  const u32x4_any z = {0u, 0u, 0u, 0u};
+  const long long stride = (long long)(gridDim.x - p.n_tiles) * kSortThreads;
+  for (long long i = p.fill_from + (long long)(blockIdx.x - p.n_tiles) * kSortThreads; i < p.fill_to; i += stride) {
+    // (of a table without padding per_row is 0: one row)
+    const long long row0 = per_row ? i / per_row : 0;
+    const long long q0 = i - row0 * per_row + threadIdx.x;
+    if (i + threadIdx.x >= p.fill_to) continue;
+    long long row = row0, q = q0;
+    if (per_row) {
+      row += (unsigned)q0 / per_row;
+      q = (unsigned)q0 % per_row;
+    }
+    char* const at = static_cast<char*>(p.table) + row * p.ld_table * kEs + q * 16;
+    const long long rest = (per_row ? (long long)p.width : p.fill_elems) * kEs - q * 16;
+    if (rest >= 16) {
+      if (p.fill_stream) __builtin_nontemporal_store(z, reinterpret_cast<u32x4_any*>(at));
+      else *reinterpret_cast<u32x4_any*>(at) = z;
+    } else {
+      for (int j = 0; j < (int)rest / kEs; ++j) {
+        if constexpr (kEs == 2) reinterpret_cast<unsigned short*>(at)[j] = 0;
+        else reinterpret_cast<unsigned*>(at)[j] = 0u;
+      }
+    }
+  }
+}
+__device__ inline bool zeroes_instead(const EmbedGradParams& p) {
+  if ((int)blockIdx.x < p.n_tiles) return false;
+  if (p.table_bf16) zero_share<2>(p);
+  else zero_share<4>(p);
+  return true;
 }
 
 // ---------------------------------------------------------------------------
@@ -98,7 +142,6 @@ __device__ inline unsigned long long same_digit(int d) {
   return m;
 }
 
-constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kSmallSort = kEmbedSmallSort;
 constexpr int kSmallSteps = kSmallSort / kSortThreads;
@@ -110,6 +153,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_small(EmbedGradParams
   __shared__ unsigned short s_tok[2][kSmallSort];
   __shared__ int s_hist[kSortWaves][kDigits];
   __shared__ int s_scan[kSortWaves];
+  if (zeroes_instead(p)) return;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -179,6 +223,7 @@ constexpr int kDigits = 1 << kEmbedDigitBits;
 static_assert(kDigits == kSortThreads, "a thread per digit");
 __global__ __launch_bounds__(kSortThreads) void embed_count(EmbedGradParams p) {
   __shared__ int s_count[kDigits];
+  if (zeroes_instead(p)) return;
   s_count[threadIdx.x] = 0;
   if (p.turn == 0 && blockIdx.x == 0 && threadIdx.x == 0) p.hdr->err_key = kNoError;
   __syncthreads();
@@ -199,6 +244,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter(EmbedGradParams p)
   __shared__ int s_hist[kSortWaves][kDigits];
   __shared__ int s_base[kDigits];
   __shared__ int s_scan[kSortWaves];
+  if (zeroes_instead(p)) return;
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -266,25 +312,46 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter(EmbedGradParams p)
 // summing
 
 constexpr int kSumCols = kEmbedTileCols;  // columns of a wave
-constexpr int kSumBatch = 8;              // rows whose loads are under way together
+constexpr int kSumBatch = 4;              // rows whose loads are under way together
 
-// A lane's eight columns of a table row: stored, or added to what is there.
+// A lane's columns of a run of 512: two units of four, 256 columns apart.
+constexpr int kSumEl = 4;
+constexpr int kSumUnits = 2;
+using SumPlace = Place<kSumEl>;
+__device__ inline void sum_places(int tile, int lane, int width, SumPlace (&at)[kSumUnits]) {
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q)
+    at[q] = place_unit<kSumEl>(tile * (kSumCols / kSumEl) + q * kWave + lane, width);
+}
+
+// They are stored, or added to what is there.
 template <bool kTab16>
-__device__ inline void write_table(const EmbedGradParams& p, int id, const Place& at, const float (&sum)[kUnit]) {
+__device__ inline void write_table(const EmbedGradParams& p, int id, const SumPlace (&at)[kSumUnits],
+                                   const float (&sum)[kSumUnits][kSumEl]) {
   char* const row = static_cast<char*>(p.table) + (long long)id * p.ld_table * (kTab16 ? 2 : 4);
-  float v[kUnit];
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) v[j] = sum[j] * p.scale;
+  Unit<kTab16, kSumEl> old[kSumUnits], out[kSumUnits];
   if (p.accumulate) {
-    Unit<kTab16> old;
-    load_unit(old, row, at, p.width);
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) v[j] += old.get(j);
+    for (int q = 0; q < kSumUnits; ++q) load_unit(old[q], row, at[q], p.width);
   }
-  Unit<kTab16> out;
-  out.set(v);
-  out.settle();
-  store_unit(out, row, at);
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q) {
+    float v[kSumEl];
+#pragma unroll
+    for (int j = 0; j < kSumEl; ++j) {
+      v[j] = sum[q][j] * p.scale;
+      if (p.accumulate) v[j] += old[q].get(j);
+    }
+    out[q].set(v);
+  }
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q) out[q].fence();
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q) store_edge(out[q], row, at[q]);
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q) store_whole(out[q], row, at[q]);
+#pragma unroll
+  for (int q = 0; q < kSumUnits; ++q) out[q].keep();
   store_gap();
 }
 
@@ -306,12 +373,12 @@ __device__ inline int first_at_least(const int* key, int n, int v) {
   return (int)lo;
 }
 
-// The table's rows [first, first + rows) that occur nowhere are zeroed.
+// Zeroes those of fill_rows table rows that no token has.
 template <bool kTab16>
-__device__ inline void zero_absent(const EmbedGradParams& p, long long block) {
+__device__ inline void zero_absent(const EmbedGradParams& p, int block) {
   __shared__ unsigned s_seen[kEmbedFillRows / 32];
   const int tid = threadIdx.x;
-  const long long first = block * p.fill_rows;
+  const long long first = (long long)block * p.fill_rows;
   const int rows = (int)(p.vocab - first < p.fill_rows ? p.vocab - first : p.fill_rows);
   for (int i = tid; i < kEmbedFillRows / 32; i += kEmbThreads) s_seen[i] = 0u;
   __syncthreads();
@@ -325,22 +392,37 @@ __device__ inline void zero_absent(const EmbedGradParams& p, long long block) {
     if (!__syncthreads_or(in)) break;  // sorted: none of those that follow either
   }
   __syncthreads();
-  const int units = (p.width + kUnit - 1) / kUnit;
-  Unit<kTab16> none;
-  none.clear();
-  none.settle();
-  for (int r = 0; r < rows; ++r) {
+  // 16 bytes a thread side by side (32 as two stores leave gaps in every line that a wave
+  // writes), as many threads to a row as it has such packs
+  constexpr int kEs = kTab16 ? 2 : 4, kPack = 16 / kEs;
+  const int packs = p.width / kPack, rest = p.width - packs * kPack;
+  int lanes = kEmbThreads;
+  while (lanes > 1 && lanes / 2 >= packs + (rest > 0)) lanes /= 2;
+  u32x4 none{0u, 0u, 0u, 0u};
+  settle_words(none);
+  for (int r = tid / lanes; r < rows; r += kEmbThreads / lanes) {
     if ((s_seen[r >> 5] >> (r & 31)) & 1u) continue;
-    char* const row = static_cast<char*>(p.table) + (first + r) * p.ld_table * (kTab16 ? 2 : 4);
-    for (int u = tid; u < units; u += kEmbThreads) store_unit(none, row, place_unit(u, p.width));
+    char* const row = static_cast<char*>(p.table) + (first + r) * p.ld_table * kEs;
+    for (int u = tid % lanes; u < packs + (rest > 0); u += lanes) {
+      if (u < packs) {
+        u32x4_any* const at = reinterpret_cast<u32x4_any*>(row + 16 * u);
+        if (p.fill_stream) __builtin_nontemporal_store(u32x4_any(none), at);
+        else *at = none;
+      } else {
+        for (int j = packs * kPack; j < p.width; ++j) {
+          if constexpr (kTab16) reinterpret_cast<unsigned short*>(row)[j] = 0;
+          else reinterpret_cast<unsigned*>(row)[j] = 0u;
+        }
+      }
+    }
   }
-  none.keep();
+  keep_alive(none);
 }
 
 template <bool kGrad16, bool kTab16>
 __global__ __launch_bounds__(kEmbThreads) void embed_sum(EmbedGradParams p) {
   if ((int)blockIdx.x >= p.sum_blocks) {
-    zero_absent<kTab16>(p, blockIdx.x - p.sum_blocks);
+    zero_absent<kTab16>(p, (int)blockIdx.x - p.sum_blocks);
     return;
   }
   const int lane = threadIdx.x & (kWave - 1);
@@ -358,27 +440,42 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum(EmbedGradParams p) {
   const int key_before = start > 0 ? keys[start - 1] : -1;
   const int key_after = start + p.run < p.n_rows ? keys[start + p.run] : p.vocab;
   const int count = __popcll(__ballot(key < p.vocab));  // sorted: the first ones
-  const Place at = place_unit(tile * (kSumCols / kUnit) + lane, p.width);
+  SumPlace at[kSumUnits];
+  sum_places(tile, lane, p.width, at);
   const long long ld = p.ld_grad * (kGrad16 ? 2 : 4);
-  float sum[kUnit];
+  float sum[kSumUnits][kSumEl];
+  auto restart = [&] {
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) sum[j] = 0.0f;
-  float* const part = p.part + (long long)run * 2 * p.part_ld + tile * kSumCols + lane * kUnit;
+    for (int q = 0; q < kSumUnits; ++q)
+#pragma unroll
+      for (int j = 0; j < kSumEl; ++j) sum[q][j] = 0.0f;
+  };
+  restart();
+  float* const part = p.part + (long long)run * 2 * p.part_ld + tile * kSumCols + lane * kSumEl;
   int begun = 0;  // position where the segment at hand begins in the run
-  for (int i0 = 0; i0 < count; i0 += kSumBatch) {
-    Unit<kGrad16> g[kSumBatch];
+  // A batch's rows are asked for before the one ahead is summed: loads behind a store are
+  // not seen until it has been acknowledged.
+  using Batch = Unit<kGrad16, kSumEl>[kSumBatch][kSumUnits];
+  auto fetch = [&](Batch& g, int i0) {
 #pragma unroll
-    for (int b = 0; b < kSumBatch; ++b) {
-      g[b].clear();
-      if (i0 + b < count)
-        load_unit(g[b], static_cast<const char*>(p.grad) + __builtin_amdgcn_readlane(tok, i0 + b) * ld, at, p.width);
-    }
+    for (int b = 0; b < kSumBatch; ++b)
+#pragma unroll
+      for (int q = 0; q < kSumUnits; ++q) {
+        g[b][q].clear();
+        if (i0 + b < count)
+          load_unit(g[b][q], static_cast<const char*>(p.grad) + __builtin_amdgcn_readlane(tok, i0 + b) * ld, at[q],
+                    p.width);
+      }
+  };
+  auto add = [&](const Batch& g, int i0) {
 #pragma unroll
     for (int b = 0; b < kSumBatch; ++b) {
       const int i = i0 + b;
       if (i >= count) break;
 #pragma unroll
-      for (int j = 0; j < kUnit; ++j) sum[j] += g[b].get(j);
+      for (int q = 0; q < kSumUnits; ++q)
+#pragma unroll
+        for (int j = 0; j < kSumEl; ++j) sum[q][j] += g[b][q].get(j);
       const int id = __builtin_amdgcn_readlane(key, i);
       const bool run_ends = i + 1 == p.run;
       const int next = run_ends ? key_after : i + 1 < count ? __builtin_amdgcn_readlane(key, i + 1) : p.vocab;
@@ -388,16 +485,31 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum(EmbedGradParams p) {
         write_table<kTab16>(p, id, at, sum);
       } else {
         // a piece: behind [1] where the segment begins here, else in front [0]
-        Unit<false> piece;
-        piece.set(sum);
-        piece.settle();
-        piece.store(reinterpret_cast<char*>(part + (whole_front ? p.part_ld : 0)), 0);
+        char* const to = reinterpret_cast<char*>(part + (whole_front ? p.part_ld : 0));
+        Unit<false, kSumEl> piece[kSumUnits];
+#pragma unroll
+        for (int q = 0; q < kSumUnits; ++q) {
+          piece[q].set(sum[q]);
+          piece[q].fence();
+        }
+#pragma unroll
+        for (int q = 0; q < kSumUnits; ++q) piece[q].store(to, q * kWave * kSumEl);
+#pragma unroll
+        for (int q = 0; q < kSumUnits; ++q) piece[q].keep();
         store_gap();
       }
       begun = i + 1;
-#pragma unroll
-      for (int j = 0; j < kUnit; ++j) sum[j] = 0.0f;
+      restart();
     }
+  };
+  Batch even, odd;
+  fetch(even, 0);
+#pragma unroll 1
+  for (int i0 = 0; i0 < count; i0 += 2 * kSumBatch) {
+    fetch(odd, i0 + kSumBatch);
+    add(even, i0);
+    fetch(even, i0 + 2 * kSumBatch);
+    add(odd, i0 + kSumBatch);
   }
 }
 
@@ -426,27 +538,33 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
     last += n;
     if (n < kWave) break;
   }
-  const long long col = tile * kSumCols + lane * kUnit;
-  const Place at = place_unit(tile * (kSumCols / kUnit) + lane, p.width);
-  float sum[kUnit];
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) sum[j] = 0.0f;
+  const float* const part = p.part + tile * kSumCols + lane * kSumEl;
+  SumPlace at[kSumUnits];
+  sum_places(tile, lane, p.width, at);
+  float sum[kSumUnits][kSumEl] = {};
 #pragma unroll 4
   for (int r = run + wid; r <= last; r += kWaves) {
-    const float* const from = p.part + ((long long)r * 2 + (r == run ? 1 : 0)) * p.part_ld + col;
-    Unit<false> x;
-    x.load(reinterpret_cast<const char*>(from), 0);
+    const char* const from = reinterpret_cast<const char*>(part + ((long long)r * 2 + (r == run ? 1 : 0)) * p.part_ld);
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) sum[j] += x.get(j);
+    for (int q = 0; q < kSumUnits; ++q) {
+      Unit<false, kSumEl> x;
+      x.load(from, q * kWave * kSumEl);
+#pragma unroll
+      for (int j = 0; j < kSumEl; ++j) sum[q][j] += x.get(j);
+    }
   }
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) s_sum[wid][lane * kUnit + j] = sum[j];
+  for (int q = 0; q < kSumUnits; ++q)
+#pragma unroll
+    for (int j = 0; j < kSumEl; ++j) s_sum[wid][(q * kSumEl + j) * kWave + lane] = sum[q][j];
   __syncthreads();
   if (wid != 0) return;
 #pragma unroll
   for (int w = 1; w < kWaves; ++w)
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) sum[j] += s_sum[w][lane * kUnit + j];
+    for (int q = 0; q < kSumUnits; ++q)
+#pragma unroll
+      for (int j = 0; j < kSumEl; ++j) sum[q][j] += s_sum[w][(q * kSumEl + j) * kWave + lane];
   write_table<kTab16>(p, id, at, sum);
 }
 
@@ -477,7 +595,8 @@ EmbedShape embed_shape(long long n, long long vocab, long long width) {
 hipError_t launch_embed(const EmbedParams& given, hipStream_t s) {
   EmbedParams p = given;
   if (p.n_rows == 0) return hipSuccess;
-  const int units = (p.width + kUnit - 1) / kUnit;
+  const int el = unit_elements(p.table_bf16, p.out_bf16);
+  const int units = (p.width + el - 1) / el;
   p.lanes = 1;
   while (p.lanes < kWave && p.lanes < units) p.lanes *= 2;
   p.parts = (units + p.lanes * kEmbUnits - 1) / (p.lanes * kEmbUnits);
@@ -493,32 +612,56 @@ hipError_t launch_embed(const EmbedParams& given, hipStream_t s) {
 
 hipError_t launch_embed_bwd(const EmbedGradParams& given, hipStream_t s) {
   EmbedGradParams p = given;
-  if (p.n_rows <= kEmbedSmallSort) {
+  const int es = p.table_bf16 ? 2 : 4;
+  // A table is zeroed whole, beside the sort, where the tokens touch little of it and the
+  // sort is worth hiding; else where it has no token, beside the sums.
+  const double bytes = (double)p.vocab * p.width * es;
+  p.fill_stream = bytes > kEmbedCachedFill;
+  const bool whole = !p.accumulate && p.n_rows <= p.vocab / 2 && bytes >= kEmbedWholeFill;
+  const bool small = p.n_rows <= kEmbedSmallSort;
+  const int turns = small ? 1 : (p.key_bits + kEmbedDigitBits - 1) / kEmbedDigitBits;
+  const int launches = small ? 1 : 2 * turns;
+  long long packs = 0, fills = 0;  // of the table, and workgroups of a launch for them
+  if (whole) {
+    const long long row = ((long long)p.width * es + 15) / 16;
+    p.fill_per_row = p.ld_table == p.width ? 0 : (unsigned)row;
+    p.fill_elems = (long long)p.vocab * p.width;
+    packs = p.fill_per_row ? row * p.vocab : (p.fill_elems * es + 15) / 16;
+    fills = (packs / launches + kSortThreads) / kSortThreads;
+    fills = fills < kEmbedFillBlocks ? fills : kEmbedFillBlocks;
+  }
+  auto share = [&](int launch) {
+    p.fill_from = packs * launch / launches;
+    p.fill_to = packs * (launch + 1) / launches;
+  };
+  if (small) {
     p.key_out = p.key[0];
     p.tok_out = p.tok[0];
-    embed_sort_small<<<1, kSortThreads, 0, s>>>(p);
-    p.key_in = p.key[0];
-    p.tok_in = p.tok[0];
-  } else {
-    const int turns = (p.key_bits + kEmbedDigitBits - 1) / kEmbedDigitBits;
-    for (p.turn = 0; p.turn < turns; ++p.turn) {
-      p.key_out = p.key[p.turn & 1];
-      p.tok_out = p.tok[p.turn & 1];
-      embed_count<<<p.n_tiles, kSortThreads, 0, s>>>(p);
-      embed_scatter<<<p.n_tiles, kSortThreads, 0, s>>>(p);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-      p.key_in = p.key_out;
-      p.tok_in = p.tok_out;
-    }
+    p.n_tiles = 1;
+    share(0);
+    embed_sort_small<<<1 + (int)fills, kSortThreads, 0, s>>>(p);
+    p.key_in = p.key_out;
+    p.tok_in = p.tok_out;
+  }
+  for (p.turn = 0; !small && p.turn < turns; ++p.turn) {
+    p.key_out = p.key[p.turn & 1];
+    p.tok_out = p.tok[p.turn & 1];
+    share(2 * p.turn);
+    embed_count<<<p.n_tiles + (int)fills, kSortThreads, 0, s>>>(p);
+    share(2 * p.turn + 1);
+    embed_scatter<<<p.n_tiles + (int)fills, kSortThreads, 0, s>>>(p);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    p.key_in = p.key_out;
+    p.tok_in = p.tok_out;
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const long long tasks = (long long)p.n_runs * p.col_tiles;
   p.sum_blocks = (int)((tasks + kEmbThreads / kWave - 1) / (kEmbThreads / kWave));
   p.fill_rows = kEmbedFillRows;
-  while (p.fill_rows > 64 && (long long)p.fill_rows * p.width > (1 << 18)) p.fill_rows /= 2;
-  const int fills = p.accumulate ? 0 : (int)(((long long)p.vocab + p.fill_rows - 1) / p.fill_rows);
-  if (p.sum_blocks + fills == 0) return hipSuccess;
-  const int grid = p.sum_blocks + fills;
+  while (p.fill_rows > 2 && (long long)p.fill_rows * p.width > kEmbedFillElems) p.fill_rows /= 2;
+  const int absent = p.accumulate || whole ? 0 : (int)(((long long)p.vocab + p.fill_rows - 1) / p.fill_rows);
+  if (p.sum_blocks + absent == 0) return hipSuccess;
+  const int grid = p.sum_blocks + absent;
   if (p.grad_bf16 && p.table_bf16) embed_sum<true, true><<<grid, kEmbThreads, 0, s>>>(p);
   else if (p.grad_bf16) embed_sum<true, false><<<grid, kEmbThreads, 0, s>>>(p);
   else if (p.table_bf16) embed_sum<false, true><<<grid, kEmbThreads, 0, s>>>(p);

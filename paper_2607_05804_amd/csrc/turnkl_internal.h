@@ -477,11 +477,15 @@ struct EmbedParams {
   int out_bf16;
 };
 
-constexpr int kEmbedSmallSort = 4096;  // tokens that one workgroup sorts
+constexpr int kEmbedSmallSort = 2048;  // tokens that one workgroup sorts
 constexpr int kEmbedDigitBits = 9;     // of a turn of the sort of more
 constexpr int kEmbedTileCols = 512;    // columns that a wave sums
 constexpr int kEmbedWaves = 4096;      // that sum at once, at least where there is work for them
 constexpr int kEmbedFillRows = 1024;   // table rows that a workgroup looks after, at most
+constexpr int kEmbedFillElems = 1 << 15;  // and elements
+constexpr long long kEmbedFillBlocks = 1 << 22;  // of a launch, which holds fewer than 2^32 threads
+constexpr double kEmbedWholeFill = 64.0 * (1 << 20);  // bytes of a table zeroed whole, at least
+constexpr double kEmbedCachedFill = 192.0 * (1 << 20);  // and through the caches, at most
 
 struct EmbedShape {
   int run;           // sorted tokens that a wave sums
@@ -523,6 +527,11 @@ struct EmbedGradParams {
   int turn;        // set at launch, like the next two
   int sum_blocks;  // workgroups that sum, before those that zero
   int fill_rows;   // table rows of one of those
+  long long fill_from;  // 16-byte packs that a launch of the sort zeroes
+  long long fill_to;
+  long long fill_elems;   // of a table without padding
+  unsigned fill_per_row;  // packs of a row with padding, or 0
+  int fill_stream;
   float scale;
   int grad_bf16;
   int table_bf16;

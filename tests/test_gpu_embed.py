@@ -90,7 +90,7 @@ def test_widths(d, dtype, gpu):
         check_bwd(rows(n, d, dtype, d + 1), ids, v, scale=1.7)
 
 
-@pytest.mark.parametrize("n", [1, 63, 64, 65, 511, 513, 4095, 4096, 4097, 6145, 20000, 70001])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 511, 513, 2047, 2048, 2049, 4097, 6145, 20000, 70001])
 @pytest.mark.parametrize("v", [1, 2, 500, 151936])
 def test_batches(n, v, gpu):
     """Both sorts and their edges, tables with a row for most tokens and for few."""
