@@ -508,6 +508,88 @@ int turnkl_norm_bwd(const void* grad_y, int64_t ld_gy, const void* x, int64_t ld
                     hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * The norms on either side of a block, fused with the block's gate and the
+ * residual sum, and their gradient.  For a row h of the residual stream and a row f
+ * of the block's output (the branch), with norms of the layer or the
+ * root-mean-square kind as in turnkl_norm_fwd ((mu_f, r_f) of f, (mu, r) of h'):
+ *   a  = (f - mu_f) r_f w_post where post_norm is set, f itself otherwise,
+ *   h' = s h + gate a,       y = (h' - mu) r w + b,
+ * and for the gradients gy of y and gh of h', with xh = (h' - mu) r and q = gy w:
+ *   t  = gh + r (q - mean q - xh mean(q xh))      (root mean square: no mean q),
+ *   dh = s t,   dgate = t a,   dw = sum over rows of gy xh,   db = sum of gy,
+ *   df = gate t; where post_norm is set, with fh = (f - mu_f) r_f, p = gate t w_post:
+ *   df = r_f (p - mean p - fh mean(p fh)),   dw_post = sum over rows of gate t fh.
+ * h' is normalised as computed, before it is rounded.  Means, sums and statistics are
+ * float; every output is rounded to nearest even once.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  TURNKL_GATE_NONE = 0,   /* ones; gate is NULL */
+  TURNKL_GATE_VECTOR = 1, /* [width] of param_dtype; its gradient is a sum over rows */
+  TURNKL_GATE_MATRIX = 2, /* [n_rows x width] of dtype */
+} turnkl_gate_kind;
+
+/*
+ * residual       h, [n_rows x width] of residual_dtype, row stride ld_residual (elements,
+ *                >= width), rows of any start.
+ * branch         f, [n_rows x width] of dtype.  residual_dtype is dtype, or
+ *                TURNKL_F32 with bf16 branches.  width is at most
+ *                TURNKL_MAX_NORM_WIDTH.
+ * gate           as gate_kind says; ld_gate is a matrix's row stride.
+ * post_weight, weight, bias   [width] of param_dtype, or NULL (ones, zeros);
+ *                post_weight and post_stats_out only with post_norm.
+ * residual_scale s, finite, used as a float.  kind, eps: as in turnkl_norm_fwd, of
+ *                both norms.
+ * residual_out   h', of residual_dtype; may equal residual with the same row stride.
+ * y              of dtype; may equal branch with the same row stride.
+ * stats_out, post_stats_out   [n_rows x 2] float (mu, r) and (mu_f, r_f), or NULL.
+ * Any other overlap of an output with an input or output is TURNKL_ERR_ALIAS.
+ */
+int turnkl_block_norm_fwd(const void* residual, int64_t ld_residual, int residual_dtype,
+                          const void* branch, int64_t ld_branch, int dtype, int64_t n_rows,
+                          int64_t width, const void* gate, int64_t ld_gate, int gate_kind,
+                          int post_norm, const void* post_weight, const void* weight,
+                          const void* bias, int param_dtype, int kind, double residual_scale,
+                          double eps, void* residual_out, int64_t ld_residual_out, void* y,
+                          int64_t ld_y, float* stats_out, float* post_stats_out,
+                          hipStream_t stream);
+
+/* Bytes of device workspace for turnkl_block_norm_bwd (host; a pure function of its
+ * arguments), 0 for invalid ones (as turnkl_norm_workspace_bytes).  No initialisation;
+ * 256-byte aligned. */
+size_t turnkl_block_norm_workspace_bytes(int64_t n_rows, int64_t width);
+
+/*
+ * grad_y         gy, of dtype.  grad_residual: gh, of residual_dtype, or NULL (zeros).
+ * residual       h', turnkl_block_norm_fwd's residual_out; stats, post_stats: its
+ *                statistics (post_stats only with post_norm).
+ * branch, gate, post_weight, weight, ...   that call's; branch is not read, and may be
+ *                NULL, without a gate and post_norm.
+ * grad_residual_out   dh, of residual_dtype, or NULL; may equal grad_residual with the
+ *                same row stride (in place).
+ * grad_branch_out     df, of dtype, or NULL; may equal grad_y with the same row stride.
+ * grad_gate_out  or NULL: of a matrix dgate of dtype, row stride ld_ggo; of a vector
+ *                [width] float, summed over rows like the next three.
+ * grad_weight, grad_bias, grad_post_weight   [width] float, or NULL; summed in a fixed
+ *                order (the same bits from call to call).  accumulate != 0 adds the sums
+ *                to their contents, 0 overwrites (with zeros when n_rows = 0).
+ * workspace      turnkl_block_norm_workspace_bytes(n_rows, width); may be NULL when no
+ *                sum is asked for.
+ * Any other overlap of an output with an input or output is TURNKL_ERR_ALIAS.
+ */
+int turnkl_block_norm_bwd(const void* grad_y, int64_t ld_gy, const void* grad_residual,
+                          int64_t ld_gr, const void* residual, int64_t ld_residual,
+                          int residual_dtype, const float* stats, const void* branch,
+                          int64_t ld_branch, int dtype, int64_t n_rows, int64_t width,
+                          const void* gate, int64_t ld_gate, int gate_kind, int post_norm,
+                          const void* post_weight, const float* post_stats, const void* weight,
+                          int param_dtype, int kind, double residual_scale,
+                          void* grad_residual_out, int64_t ld_gro, void* grad_branch_out,
+                          int64_t ld_gbo, void* grad_gate_out, int64_t ld_ggo,
+                          float* grad_weight, float* grad_bias, float* grad_post_weight,
+                          int accumulate, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Rows of an embedding table for tokens, and the table's gradient:
  *   y_i  = s E[t_i],      dE[v] (+)= s sum over the tokens i with t_i = v of g_i.
  * Products and sums are float; y and dE are rounded to nearest even once.

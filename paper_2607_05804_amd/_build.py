@@ -8,9 +8,10 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["turnkl_api.hip", "segment.hip", "rowkl.hip", "rowkl_ragged.hip", "rowkl_whole.hip",
-           "rowfwd.hip", "reduce.hip", "topk.hip", "logprobs.hip",
-           "logprobs_bwd.hip", "norm.hip", "output_api.hip", "embed.hip", "boundary_api.hip", "controller.cpp", "diagnostics.cpp"]
+SOURCES = ["block_norm_bf16.hip", "block_norm_f32.hip", "block_norm_mixed.hip", "block_norm.hip",
+           "turnkl_api.hip", "segment.hip", "rowkl.hip", "rowkl_ragged.hip", "rowkl_whole.hip",
+           "rowfwd.hip", "reduce.hip", "topk.hip", "logprobs.hip", "logprobs_bwd.hip", "norm.hip",
+           "output_api.hip", "embed.hip", "boundary_api.hip", "controller.cpp", "diagnostics.cpp"]
 LIB = os.path.join(HERE, "libturnkl.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

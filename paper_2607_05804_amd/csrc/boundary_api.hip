@@ -34,6 +34,42 @@ EmbedLayout embed_layout(int64_t n_tokens, const EmbedShape& s) {
   return L;
 }
 
+// What both directions of the block norm share, apart from their matrices.
+bool block_sizes_ok(int dtype, int residual_dtype, int param_dtype, int kind, int gate_kind, int64_t n_rows,
+                    int64_t width) {
+  return known_dtype(dtype) && known_dtype(residual_dtype) && known_dtype(param_dtype) &&
+         (residual_dtype == dtype || residual_dtype == TURNKL_F32) &&
+         (kind == TURNKL_NORM_LAYER || kind == TURNKL_NORM_RMS) && gate_kind >= TURNKL_GATE_NONE &&
+         gate_kind <= TURNKL_GATE_MATRIX && n_rows >= 0 && n_rows <= 0x7FFFFFFFll && width >= 1 &&
+         width <= TURNKL_MAX_NORM_WIDTH;
+}
+
+bool block_gate_ok(const void* gate, int64_t ld_gate, int gate_kind, int64_t n_rows, int64_t width, size_t es,
+                   size_t ps) {
+  if (gate_kind == TURNKL_GATE_NONE) return !gate;
+  if (gate_kind == TURNKL_GATE_VECTOR) return gate && !misaligned(gate, ps);
+  return n_rows == 0 || rows_ok(gate, ld_gate, width, es);
+}
+
+void block_params(BlockNormParams& p, int dtype, int residual_dtype, int param_dtype, int kind, int gate_kind,
+                  int post_norm, int64_t n_rows, int64_t width, bool bwd) {
+  p.n_rows = (int)n_rows;
+  p.width = (int)width;
+  p.branch_bf16 = dtype == TURNKL_BF16;
+  p.residual_bf16 = residual_dtype == TURNKL_BF16;
+  p.param_bf16 = param_dtype == TURNKL_BF16;
+  p.post = post_norm != 0;
+  p.gate_matrix = gate_kind == TURNKL_GATE_MATRIX;
+  p.rms = kind == TURNKL_NORM_RMS;
+  const int el = p.branch_bf16 && p.residual_bf16 ? 8 : 4;
+  p.ragged = width % el != 0;
+  const BlockShape s = block_norm_shape(n_rows, width, el, bwd, p.post != 0);
+  p.threads = s.threads;
+  p.lanes = s.lanes;
+  p.units = s.units;
+  p.n_groups = s.groups;
+}
+
 bool finite_float(double x) { return x == x && fabs(x) <= FLT_MAX; }
 
 }  // namespace
@@ -127,6 +163,173 @@ int turnkl_embed_bwd(const void* grad_out, int64_t ld_grad, int grad_dtype, int6
   p.table_bf16 = table_dtype == TURNKL_BF16;
   p.accumulate = accumulate != 0;
   return launch_embed_bwd(p, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;
+}
+
+int turnkl_block_norm_fwd(const void* residual, int64_t ld_residual, int residual_dtype,
+                          const void* branch, int64_t ld_branch, int dtype, int64_t n_rows,
+                          int64_t width, const void* gate, int64_t ld_gate, int gate_kind,
+                          int post_norm, const void* post_weight, const void* weight,
+                          const void* bias, int param_dtype, int kind, double residual_scale,
+                          double eps, void* residual_out, int64_t ld_residual_out, void* y,
+                          int64_t ld_y, float* stats_out, float* post_stats_out,
+                          hipStream_t stream) {
+  if (!block_sizes_ok(dtype, residual_dtype, param_dtype, kind, gate_kind, n_rows, width) ||
+      !finite_float(residual_scale) || !(eps >= 0.0) || eps > FLT_MAX)
+    return TURNKL_ERR_INVALID_ARG;
+  const size_t es = elem_size(dtype), rs = elem_size(residual_dtype), ps = elem_size(param_dtype);
+  const size_t w = (size_t)width, n = (size_t)n_rows;
+  if (!block_gate_ok(gate, ld_gate, gate_kind, n_rows, width, es, ps)) return TURNKL_ERR_INVALID_ARG;
+  if (!post_norm && (post_weight || post_stats_out)) return TURNKL_ERR_INVALID_ARG;
+  if (n_rows == 0) return TURNKL_OK;
+  if (!rows_ok(residual, ld_residual, width, rs) || !rows_ok(branch, ld_branch, width, es) ||
+      !rows_ok(residual_out, ld_residual_out, width, rs) || !rows_ok(y, ld_y, width, es))
+    return TURNKL_ERR_INVALID_ARG;
+  if (misaligned(weight, ps) || misaligned(bias, ps) || misaligned(post_weight, ps) ||
+      misaligned(stats_out, 4) || misaligned(post_stats_out, 4))
+    return TURNKL_ERR_INVALID_ARG;
+  const bool over_h = residual_out == residual && ld_residual_out == ld_residual;
+  const bool over_f = y == branch && ld_y == ld_branch;
+  const Region h{residual, matrix_bytes(n_rows, ld_residual, width, rs)};
+  const Region f{branch, matrix_bytes(n_rows, ld_branch, width, es)};
+  const Region g{gate, gate_kind == TURNKL_GATE_MATRIX ? matrix_bytes(n_rows, ld_gate, width, es) : w * ps};
+  const Region out{residual_out, matrix_bytes(n_rows, ld_residual_out, width, rs)};
+  const Region norm{y, matrix_bytes(n_rows, ld_y, width, es)};
+  if (overlaps_any(out.p, out.n, {over_h ? Region{} : h, f}) ||
+      overlaps_any(norm.p, norm.n, {h, over_f ? Region{} : f}))
+    return TURNKL_ERR_ALIAS;
+  if (any_overlap({g, {weight, w * ps}, {bias, w * ps}, {post_weight, w * ps}},
+                  {out, norm, {stats_out, n * 8}, {post_stats_out, n * 8}}) ||
+      any_overlap({h, f}, {{stats_out, n * 8}, {post_stats_out, n * 8}}))
+    return TURNKL_ERR_ALIAS;
+  BlockNormParams p{};
+  block_params(p, dtype, residual_dtype, param_dtype, kind, gate_kind, post_norm, n_rows, width, false);
+  p.residual = residual;
+  p.branch = branch;
+  p.gate = gate;
+  p.weight = weight;
+  p.bias = bias;
+  p.post_weight = post_weight;
+  p.out = residual_out;
+  p.y = y;
+  p.stats = stats_out;
+  p.post_stats = post_stats_out;
+  p.ld_residual = ld_residual;
+  p.ld_branch = ld_branch;
+  p.ld_gate = ld_gate;
+  p.ld_out = ld_residual_out;
+  p.ld_y = ld_y;
+  p.scale = (float)residual_scale;
+  // (rows without variance have an r for every eps but 0)
+  p.eps = eps > 0.0 && (float)eps == 0.0f ? FLT_TRUE_MIN : (float)eps;
+  return launch_block_norm(p, false, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;
+}
+
+size_t turnkl_block_norm_workspace_bytes(int64_t n_rows, int64_t width) {
+  if (n_rows < 0 || n_rows > 0x7FFFFFFFll || width < 1 || width > TURNKL_MAX_NORM_WIDTH) return 0;
+  int most = 0;
+  for (int el : {4, 8})
+    for (bool post : {false, true}) {
+      const int g = block_norm_shape(n_rows, width, el, true, post).groups;
+      most = g > most ? g : most;
+    }
+  return align256((size_t)most * 4 * (size_t)width * sizeof(float));
+}
+
+int turnkl_block_norm_bwd(const void* grad_y, int64_t ld_gy, const void* grad_residual,
+                          int64_t ld_gr, const void* residual, int64_t ld_residual,
+                          int residual_dtype, const float* stats, const void* branch,
+                          int64_t ld_branch, int dtype, int64_t n_rows, int64_t width,
+                          const void* gate, int64_t ld_gate, int gate_kind, int post_norm,
+                          const void* post_weight, const float* post_stats, const void* weight,
+                          int param_dtype, int kind, double residual_scale,
+                          void* grad_residual_out, int64_t ld_gro, void* grad_branch_out,
+                          int64_t ld_gbo, void* grad_gate_out, int64_t ld_ggo,
+                          float* grad_weight, float* grad_bias, float* grad_post_weight,
+                          int accumulate, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  if (!block_sizes_ok(dtype, residual_dtype, param_dtype, kind, gate_kind, n_rows, width) ||
+      !finite_float(residual_scale))
+    return TURNKL_ERR_INVALID_ARG;
+  const size_t es = elem_size(dtype), rs = elem_size(residual_dtype), ps = elem_size(param_dtype);
+  const size_t w = (size_t)width, n = (size_t)n_rows;
+  const bool matrix = gate_kind == TURNKL_GATE_MATRIX, needs_f = post_norm || gate_kind != TURNKL_GATE_NONE;
+  if (!block_gate_ok(gate, ld_gate, gate_kind, n_rows, width, es, ps)) return TURNKL_ERR_INVALID_ARG;
+  if (!post_norm && (post_weight || grad_post_weight)) return TURNKL_ERR_INVALID_ARG;
+  if (gate_kind == TURNKL_GATE_NONE && grad_gate_out) return TURNKL_ERR_INVALID_ARG;
+  float* const gate_sums = matrix ? nullptr : static_cast<float*>(grad_gate_out);
+  if (!grad_residual_out && !grad_branch_out && !grad_gate_out && !grad_weight && !grad_bias && !grad_post_weight)
+    return TURNKL_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (!rows_ok(grad_y, ld_gy, width, es) || !rows_ok(residual, ld_residual, width, rs) || !stats ||
+        (grad_residual && !rows_ok(grad_residual, ld_gr, width, rs)) ||
+        (needs_f && !rows_ok(branch, ld_branch, width, es)) || (post_norm && !post_stats) ||
+        (grad_residual_out && !rows_ok(grad_residual_out, ld_gro, width, rs)) ||
+        (grad_branch_out && !rows_ok(grad_branch_out, ld_gbo, width, es)) ||
+        (matrix && grad_gate_out && !rows_ok(grad_gate_out, ld_ggo, width, es)))
+      return TURNKL_ERR_INVALID_ARG;
+  }
+  if (misaligned(weight, ps) || misaligned(post_weight, ps)) return TURNKL_ERR_INVALID_ARG;
+  for (const void* q : {(const void*)stats, (const void*)post_stats, (const void*)gate_sums,
+                        (const void*)grad_weight, (const void*)grad_bias, (const void*)grad_post_weight})
+    if (misaligned(q, 4)) return TURNKL_ERR_INVALID_ARG;
+  const int sums = (grad_weight ? 1 : 0) | (grad_bias ? 2 : 0) | (grad_post_weight ? 4 : 0) | (gate_sums ? 8 : 0);
+  const size_t need = sums ? turnkl_block_norm_workspace_bytes(n_rows, width) : 0;
+  if (sums) {
+    if (!workspace) return TURNKL_ERR_INVALID_ARG;
+    if (misaligned(workspace, 256) || workspace_bytes < need) return TURNKL_ERR_WORKSPACE;
+  }
+  const Region gy{n ? grad_y : nullptr, matrix_bytes(n_rows, ld_gy, width, es)};
+  const Region gr{n ? grad_residual : nullptr, matrix_bytes(n_rows, ld_gr, width, rs)};
+  const Region h{n ? residual : nullptr, matrix_bytes(n_rows, ld_residual, width, rs)};
+  const Region f{n && needs_f ? branch : nullptr, matrix_bytes(n_rows, ld_branch, width, es)};
+  const Region g{matrix && !n ? nullptr : gate, matrix ? matrix_bytes(n_rows, ld_gate, width, es) : w * ps};
+  const Region gro{n ? grad_residual_out : nullptr, matrix_bytes(n_rows, ld_gro, width, rs)};
+  const Region gbo{n ? grad_branch_out : nullptr, matrix_bytes(n_rows, ld_gbo, width, es)};
+  const Region ggo{n && matrix ? grad_gate_out : nullptr, matrix_bytes(n_rows, ld_ggo, width, es)};
+  const bool over_r = grad_residual_out && grad_residual_out == grad_residual && ld_gro == ld_gr;
+  const bool over_y = grad_branch_out && grad_branch_out == grad_y && ld_gbo == ld_gy;
+  const Region none{};
+  if ((gro.p && overlaps_any(gro.p, gro.n, {gy, over_r ? none : gr, h, f, g})) ||
+      (gbo.p && overlaps_any(gbo.p, gbo.n, {over_y ? none : gy, gr, h, f, g})) ||
+      (ggo.p && overlaps_any(ggo.p, ggo.n, {gy, gr, h, f, g})))
+    return TURNKL_ERR_ALIAS;
+  if (any_overlap({{weight, w * ps}, {post_weight, w * ps}, {stats, n * 8}, {post_stats, post_norm ? n * 8 : 0}},
+                  {gro, gbo, ggo, {grad_weight, w * 4}, {grad_bias, w * 4}, {grad_post_weight, w * 4},
+                   {gate_sums, w * 4}, {workspace, need}}) ||
+      any_overlap({gy, gr, h, f, g}, {{grad_weight, w * 4}, {grad_bias, w * 4}, {grad_post_weight, w * 4},
+                                      {gate_sums, w * 4}, {workspace, need}}))
+    return TURNKL_ERR_ALIAS;
+  BlockNormParams p{};
+  block_params(p, dtype, residual_dtype, param_dtype, kind, gate_kind, post_norm, n_rows, width, true);
+  p.residual = residual;
+  p.branch = needs_f ? branch : nullptr;
+  p.gate = gate;
+  p.weight = weight;
+  p.post_weight = post_weight;
+  p.grad_y = grad_y;
+  p.grad_h = grad_residual;
+  p.out = grad_residual_out;
+  p.grad_branch = grad_branch_out;
+  p.grad_gate = matrix ? grad_gate_out : nullptr;
+  p.stats = const_cast<float*>(stats);  // read only
+  p.post_stats = const_cast<float*>(post_stats);
+  p.part = sums ? static_cast<float*>(workspace) : nullptr;
+  p.gw = grad_weight;
+  p.gbias = grad_bias;
+  p.gpost = grad_post_weight;
+  p.ggate = gate_sums;
+  p.sums = sums;
+  p.ld_residual = ld_residual;
+  p.ld_branch = ld_branch;
+  p.ld_gate = ld_gate;
+  p.ld_gy = ld_gy;
+  p.ld_gh = ld_gr;
+  p.ld_out = ld_gro;
+  p.ld_gb = ld_gbo;
+  p.ld_gg = ld_ggo;
+  p.scale = (float)residual_scale;
+  p.accumulate = accumulate != 0;
+  return launch_block_norm(p, true, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;
 }
 
 }  // extern "C"

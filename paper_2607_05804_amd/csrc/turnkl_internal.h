@@ -542,6 +542,57 @@ EmbedShape embed_shape(long long n, long long vocab, long long width);
 hipError_t launch_embed(const EmbedParams& p, hipStream_t s);
 hipError_t launch_embed_bwd(const EmbedGradParams& p, hipStream_t s);
 
+// Norms on either side of a block (block_norm.h), forward and backward.
+struct BlockNormParams {
+  const void* residual;  // forward: h; backward: h'
+  const void* branch;    // f (backward: null where it is not needed)
+  const void* gate;      // vector of parameters, matrix (gate_matrix), or null: ones
+  const void* weight;    // vectors of parameters, or null: ones, zeros
+  const void* bias;
+  const void* post_weight;
+  const void* grad_y;    // backward
+  const void* grad_h;    // or null: zeros
+  void* out;             // forward: h'; backward: the gradient of h, or null
+  void* y;               // forward
+  void* grad_branch;     // backward, or null
+  void* grad_gate;       // of a gate that is a matrix, or null
+  float* stats;          // forward: output or null; backward: input
+  float* post_stats;
+  float* part;           // backward: [n_groups][4][width] partial sums, or null
+  float* gw;             // sums: of the weight, the bias, the branch's weight, the gate; or null
+  float* gbias;
+  float* gpost;
+  float* ggate;
+  long long ld_residual, ld_branch, ld_gate, ld_gy, ld_gh, ld_out, ld_y, ld_gb, ld_gg;
+  int n_rows;
+  int width;
+  int n_groups;   // workgroups over the rows
+  int threads;    // of each
+  int lanes;      // of a row that shares a wave, or 0
+  int units;      // of a thread
+  int sums;       // a bit for each of the sums asked for
+  float scale;    // of the residual
+  float eps;
+  int branch_bf16;
+  int residual_bf16;
+  int param_bf16;
+  int post;        // the branch is normalised
+  int gate_matrix;
+  int rms;
+  int ragged;      // rows of any start and length
+  int accumulate;
+};
+
+struct BlockShape {
+  int threads, lanes, units, groups;
+};
+
+BlockShape block_norm_shape(long long n_rows, long long width, int el, bool bwd, bool post);
+hipError_t launch_block_norm(const BlockNormParams& p, bool bwd, hipStream_t s);
+hipError_t launch_block_norm_bf16(const BlockNormParams& p, bool bwd, hipStream_t s);
+hipError_t launch_block_norm_f32(const BlockNormParams& p, bool bwd, hipStream_t s);
+hipError_t launch_block_norm_mixed(const BlockNormParams& p, bool bwd, hipStream_t s);
+
 // status_out: optional device int32 that receives the call's status
 // (TURNKL_OK or the device-detected error) once the loss is written.
 hipError_t launch_reduce(const SegParams& p, const Ws& ws, const float* kl, double alpha,

@@ -43,6 +43,10 @@ MAX_ALTERNATIVES = 128
 # Kinds of normalisation (turnkl_norm_kind).
 NORM_LAYER = 0
 NORM_RMS = 1
+# Kinds of a block's gate (turnkl_gate_kind).
+GATE_NONE = 0
+GATE_VECTOR = 1
+GATE_MATRIX = 2
 
 # Names of every entry point include/turnkl.h declares.
 EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
@@ -53,7 +57,8 @@ EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
            "turnkl_outcome_gap", "turnkl_token_logprobs_workspace_bytes",
            "turnkl_token_logprobs", "turnkl_token_logprobs_bwd", "turnkl_norm_fwd",
            "turnkl_norm_workspace_bytes", "turnkl_norm_bwd", "turnkl_embed_fwd",
-           "turnkl_embed_workspace_bytes", "turnkl_embed_bwd")
+           "turnkl_embed_workspace_bytes", "turnkl_embed_bwd", "turnkl_block_norm_fwd",
+           "turnkl_block_norm_workspace_bytes", "turnkl_block_norm_bwd")
 # ... and every entry point include/turnkl_testing.h declares (measurement and
 # test hooks).
 TESTING_EXPORTS = ("turnkl_profile_row_kernel", "turnkl_set_row_tiling",
@@ -205,6 +210,17 @@ def lib() -> ctypes.CDLL:
         l.turnkl_embed_bwd.argtypes = [
             c.c_void_p, c.c_int64, c.c_int, c.c_int64, c.c_int64, c.c_void_p, c.c_void_p, c.c_int64,
             c.c_double, c.c_void_p, c.c_int64, c.c_int, c.c_int, c.c_void_p, c.c_size_t, c.c_void_p]
+        p, i = c.c_void_p, c.c_int64
+        l.turnkl_block_norm_fwd.restype = c.c_int
+        l.turnkl_block_norm_fwd.argtypes = [
+            p, i, c.c_int, p, i, c.c_int, i, i, p, i, c.c_int, c.c_int, p, p, p, c.c_int, c.c_int,
+            c.c_double, c.c_double, p, i, p, i, p, p, p]
+        l.turnkl_block_norm_workspace_bytes.restype = c.c_size_t
+        l.turnkl_block_norm_workspace_bytes.argtypes = [i, i]
+        l.turnkl_block_norm_bwd.restype = c.c_int
+        l.turnkl_block_norm_bwd.argtypes = [
+            p, i, p, i, p, i, c.c_int, p, p, i, c.c_int, i, i, p, i, c.c_int, c.c_int, p, p, p, c.c_int,
+            c.c_int, c.c_double, p, i, p, i, p, i, p, p, p, c.c_int, p, c.c_size_t, p]
         _lib = l
     return _lib
 
@@ -898,6 +914,168 @@ def norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None,
     if rc != OK:
         raise TurnKLError(rc, "turnkl_norm_bwd")
     return grad_x, grad_weight, grad_bias
+
+
+class BlockNorm(NamedTuple):
+    """Outputs of block_norm_fwd."""
+    residual: torch.Tensor           # [N, D] of the residual stream's type, h'
+    y: torch.Tensor                  # [N, D] of the branch's type
+    stats: torch.Tensor | None       # float32 [N, 2], (mean, 1 / standard deviation) of h'
+    post_stats: torch.Tensor | None  # float32 [N, 2], the same of the branch (post_norm)
+
+
+class BlockNormGrads(NamedTuple):
+    """Gradients that block_norm_bwd writes (None: not asked for)."""
+    residual: torch.Tensor | None     # [N, D] of the residual stream's type
+    branch: torch.Tensor | None       # [N, D] of the branch's type
+    gate: torch.Tensor | None         # of a matrix [N, D] of its type, of a vector float32 [D]
+    weight: torch.Tensor | None       # float32 [D]
+    bias: torch.Tensor | None         # float32 [D]
+    post_weight: torch.Tensor | None  # float32 [D]
+
+
+class BlockNormWorkspace(_Scratch):
+    """Caller-owned device scratch for turnkl_block_norm_bwd of up to n_rows rows."""
+
+    def __init__(self, n_rows: int, width: int, device="cuda"):
+        super().__init__(int(lib().turnkl_block_norm_workspace_bytes(n_rows, width)),
+                         "turnkl_block_norm_workspace_bytes", device)
+
+
+def new_block_norm_grads(n_rows: int, width: int, dtype=torch.bfloat16, residual_dtype=None, *,
+                         gate: str = "none", weight: bool = True, bias: bool = False,
+                         post_weight: bool = False, pad_cols: int = 0, device="cuda") -> BlockNormGrads:
+    """Buffers for block_norm_bwd.  gate: "none", "vector" or "matrix"; pad_cols: columns
+    between the rows of the matrices."""
+    if gate not in ("none", "vector", "matrix"):
+        raise ValueError(gate)
+    matrix = lambda t: torch.empty((n_rows, width + pad_cols), dtype=t, device=device)[:, :width]  # noqa: E731
+    vector = lambda on: torch.empty(width, dtype=torch.float32, device=device) if on else None  # noqa: E731
+    return BlockNormGrads(matrix(residual_dtype or dtype), matrix(dtype),
+                          matrix(dtype) if gate == "matrix" else vector(gate == "vector"),
+                          vector(weight), vector(bias), vector(post_weight))
+
+
+def _block_inputs(residual, branch, gate, post_weight, weight, bias):
+    """What both directions of the block norm take of their inputs."""
+    dt, shape, index = _check_rows(branch, "branch")
+    rt, rshape, rindex = _check_rows(residual, "residual")
+    if rindex != index or rshape != shape:
+        raise ValueError("residual and branch must share a device and shape")
+    n, d = shape
+    pt = None
+    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"),
+                    (gate if gate is not None and gate.dim() == 1 else None, "gate")):
+        if t is None:
+            continue
+        _parameter(t, d, name, index)
+        code = _dtype_code(t)
+        if pt is not None and code != pt:
+            raise TypeError("weight, bias, post_weight and a gate that is a vector must share a dtype")
+        pt = code
+    kind, gate_at, ld_gate = GATE_NONE, None, 0
+    if gate is not None:
+        if gate.dim() == 1:
+            kind, gate_at = GATE_VECTOR, gate.data_ptr()
+        else:
+            _like(gate, dt, index, shape, "gate")
+            kind, (gate_at, ld_gate) = GATE_MATRIX, _matrix(gate, n, d)
+    return dt, rt, dt if pt is None else pt, n, d, index, kind, gate_at, ld_gate
+
+
+def _at(t: torch.Tensor | None):
+    return None if t is None else t.data_ptr()
+
+
+def block_norm_fwd(residual: torch.Tensor, branch: torch.Tensor, weight: torch.Tensor | None = None,
+                   bias: torch.Tensor | None = None, *, gate: torch.Tensor | None = None,
+                   post_norm: bool = False, post_weight: torch.Tensor | None = None,
+                   residual_scale: float = 1.0, rms: bool = False, eps: float = 1e-6,
+                   out: BlockNorm | None = None) -> BlockNorm:
+    """turnkl_block_norm_fwd on the current stream: a block's output joins the residual
+    stream, h' = residual_scale residual + gate branch (with post_norm the branch is
+    normalised first and multiplied by post_weight), and h' is normalised for the next
+    block, y = norm(h') weight + bias.  Layer norms, or (rms) by the root mean square.
+
+    residual: [N, D] bf16 or float32; branch: [N, D] of the same type, or bf16 over a
+    float32 residual; gate: a vector [D] like the weights, a matrix [N, D] like the branch,
+    or None; weight, bias, post_weight: [D] of either type or None; out: buffers to write,
+    whose residual may be the given residual and whose y the branch (in place); its stats
+    may be None.  Returns out.
+    """
+    dt, rt, pt, n, d, index, kind, gate_at, ld_gate = _block_inputs(residual, branch, gate, post_weight,
+                                                                    weight, bias)
+    if out is None:
+        stats = lambda: torch.empty((n, 2), dtype=torch.float32, device=branch.device)  # noqa: E731
+        out = BlockNorm(torch.empty_like(residual), torch.empty_like(branch), stats(),
+                        stats() if post_norm else None)
+    else:
+        _like(out.residual, rt, index, (n, d), "out.residual")
+        _like(out.y, dt, index, (n, d), "out.y")
+    rc = _on(index, lib().turnkl_block_norm_fwd)(
+        *_matrix(residual, n, d), rt, *_matrix(branch, n, d), dt, n, d, gate_at, ld_gate, kind,
+        1 if post_norm else 0, _at(post_weight), _at(weight), _at(bias), pt,
+        NORM_RMS if rms else NORM_LAYER, residual_scale, eps, *_matrix(out.residual, n, d),
+        *_matrix(out.y, n, d), _vector(out.stats, 2 * n, "out.stats", index),
+        _vector(out.post_stats, 2 * n, "out.post_stats", index), _stream(index))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_block_norm_fwd")
+    return out
+
+
+def block_norm_bwd(grad_y: torch.Tensor, grad_residual: torch.Tensor | None, residual: torch.Tensor,
+                   stats: torch.Tensor, branch: torch.Tensor, weight: torch.Tensor | None, *,
+                   gate: torch.Tensor | None = None, post_norm: bool = False,
+                   post_weight: torch.Tensor | None = None, post_stats: torch.Tensor | None = None,
+                   residual_scale: float = 1.0, rms: bool = False, out: BlockNormGrads | None = None,
+                   accumulate: bool = False, workspace: BlockNormWorkspace | None = None) -> BlockNormGrads:
+    """turnkl_block_norm_bwd on the current stream: the gradients of block_norm_fwd's inputs
+    and parameters from those of its y (grad_y) and of its residual (grad_residual; None:
+    zeros).
+
+    residual, stats, post_stats: block_norm_fwd's outputs; branch, weight, gate, ...: its
+    inputs; out: buffers to write (new_block_norm_grads), of which any may be None and whose
+    residual may be grad_residual and branch grad_y (in place), or None for new ones without
+    a bias; accumulate: the sums over rows (weight, bias, post_weight and a vector's gate) are
+    added to their buffers.  Returns out.
+    """
+    dt, rt, pt, n, d, index, kind, gate_at, ld_gate = _block_inputs(residual, branch, gate, post_weight,
+                                                                    weight, None)
+    _like(grad_y, dt, index, (n, d), "grad_y")
+    if grad_residual is not None:
+        _like(grad_residual, rt, index, (n, d), "grad_residual")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs buffers for the sums")
+        out = new_block_norm_grads(n, d, branch.dtype, residual.dtype,
+                                   gate=("none", "vector", "matrix")[kind], post_weight=post_norm,
+                                   device=branch.device)
+    matrices = []
+    for t, code, name in ((out.residual, rt, "out.residual"), (out.branch, dt, "out.branch")):
+        if t is not None:
+            _like(t, code, index, (n, d), name)
+        matrices += (None, 0) if t is None else _matrix(t, n, d)
+    if out.gate is not None and kind == GATE_MATRIX:
+        _like(out.gate, dt, index, (n, d), "out.gate")
+        matrices += _matrix(out.gate, n, d)
+    else:
+        matrices += _vector(out.gate, d, "out.gate", index), 0
+    sums = [_vector(t, d, f"out.{name}", index) for t, name in
+            ((out.weight, "weight"), (out.bias, "bias"), (out.post_weight, "post_weight"))]
+    ws_at, ws_bytes = None, 0
+    if any(s is not None for s in sums) or (out.gate is not None and kind == GATE_VECTOR):
+        if workspace is None:
+            workspace = BlockNormWorkspace(n, d, device=branch.device)
+        ws_at, ws_bytes = _scratch(workspace, index)
+    rc = _on(index, lib().turnkl_block_norm_bwd)(
+        *_matrix(grad_y, n, d), *((None, 0) if grad_residual is None else _matrix(grad_residual, n, d)),
+        *_matrix(residual, n, d), rt, _vector(stats, 2 * n, "stats", index), *_matrix(branch, n, d), dt, n,
+        d, gate_at, ld_gate, kind, 1 if post_norm else 0, _at(post_weight),
+        _vector(post_stats, 2 * n, "post_stats", index), _at(weight), pt, NORM_RMS if rms else NORM_LAYER,
+        residual_scale, *matrices, *sums, 1 if accumulate else 0, ws_at, ws_bytes, _stream(index))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_block_norm_bwd")
+    return out
 
 
 def embed_fwd(table: torch.Tensor, token_ids: torch.Tensor, *, scale: float = 1.0,
