@@ -41,11 +41,12 @@ __device__ inline void block_row_sums(float (&v)[kN], float* lds, int lanes, int
 #pragma unroll
       for (int i = 0; i < kN; ++i) s[(threadIdx.x / kWave) * kN + i] = v[i];
     __syncthreads();
+    // (a lane per wave: one load's latency, not one after the other)
+    const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = s[i];
-    for (int w = 1; w < waves; ++w)
+    for (int i = 0; i < kN; ++i) v[i] = lane < waves ? s[lane * kN + i] : 0.0f;
 #pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] += s[w * kN + i];
+    for (int i = 0; i < kN; ++i) v[i] = wave_sum_dpp(v[i]);
   }
 }
 

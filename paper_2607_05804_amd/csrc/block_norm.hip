@@ -52,11 +52,12 @@ BlockShape block_norm_shape(long long n_rows, long long width, int el, bool bwd,
     s.units = 0;
     s.threads = 512;
   } else {
-    s.units = units <= 512 ? 1 : units <= 1024 ? 2 : 4;
+    s.units = units <= (bwd ? 512 : 256) ? 1 : units <= 1024 ? 2 : 4;
     s.threads = ((units + s.units - 1) / s.units + kWave - 1) / kWave * kWave;
   }
   const int waves = s.threads / kWave;
-  const int fill = 256 * (16 / waves > 1 ? 16 / waves : 1);
+  const int most = (bwd ? el == 8 && post : s.units == 2) ? 12 : 16;  // waves of a CU
+  const int fill = 256 * (most / waves > 1 ? most / waves : 1);
   const long long per = (bwd ? 2 : 1) * (long long)side;
   const long long g = (n_rows + per - 1) / per;
   s.groups = (int)(g < 1 ? 1 : g < fill ? g : fill);
