@@ -72,6 +72,8 @@ typedef enum {
   TURNKL_ERR_OUTCOME = -10,      /* device: outcome flag not constant over a trajectory */
   TURNKL_ERR_SCRATCH = -11,      /* turnkl_fwd_bwd_noalloc: problem larger than its scratch */
   TURNKL_ERR_TOKEN_ID = -12,     /* device: a given token's id outside [0, vocab) */
+  TURNKL_ERR_SAMPLING = -13,     /* device: a row's sampling parameter or random number
+                                    out of range */
 } turnkl_status;
 
 /* Statistics of one turn index t over the supervised tokens at that turn. */
@@ -449,6 +451,64 @@ int turnkl_token_logprobs_bwd(const void* logits, int64_t ld, int dtype, int64_t
                               const float* log_z, const float* entropy, const float* grad_logp,
                               const float* grad_entropy, void* grad_out, int64_t ld_grad,
                               hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A token sampled from each row of logits, from a given random number (a rollout's next
+ * token).  For row i with logits z, M = max_v z_v, temperature T and
+ * w_v = exp((z_v - M) / T), the tokens in descending order of their logits, the lower id
+ * first among equal ones, are cut off one filter after the other:
+ *   top-k   the first k of them;
+ *   top-p   of those the ones before which less than p of those's mass lies;
+ *   min-p   of those the ones with w_v >= min_p (w of the first is 1);
+ *   the first one always stays.
+ * With the support S that is left and q_v = w_v / sum_{S} w, the token is the first v of S,
+ * in the order of ids, with
+ *   sum over S up to v of q > u.
+ * Weights and sums are double, so that the token is the one that exact sums give unless u
+ * lies within about 1e-14 of a border.  A logit of -inf is a forbidden token.
+ * ------------------------------------------------------------------------ */
+
+/* Sampling parameters: numbers for all rows, or device arrays [n_tokens] with one for each
+ * (NULL: the number).  A row with one out of range, or with a random number outside
+ * [0, 1), gets token -1 and NaN, and TURNKL_ERR_SAMPLING is recorded. */
+typedef struct {
+  double temperature; /* T >= 0 and finite, used as a float; 0: the likeliest token */
+  int32_t top_k;      /* <= 0 or >= vocab: no limit */
+  double top_p;       /* >= 0, used as a float; >= 1: no limit, 0: the likeliest token */
+  double min_p;       /* >= 0, used as a float; 0: no limit */
+  const float* row_temperature;
+  const int32_t* row_top_k;
+  const float* row_top_p;
+  const float* row_min_p;
+} turnkl_sampling;
+
+/* Bytes of device workspace for turnkl_sample_tokens (host; a pure function of its
+ * arguments, which does not fall as one of them grows), 0 for invalid ones (n_tokens < 0
+ * or above 2^31 - 1, vocab < 1 or above 2^24).  No initialisation; 256-byte aligned. */
+size_t turnkl_sample_workspace_bytes(int64_t n_tokens, int64_t vocab);
+
+/*
+ * logits         [n_tokens x vocab] of `dtype`, row stride ld (elements, >= vocab), rows
+ *                of any start.
+ * mask           [n_tokens] nonzero: the row is asked for; NULL: every row is.  Rows not
+ *                asked for are never read: token -1, logq 0, logp 0.
+ * sampling       host; NULL: temperature 1, no filter.
+ * uniforms       [n_tokens] double, u in [0, 1).
+ * token_ids_out  [n_tokens] the tokens.  A row of which every logit is -inf has token -1
+ *                and logq = logp = -inf, one that holds +inf or NaN token -1 and NaN.
+ * logq_out       [n_tokens] float, or NULL: ln q of the token, its log probability in the
+ *                distribution it was sampled from.
+ * logp_out       [n_tokens] float, or NULL: its log probability at temperature 1 without
+ *                filters, as turnkl_token_logprobs gives it.
+ * No output may overlap an input or another output (TURNKL_ERR_ALIAS).  Host numbers out
+ * of range are TURNKL_ERR_INVALID_ARG.  The device-side status is read with
+ * turnkl_get_status (of several bad rows the first one decides).
+ */
+int turnkl_sample_tokens(const void* logits, int64_t ld, int dtype, int64_t n_tokens,
+                         int64_t vocab, const uint8_t* mask, const turnkl_sampling* sampling,
+                         const double* uniforms, int32_t* token_ids_out, float* logq_out,
+                         float* logp_out, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Normalisation of the rows that a vocabulary projection turns into logits,

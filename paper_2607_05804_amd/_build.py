@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["block_norm_bf16.hip", "block_norm_f32.hip", "block_norm_mixed.hip", "block_norm.hip",
            "turnkl_api.hip", "segment.hip", "rowkl.hip", "rowkl_ragged.hip", "rowkl_whole.hip",
            "rowfwd.hip", "reduce.hip", "topk.hip", "logprobs.hip", "logprobs_bwd.hip", "norm.hip",
-           "output_api.hip", "embed.hip", "boundary_api.hip", "controller.cpp", "diagnostics.cpp"]
+           "output_api.hip", "sample.hip", "embed.hip", "boundary_api.hip", "controller.cpp", "diagnostics.cpp"]
 LIB = os.path.join(HERE, "libturnkl.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -70,6 +70,28 @@ void block_params(BlockNormParams& p, int dtype, int residual_dtype, int param_d
   p.n_groups = s.groups;
 }
 
+struct SampleLayout {
+  size_t mass, most, sum, unit, total;
+  int n_segs;
+};
+
+bool sample_sizes_ok(int64_t n_tokens, int64_t vocab) {
+  return n_tokens >= 0 && n_tokens <= 0x7FFFFFFFll && vocab >= 1 && vocab <= kMaxLogprobVocab;
+}
+
+SampleLayout sample_layout(int64_t n_tokens, int64_t vocab) {
+  SampleLayout L{};
+  // (rows of any start lie up to 63 elements behind the line their first one is on)
+  L.n_segs = (int)((vocab + 63 + kSampleSegment - 1) / kSampleSegment);
+  const size_t segs = (size_t)n_tokens * L.n_segs;
+  L.mass = align256(sizeof(Header));
+  L.most = align256(L.mass + segs * sizeof(double));
+  L.sum = align256(L.most + segs * sizeof(float));
+  L.unit = align256(L.sum + segs * sizeof(float));
+  L.total = align256(L.unit + segs * 64 * sizeof(unsigned short));
+  return L;
+}
+
 bool finite_float(double x) { return x == x && fabs(x) <= FLT_MAX; }
 
 }  // namespace
@@ -330,6 +352,70 @@ int turnkl_block_norm_bwd(const void* grad_y, int64_t ld_gy, const void* grad_re
   p.scale = (float)residual_scale;
   p.accumulate = accumulate != 0;
   return launch_block_norm(p, true, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;
+}
+
+size_t turnkl_sample_workspace_bytes(int64_t n_tokens, int64_t vocab) {
+  if (!sample_sizes_ok(n_tokens, vocab)) return 0;
+  return sample_layout(n_tokens, vocab).total;
+}
+
+int turnkl_sample_tokens(const void* logits, int64_t ld, int dtype, int64_t n_tokens,
+                         int64_t vocab, const uint8_t* mask, const turnkl_sampling* sampling,
+                         const double* uniforms, int32_t* token_ids_out, float* logq_out,
+                         float* logp_out, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream) {
+  if (!known_dtype(dtype) || !sample_sizes_ok(n_tokens, vocab) || !workspace) return TURNKL_ERR_INVALID_ARG;
+  turnkl_sampling s{};
+  s.temperature = 1.0;
+  s.top_p = 1.0;
+  if (sampling) s = *sampling;
+  if (!s.row_temperature && (!finite_float(s.temperature) || s.temperature < 0.0)) return TURNKL_ERR_INVALID_ARG;
+  if (!s.row_top_p && !(s.top_p >= 0.0)) return TURNKL_ERR_INVALID_ARG;
+  if (!s.row_min_p && !(s.min_p >= 0.0)) return TURNKL_ERR_INVALID_ARG;
+  const size_t es = elem_size(dtype), n = (size_t)n_tokens;
+  if (n_tokens > 0 && (!rows_ok(logits, ld, vocab, es) || !uniforms || !token_ids_out))
+    return TURNKL_ERR_INVALID_ARG;
+  if (misaligned(uniforms, 8)) return TURNKL_ERR_INVALID_ARG;
+  for (const void* q : {(const void*)s.row_temperature, (const void*)s.row_top_k, (const void*)s.row_top_p,
+                        (const void*)s.row_min_p, (const void*)token_ids_out, (const void*)logq_out,
+                        (const void*)logp_out})
+    if (misaligned(q, 4)) return TURNKL_ERR_INVALID_ARG;
+  const SampleLayout L = sample_layout(n_tokens, vocab);
+  if (misaligned(workspace, 256) || workspace_bytes < L.total) return TURNKL_ERR_WORKSPACE;
+  if (n_tokens > 0 &&
+      any_overlap({{logits, matrix_bytes(n_tokens, ld, vocab, es)}, {mask, n}, {uniforms, n * 8},
+                   {s.row_temperature, n * 4}, {s.row_top_k, n * 4}, {s.row_top_p, n * 4}, {s.row_min_p, n * 4}},
+                  {{token_ids_out, n * 4}, {logq_out, n * 4}, {logp_out, n * 4}, {workspace, L.total}}))
+    return TURNKL_ERR_ALIAS;
+  char* const ws = static_cast<char*>(workspace);
+  SampleParams p{};
+  p.z = logits;
+  p.mask = mask;
+  p.u = uniforms;
+  p.row_temperature = s.row_temperature;
+  p.row_top_k = s.row_top_k;
+  p.row_top_p = s.row_top_p;
+  p.row_min_p = s.row_min_p;
+  p.ids = token_ids_out;
+  p.logq = logq_out;
+  p.logp = logp_out;
+  p.hdr = reinterpret_cast<Header*>(ws);
+  p.seg_mass = reinterpret_cast<double*>(ws + L.mass);
+  p.seg_max = reinterpret_cast<float*>(ws + L.most);
+  p.seg_sum = reinterpret_cast<float*>(ws + L.sum);
+  p.unit = reinterpret_cast<unsigned short*>(ws + L.unit);
+  p.ld = ld;
+  p.n_rows = (int)n_tokens;
+  p.vocab = (int)vocab;
+  p.n_segs = L.n_segs;
+  p.top_k = s.top_k;
+  p.temperature = (float)s.temperature;
+  // (beyond a float's range they limit nothing, or everything but the likeliest)
+  p.top_p = (float)(s.top_p < 2.0 ? s.top_p : 2.0);
+  p.min_p = (float)(s.min_p < 2.0 ? s.min_p : 2.0);
+  p.bf16 = dtype == TURNKL_BF16;
+  p.ragged = misaligned(logits, 16) || (vocab * es) % 16 != 0 || (n_tokens > 1 && (ld * es) % 16 != 0);
+  return launch_sample(p, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;
 }
 
 }  // extern "C"

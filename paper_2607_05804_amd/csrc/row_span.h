@@ -38,7 +38,7 @@ struct RowSpan {
 
   // Pack i of the span: the element its load starts at, moved inside the row where
   // the pack sticks out, and which of the loaded elements are its own.
-  __device__ int place(int i, unsigned& bits) const {
+  __device__ __forceinline__ int place(int i, unsigned& bits) const {
     const int e = col + i * kEpv;
     if constexpr (kRagged) {
       const int at = inside_row(e, vocab > kEpv ? vocab - kEpv : 0);
@@ -51,7 +51,7 @@ struct RowSpan {
     }
   }
   // Load at an element that place() gave.
-  __device__ void load(P& x, int at) const {
+  __device__ __forceinline__ void load(P& x, int at) const {
     if constexpr (kRagged) {
       if (vocab < kEpv) {  // a row shorter than a pack: element by element
         if constexpr (kBf16) {

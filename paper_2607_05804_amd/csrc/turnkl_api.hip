@@ -660,6 +660,7 @@ const char* turnkl_status_string(int status) {
     case TURNKL_ERR_SCRATCH:
       return "problem larger than the built-in scratch of turnkl_fwd_bwd_noalloc";
     case TURNKL_ERR_TOKEN_ID: return "a given token's id outside [0, vocab)";
+    case TURNKL_ERR_SAMPLING: return "a row's sampling parameter or random number out of range";
     default: return "unknown status";
   }
 }

@@ -25,6 +25,7 @@ enum : unsigned {
   kPrioTopkId = 4,  // top-K path: a support id outside [0, vocab)
   kPrioOutcome = 5,  // outcome flag not constant over a trajectory
   kPrioTokenId = 6,  // a given token's id outside [0, vocab)
+  kPrioSampling = 7,  // a row's sampling parameter or random number out of range
 };
 
 __host__ __device__ inline unsigned long long err_key(long long pos, unsigned prio) {
@@ -40,6 +41,7 @@ __host__ __device__ inline int status_from_key(unsigned long long key) {
     case kPrioTopkId: return TURNKL_ERR_TOPK_ID;
     case kPrioOutcome: return TURNKL_ERR_OUTCOME;
     case kPrioTokenId: return TURNKL_ERR_TOKEN_ID;
+    case kPrioSampling: return TURNKL_ERR_SAMPLING;
     default: return TURNKL_ERR_SYNC_TIMEOUT;
   }
 }
@@ -592,6 +594,39 @@ hipError_t launch_block_norm(const BlockNormParams& p, bool bwd, hipStream_t s);
 hipError_t launch_block_norm_bf16(const BlockNormParams& p, bool bwd, hipStream_t s);
 hipError_t launch_block_norm_f32(const BlockNormParams& p, bool bwd, hipStream_t s);
 hipError_t launch_block_norm_mixed(const BlockNormParams& p, bool bwd, hipStream_t s);
+
+// Sampled tokens (sample.hip).  A row is cut into n_segs segments.
+struct SampleParams {
+  const void* z;
+  const unsigned char* mask;        // or null: every row
+  const double* u;                  // [n_rows] in [0, 1)
+  const float* row_temperature;     // [n_rows] each, or null: the numbers below
+  const int* row_top_k;
+  const float* row_top_p;
+  const float* row_min_p;
+  int* ids;
+  float* logq;                      // or null, like the next one
+  float* logp;
+  Header* hdr;
+  float* seg_max;                   // [n_rows][n_segs] each
+  float* seg_sum;                   // of exp(z - maximum)
+  double* seg_mass;                 // of exp((z - maximum) / T)
+  unsigned short* unit;             // [n_rows][n_segs][64] orders of lanes' maxima, upper halves
+  long long ld;
+  int n_rows;
+  int vocab;
+  int n_segs;
+  int top_k;
+  float temperature;
+  float top_p;
+  float min_p;
+  int bf16;
+  int ragged;
+};
+
+constexpr int kSampleSegment = 2048;  // elements
+
+hipError_t launch_sample(const SampleParams& p, hipStream_t s);
 
 // status_out: optional device int32 that receives the call's status
 // (TURNKL_OK or the device-detected error) once the loss is written.

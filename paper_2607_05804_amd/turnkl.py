@@ -31,6 +31,7 @@ ERR_TOPK_ID = -9
 ERR_OUTCOME = -10
 ERR_SCRATCH = -11
 ERR_TOKEN_ID = -12
+ERR_SAMPLING = -13
 
 # Size of the scratch array of turnkl_fwd_bwd_noalloc (TURNKL_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -58,7 +59,8 @@ EXPORTS = ("turnkl_workspace_bytes", "turnkl_fwd_bwd", "turnkl_fwd_bwd_noalloc",
            "turnkl_token_logprobs", "turnkl_token_logprobs_bwd", "turnkl_norm_fwd",
            "turnkl_norm_workspace_bytes", "turnkl_norm_bwd", "turnkl_embed_fwd",
            "turnkl_embed_workspace_bytes", "turnkl_embed_bwd", "turnkl_block_norm_fwd",
-           "turnkl_block_norm_workspace_bytes", "turnkl_block_norm_bwd")
+           "turnkl_block_norm_workspace_bytes", "turnkl_block_norm_bwd",
+           "turnkl_sample_workspace_bytes", "turnkl_sample_tokens")
 # ... and every entry point include/turnkl_testing.h declares (measurement and
 # test hooks).
 TESTING_EXPORTS = ("turnkl_profile_row_kernel", "turnkl_set_row_tiling",
@@ -79,6 +81,14 @@ class Options(ctypes.Structure):
     _fields_ = [("support_floor", ctypes.c_int32), ("support_frac", ctypes.c_double),
                 ("success", ctypes.c_void_p), ("outcome_stats_out", ctypes.c_void_p),
                 ("token_weight_out", ctypes.c_void_p), ("token_lse_out", ctypes.c_void_p)]
+
+
+class Sampling(ctypes.Structure):
+    """turnkl_sampling (include/turnkl.h)."""
+    _fields_ = [("temperature", ctypes.c_double), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_double),
+                ("min_p", ctypes.c_double), ("row_temperature", ctypes.c_void_p),
+                ("row_top_k", ctypes.c_void_p), ("row_top_p", ctypes.c_void_p),
+                ("row_min_p", ctypes.c_void_p)]
 
 
 class DepthConfig(ctypes.Structure):
@@ -221,6 +231,11 @@ def lib() -> ctypes.CDLL:
         l.turnkl_block_norm_bwd.argtypes = [
             p, i, p, i, p, i, c.c_int, p, p, i, c.c_int, i, i, p, i, c.c_int, c.c_int, p, p, p, c.c_int,
             c.c_int, c.c_double, p, i, p, i, p, i, p, p, p, c.c_int, p, c.c_size_t, p]
+        l.turnkl_sample_workspace_bytes.restype = c.c_size_t
+        l.turnkl_sample_workspace_bytes.argtypes = [i, i]
+        l.turnkl_sample_tokens.restype = c.c_int
+        l.turnkl_sample_tokens.argtypes = [p, i, c.c_int, i, i, p, c.POINTER(Sampling), p, p, p, p, p,
+                                           c.c_size_t, p]
         _lib = l
     return _lib
 
@@ -816,6 +831,73 @@ def token_logprobs_bwd(logits: torch.Tensor, token_ids: torch.Tensor | None, log
     if rc != OK:
         raise TurnKLError(rc, "turnkl_token_logprobs_bwd")
     return grad
+
+
+class SampledTokens(NamedTuple):
+    """Outputs of sample_tokens, one entry per row (None: not asked for)."""
+    ids: torch.Tensor          # int32 [N]
+    logq: torch.Tensor | None  # float32 [N], ln q of the token where it was sampled from
+    logp: torch.Tensor | None  # float32 [N], its log p at temperature 1 without filters
+
+
+def new_sampled_tokens(n_tokens: int, device="cuda", logp: bool = True) -> SampledTokens:
+    """Output buffers for sample_tokens."""
+    f = dict(dtype=torch.float32, device=device)
+    return SampledTokens(torch.empty(n_tokens, dtype=torch.int32, device=device),
+                         torch.empty(n_tokens, **f), torch.empty(n_tokens, **f) if logp else None)
+
+
+class SampleWorkspace(_StatusScratch):
+    """Caller-owned device scratch for turnkl_sample_tokens of up to n_tokens rows and vocab
+    columns."""
+
+    def __init__(self, n_tokens: int, vocab: int, device="cuda"):
+        super().__init__(int(lib().turnkl_sample_workspace_bytes(n_tokens, vocab)),
+                         "turnkl_sample_workspace_bytes", device)
+
+
+def sample_tokens(logits: torch.Tensor, uniforms: torch.Tensor, *, temperature: float | torch.Tensor = 1.0,
+                  top_k: int | torch.Tensor = 0, top_p: float | torch.Tensor = 1.0,
+                  min_p: float | torch.Tensor = 0.0, mask: torch.Tensor | None = None,
+                  out: SampledTokens | None = None, workspace: SampleWorkspace | None = None,
+                  check: bool = True) -> SampledTokens:
+    """turnkl_sample_tokens on the current stream: a token from each row's distribution at a
+    temperature, cut off by top-k, top-p and min-p in this order, where the running sum of
+    probabilities, in the order of ids, passes the row's random number.
+
+    logits: [N, V] bf16 or float32 of any row stride; uniforms: float64 [N] in [0, 1);
+    temperature (0: the likeliest token), top_k (0: no limit), top_p, min_p: numbers, or
+    float32 (top_k: int32) [N] with one for each row; mask: uint8 [N] or None (rows with 0
+    are not read: id -1); out: buffers to write (new_sampled_tokens), of which logq and logp
+    may be None; check: read the device status once at the end and raise where a row's
+    parameter or random number is out of range.  Returns out.
+    """
+    dt, shape, index = _check_rows(logits, "logits")
+    n, v = shape
+    given = Sampling()
+    for name, x, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(x, torch.Tensor):
+            setattr(given, "row_" + name, _per_row(x, n, name, index, dtype))
+        else:
+            setattr(given, name, x)
+    u_at = _per_row(uniforms, n, "uniforms", index, torch.float64)
+    mask_at = _per_row(mask, n, "mask", index, torch.uint8)
+    if out is None:
+        out = new_sampled_tokens(n, device=logits.device)
+    if workspace is None:
+        workspace = SampleWorkspace(n, v, device=logits.device)
+    rc = _on(index, lib().turnkl_sample_tokens)(
+        *_matrix(logits, n, v), dt, n, v, mask_at, given, u_at,
+        _vector(out.ids, n, "ids", index, torch.int32), _vector(out.logq, n, "logq", index),
+        _vector(out.logp, n, "logp", index), *_scratch(workspace, index), _stream(index))
+    if rc != OK:
+        raise TurnKLError(rc, "turnkl_sample_tokens")
+    if check:
+        st = workspace.status()
+        if st != OK:
+            raise TurnKLError(st, "turnkl_sample_tokens (device)")
+    return out
 
 
 class NormWorkspace(_Scratch):
