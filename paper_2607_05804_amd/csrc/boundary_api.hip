@@ -71,7 +71,7 @@ void block_params(BlockNormParams& p, int dtype, int residual_dtype, int param_d
 }
 
 struct SampleLayout {
-  size_t mass, most, sum, unit, total;
+  size_t mass, most, sum, unit, todo, total;
   int n_segs;
 };
 
@@ -88,7 +88,8 @@ SampleLayout sample_layout(int64_t n_tokens, int64_t vocab) {
   L.most = align256(L.mass + segs * sizeof(double));
   L.sum = align256(L.most + segs * sizeof(float));
   L.unit = align256(L.sum + segs * sizeof(float));
-  L.total = align256(L.unit + segs * 64 * sizeof(unsigned short));
+  L.todo = align256(L.unit + segs * 64 * sizeof(unsigned short));
+  L.total = align256(L.todo + (size_t)n_tokens);
   return L;
 }
 
@@ -404,6 +405,7 @@ int turnkl_sample_tokens(const void* logits, int64_t ld, int dtype, int64_t n_to
   p.seg_max = reinterpret_cast<float*>(ws + L.most);
   p.seg_sum = reinterpret_cast<float*>(ws + L.sum);
   p.unit = reinterpret_cast<unsigned short*>(ws + L.unit);
+  p.todo = reinterpret_cast<unsigned char*>(ws + L.todo);
   p.ld = ld;
   p.n_rows = (int)n_tokens;
   p.vocab = (int)vocab;
@@ -413,6 +415,8 @@ int turnkl_sample_tokens(const void* logits, int64_t ld, int dtype, int64_t n_to
   // (beyond a float's range they limit nothing, or everything but the likeliest)
   p.top_p = (float)(s.top_p < 2.0 ? s.top_p : 2.0);
   p.min_p = (float)(s.min_p < 2.0 ? s.min_p : 2.0);
+  p.any_filter = s.row_temperature || s.row_top_k || s.row_top_p || s.row_min_p || p.top_k > 0 || p.top_p < 1.0f ||
+                 p.min_p > 0.0f || p.temperature == 0.0f;
   p.bf16 = dtype == TURNKL_BF16;
   p.ragged = misaligned(logits, 16) || (vocab * es) % 16 != 0 || (n_tokens > 1 && (ld * es) % 16 != 0);
   return launch_sample(p, stream) == hipSuccess ? TURNKL_OK : TURNKL_ERR_HIP;

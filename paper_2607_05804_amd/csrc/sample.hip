@@ -9,16 +9,19 @@
 // weights and sums have 64 bits: with 32, where a row is flat, one row in a hundred would
 // get a neighbour of its token.
 //
-// Two kernels.  sample_scan goes over the logits once: a wave takes a segment of 2,048
-// elements and leaves its maximum and, where the row's filters need the mass of the whole
-// row, its sum of weights; of rows with a filter also the largest of every lane's 32
-// elements (a unit), by its upper 16 bits.  sample_pick joins a row's segments, a workgroup
-// a row.  Without a filter it looks for the segment where the running sum passes the bound
-// and reads that one again.  With one it needs the elements at the top of the row only: the
-// n-th largest unit maximum is a bound that at least n elements reach, and only units that
-// reach it are read again.  Up to 512 such elements are ranked against each other; up to
-// 4,096 the borders of the support are found bit by bit; where more are needed (flat rows,
-// long runs of equal logits) the same goes over the row itself.
+// sample_scan goes over the logits once: a wave takes a segment of 2,048 elements and leaves
+// its maximum and, where the row's filters need the mass of the whole row, its sum of
+// weights; of rows with a filter also the largest of every lane's 32 elements (a unit), by
+// its upper 16 bits.  sample_pick joins a row's segments, a workgroup a row.  Without a
+// filter it looks for the segment where the running sum passes the bound and reads that one
+// again.  With one it needs the elements at the top of the row only: the n-th largest unit
+// maximum is a bound that at least n elements reach, units that reach it are read again, and
+// up to 1,024 such elements are ranked against each other.  Where that is not enough (flat
+// rows, long runs of equal logits) a histogram over the row shows between which logits the
+// border lies, the mass above them is summed exactly, and the border is found bit by bit
+// among the elements between them.
+
+#include <type_traits>
 
 #include "row_span.h"
 
@@ -30,11 +33,15 @@ constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kSegElems = kSampleSegment;
 constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / kWave;
-constexpr int kRanked = 512;     // candidates that are ranked against each other
-constexpr int kListed = 4096;    // candidates that LDS holds
-constexpr int kUnitsHeld = 2048; // units that are read again
-constexpr int kFirstWant = 200;  // elements that are asked for where only top-p limits a row,
-constexpr int kMoreWant = 2400;  // and where those do not hold enough
+constexpr int kRankEach = 2;                           // of a thread
+constexpr int kRanked = kRankEach * kPickThreads;      // candidates that are ranked against each other
+constexpr int kRankPad = 8;
+constexpr int kUnitsHeld = 2048;  // units that are read again, at most
+constexpr int kUnitEach = 16;     // units of a thread that its registers hold
+constexpr int kWantByMass = 500;  // elements that are asked for where only top-p limits a row
+constexpr int kBins = 2 * kPickThreads;                // of the histogram
+constexpr int kBinEach = 8;                            // elements of a lane between two bins' edges
+constexpr int kBinHeld = kBinEach * kWave;             // of a wave
 
 // The logit's bits in an order of unsigned numbers (-0 and +0 alike, NaN as -inf).
 __device__ inline unsigned order_of(float z) {
@@ -45,27 +52,39 @@ __device__ inline float logit_of(unsigned o) {
   return __uint_as_float(o ^ ((unsigned)((int)~o >> 31) | 0x80000000u));
 }
 constexpr unsigned kNothing = 0x007FFFFFu;  // the order of -inf
+constexpr double kLog2e64 = 1.4426950408889634074;
+constexpr double kLn264 = 0.69314718055994530942;
 
-// 2^x for x <= 0, from the series of exp around 0 in 64 bits: on [-1/2, 1/2] its remainder
-// past the twelfth power is below 2e-16.
+// 2^r on [-1/2, 1/2]: a polynomial through 2^r at eleven Chebyshev points and 0, where it is
+// exact; elsewhere it is off by 2e-17.
+__device__ __forceinline__ double pow2_fraction(double r) {
+  double s = 4.4549794711760616e-10;
+  s = fma(s, r, 7.072621356539349e-09);
+  s = fma(s, r, 1.0178062351388103e-07);
+  s = fma(s, r, 1.3215442410711872e-06);
+  s = fma(s, r, 1.525273382999124e-05);
+  s = fma(s, r, 0.0001540353044202707);
+  s = fma(s, r, 0.0013333558146416842);
+  s = fma(s, r, 0.009618129107606715);
+  s = fma(s, r, 0.0555041086648216);
+  s = fma(s, r, 0.24022650695910097);
+  s = fma(s, r, 0.6931471805599453);
+  return fma(s, r, 1.0);
+}
+// 2^x for x <= 0
 __device__ __forceinline__ double pow2(double x) {
   x = fmax(x, -1100.0);  // 0 from there on, -inf included
   const double n = rint(x);
-  const double r = (x - n) * 0.69314718055994530942;
-  double s = 1.0 / 479001600.0;
-  s = fma(s, r, 1.0 / 39916800.0);
-  s = fma(s, r, 1.0 / 3628800.0);
-  s = fma(s, r, 1.0 / 362880.0);
-  s = fma(s, r, 1.0 / 40320.0);
-  s = fma(s, r, 1.0 / 5040.0);
-  s = fma(s, r, 1.0 / 720.0);
-  s = fma(s, r, 1.0 / 120.0);
-  s = fma(s, r, 1.0 / 24.0);
-  s = fma(s, r, 1.0 / 6.0);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.0);
-  s = fma(s, r, 1.0);
-  return ldexp(s, (int)n);
+  return ldexp(pow2_fraction(x - n), (int)n);
+}
+// the same for -1020 <= x <= 0: x's integer part comes out of an addition that leaves no
+// bits for a fraction, in the sum's low word, and goes straight into the exponent
+__device__ __forceinline__ double pow2_tame(double x) {
+  const double kRound = 6755399441055744.0;  // 1.5 2^52
+  const double t = x + kRound;
+  const double f = pow2_fraction(x - (t - kRound));
+  const int hi = __double2hiint(f) + (__double2loint(t) << 20);
+  return __hiloint2double(hi, __double2loint(f));
 }
 
 // What a row's parameters ask for.
@@ -85,7 +104,7 @@ __device__ inline Plan plan_of(const SampleParams& s, long long row) {
   Plan a;
   a.bad = !(t >= 0.0f && t < INFINITY) || !(p >= 0.0f) || !(m >= 0.0f);
   const bool first = t == 0.0f || p == 0.0f;  // the likeliest one alone
-  a.rate = 1.4426950408889634074 / (t == 0.0f ? 1.0 : (double)t);
+  a.rate = kLog2e64 / (t == 0.0f ? 1.0 : (double)t);
   a.k = first ? 1 : k <= 0 || k >= s.vocab ? 0 : k;
   a.p = first ? 1.0f : fminf(p, 1.0f);
   a.min_p = first ? 0.0f : fminf(m, 1.0f);
@@ -128,6 +147,13 @@ __device__ __forceinline__ double wave_sum64(double v) {
   return v;
 }
 
+// The largest of three, NaN where one is.
+__device__ __forceinline__ float most3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
+// Bound: the 64-bit exponentials, some twenty operations an element (they run at the rate
+// of 32-bit ones here); HBM where only top-k or min-p limit the rows.
 template <bool kBf16, bool kRagged>
 __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
   using R = Row<kBf16, kRagged>;
@@ -147,131 +173,197 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
     int at[R::kPacks];
     unsigned bits[R::kPacks];
     r.load(g, x, at, bits);
-    auto value = [&](int q, int j) { return (bits[q] >> j) & 1u ? x[q].get(j) : -INFINITY; };
-    float best = -INFINITY;
-    bool none = false;  // whether one is no number
+    auto sums = [&](auto edge) {
+      constexpr bool kEdge = decltype(edge)::value;
+      auto value = [&](int q, int j) {
+        return !kEdge || ((bits[q] >> j) & 1u) ? x[q].get(j) : -INFINITY;
+      };
+      float best = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < R::kPacks; ++q)
+      for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
-      for (int j = 0; j < R::kEpv; ++j) {
-        const float z = value(q, j);
-        none = none || z != z;
-        best = fmaxf(best, z);
+        for (int j = 0; j < R::kEpv; j += 2) best = most3(best, value(q, j), value(q, j + 1));
+        x[q].fence();
       }
-    if (plan.filtered) p.unit[task * kWave + lane] = (unsigned short)(order_of(best) >> 16);
-    const float m = __any(none) ? __builtin_nanf("") : wave_max_dpp(best);
-    double mass = 0.0;
-    float sum = 0.0f;
-    const bool numbers = fabsf(m) < INFINITY;
-    if (plan.mass && numbers) {
+      const bool none = __any(best != best);  // one is no number
+      if (plan.filtered) p.unit[task * kWave + lane] = (unsigned short)(order_of(best) >> 16);
+      const float m = none ? __builtin_nanf("") : wave_max_dpp(best);
+      double mass = 0.0;
+      float sum = 0.0f;
+      const bool numbers = fabsf(m) < INFINITY;
+      if (plan.mass && numbers) {
+        const double shift = -(double)m * plan.rate;
+        if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0) {
+          // x = z rate - m rate: the product of the maximum is rounded (1e-13 at most, the
+          // same for the whole segment).  Nothing below 2^-1000 counts, nor does it here.
+          const float low = (float)((double)m - 1000.0 / plan.rate);
 #pragma unroll
-      for (int q = 0; q < R::kPacks; ++q)
+          for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
-        for (int j = 0; j < R::kEpv; ++j) mass += pow2(((double)value(q, j) - (double)m) * plan.rate);
-      mass = wave_sum64(mass);
-    }
-    if (p.logp && numbers) {
+            for (int j = 0; j < R::kEpv; ++j) {
+              mass += pow2_tame(fma((double)fmaxf(value(q, j), low), plan.rate, shift));
+              if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // not all 64-bit numbers at once
+            }
+            x[q].fence();
+          }
+        } else {
 #pragma unroll
-      for (int q = 0; q < R::kPacks; ++q)
+          for (int q = 0; q < R::kPacks; ++q)
 #pragma unroll
-        for (int j = 0; j < R::kEpv; ++j) sum += exp2_fast((value(q, j) - m) * kLog2e);
-      sum = wave_sum_dpp(sum);
-    }
-    if (lane == 0) {
-      p.seg_max[task] = m;
-      p.seg_sum[task] = sum;
-      p.seg_mass[task] = mass;
-    }
+            for (int j = 0; j < R::kEpv; ++j) {
+              mass += pow2(((double)value(q, j) - (double)m) * plan.rate);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        mass = wave_sum64(mass);
+      }
+      if (p.logp && numbers && !(plan.mass && plan.rate == kLog2e64)) {
+#pragma unroll
+        for (int q = 0; q < R::kPacks; ++q)
+#pragma unroll
+          for (int j = 0; j < R::kEpv; ++j) sum += exp2_fast((value(q, j) - m) * kLog2e);
+        sum = wave_sum_dpp(sum);
+      }
+      if (lane == 0) {
+        p.seg_max[task] = m;
+        p.seg_sum[task] = sum;
+        p.seg_mass[task] = mass;
+      }
+    };
+    const int first = g * kSegElems - r.pre;
+    if (first >= 0 && first + kSegElems <= p.vocab) sums(std::false_type{});
+    else sums(std::true_type{});
   }
 }
 
 // ---------------------------------------------------------------------------
 // picking
 
-// A workgroup's sums and scans in a fixed order; each has two barriers, after the second
-// of which `lds` may be used again.
+// A workgroup's sums and scans in a fixed order, through LDS that alternates between two
+// halves: one barrier each.
 struct Group {
-  double* lds;  // LDS, kPickWaves
-  int* ilds;    // LDS, kPickWaves
+  double (*lds)[kPickWaves * 3];  // LDS, two of them
+  int (*ilds)[kPickWaves * 3];
+  int turn = 0;
 
-  __device__ __forceinline__ double sum(double v) const {
-    v = wave_sum64(v);
-    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = v;
-    __syncthreads();
-    double s = lds[0];
+  template <int kN>
+  __device__ __forceinline__ void sums(double (&v)[kN]) {
+    turn ^= 1;
 #pragma unroll
-    for (int w = 1; w < kPickWaves; ++w) s += lds[w];
+    for (int i = 0; i < kN; ++i) v[i] = wave_sum64(v[i]);
+    if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) lds[turn][threadIdx.x / kWave * kN + i] = v[i];
     __syncthreads();
-    return s;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      v[i] = lds[turn][i];
+#pragma unroll
+      for (int w = 1; w < kPickWaves; ++w) v[i] += lds[turn][w * kN + i];
+    }
   }
-  // the sum of the threads before this one and itself; *total: of all
-  __device__ __forceinline__ double scan(double v, double* total) const {
+  template <int kN>
+  __device__ __forceinline__ void sums(int (&v)[kN]) {
+    turn ^= 1;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) wave_exclusive_dpp(v[i], &v[i]);
+    if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) ilds[turn][threadIdx.x / kWave * kN + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      v[i] = ilds[turn][i];
+#pragma unroll
+      for (int w = 1; w < kPickWaves; ++w) v[i] += ilds[turn][w * kN + i];
+    }
+  }
+  template <typename V>
+  __device__ __forceinline__ V sum(V v) {
+    V one[1] = {v};
+    sums(one);
+    return one[0];
+  }
+  // the sum of the threads up to and with this one; *total: of all
+  __device__ __forceinline__ double scan(double v, double* total) {
+    turn ^= 1;
     const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const double u = __shfl_up(v, o, kWave);
       if (lane >= o) v += u;
     }
-    if (lane == kWave - 1) lds[wid] = v;
+    if (lane == kWave - 1) lds[turn][wid] = v;
     __syncthreads();
     double before = 0.0, all = 0.0;
 #pragma unroll
     for (int w = 0; w < kPickWaves; ++w) {
-      const double s = lds[w];
+      const double s = lds[turn][w];
       before += w < wid ? s : 0.0;
       all += s;
     }
-    __syncthreads();
     *total = all;
     return before + v;
   }
-  __device__ __forceinline__ int scan(int v, int* total) const {  // of the threads before this one
-    return block_exclusive_scan<kPickThreads>(v, ilds, total);
+  // the sum of the threads before this one
+  __device__ __forceinline__ int scan(int v, int* total) {
+    turn ^= 1;
+    const int wid = threadIdx.x / kWave;
+    int all_wave;
+    const int mine = wave_exclusive_dpp(v, &all_wave);
+    if ((threadIdx.x & (kWave - 1)) == 0) ilds[turn][wid] = all_wave;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) {
+      const int s = ilds[turn][w];
+      before += w < wid ? s : 0;
+      all += s;
+    }
+    *total = all;
+    return before + mine;
   }
-  __device__ __forceinline__ int sum(int v) const {
-    int all;
-    block_exclusive_scan<kPickThreads>(v, ilds, &all);
-    return all;
-  }
-  __device__ __forceinline__ int largest(int v) const {
+  __device__ __forceinline__ int largest(int v) {
+    turn ^= 1;
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) {
       const int u = __shfl_xor(v, o, kWave);
       v = u > v ? u : v;
     }
-    if ((threadIdx.x & (kWave - 1)) == 0) ilds[threadIdx.x / kWave] = v;
+    if ((threadIdx.x & (kWave - 1)) == 0) ilds[turn][threadIdx.x / kWave] = v;
     __syncthreads();
-    int m = ilds[0];
+    int m = ilds[turn][0];
 #pragma unroll
-    for (int w = 1; w < kPickWaves; ++w) m = ilds[w] > m ? ilds[w] : m;
-    __syncthreads();
+    for (int w = 1; w < kPickWaves; ++w) m = ilds[turn][w] > m ? ilds[turn][w] : m;
     return m;
   }
 };
+// orders as signed numbers of the same order
+__device__ __forceinline__ int signed_order(unsigned o) { return (int)(o ^ 0x80000000u); }
+__device__ __forceinline__ unsigned unsigned_order(int o) { return (unsigned)o ^ 0x80000000u; }
 
-// The border of a support: orders above `order`, and at it ids up to `id`.
+// Where a support ends: orders above `order`, and at it ids up to `id`.
 struct Border {
   unsigned order;
   int id;
 };
 
-// A row being picked from.
+// A row being picked from.  All threads of the workgroup call every function.
 template <bool kBf16, bool kRagged>
 struct Pick {
   using R = Row<kBf16, kRagged>;
   const SampleParams& p;
   const R row;
   const Plan plan;
-  const Group group;
+  Group& group;
   const long long first;  // segment
   float m;                // M
-  int* found;             // LDS
-  double* held;           // LDS
-  unsigned long long* list;  // LDS, kListed
+  int* found;             // LDS, 4
+  double* held;           // LDS, 1 + kPickWaves
 
   __device__ __forceinline__ double weight(float z) const { return pow2(((double)z - (double)m) * plan.rate); }
 
-  // Hands every own element of segment g to use(value, id).
+  // Hands the elements of segment g to use(value, id, whether it is an own one) in all lanes.
   template <typename F>
   __device__ __forceinline__ void each_of(int g, F use) const {
     typename R::P x[R::kPacks];
@@ -281,25 +373,26 @@ struct Pick {
 #pragma unroll
     for (int q = 0; q < R::kPacks; ++q)
 #pragma unroll
-      for (int j = 0; j < R::kEpv; ++j)
-        if ((bits[q] >> j) & 1u) use(x[q].get(j), at[q] + j);
+      for (int j = 0; j < R::kEpv; ++j) {
+        use(x[q].get(j), at[q] + j, ((bits[q] >> j) & 1u) != 0);
+        if (j % 2 == 1) __builtin_amdgcn_sched_barrier(0);  // not all elements' 64-bit numbers at once
+      }
   }
   // The same for all segments whose maximum reaches `least`, a wave each in turn.
   template <typename F>
   __device__ __forceinline__ void each(unsigned least, F use) const {
-    for (int g = threadIdx.x / kWave; g < p.n_segs; g += kPickWaves)
+    for (int g = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); g < p.n_segs; g += kPickWaves)
       if (order_of(p.seg_max[first + g]) >= least) each_of(g, use);
   }
 
-  // The first id where the running sum of weight(z) over kept elements passes target x
-  // total, when a segment's share is share(g) (and each segment's elements are weighed
-  // again); *total: of all shares.
-  template <typename Share, typename Keep>
-  __device__ __forceinline__ int by_segment(double u, Share share, Keep keep, double* total) const {
+  // The first id where the running sum of value(z, id) passes target_of(total), when a
+  // segment's share of it is share(g); *total: of all shares.
+  template <typename Target, typename Share, typename Value>
+  __device__ __forceinline__ int by_segment(Target target_of, Share share, Value value, double* total) {
     // a run of segments a thread, so that the threads are in the order of ids
-    const int each_run = (p.n_segs + kPickThreads - 1) / kPickThreads;
-    const int lo = threadIdx.x * each_run;
-    const int hi = lo + each_run < p.n_segs ? lo + each_run : p.n_segs;
+    const int run_of = (p.n_segs + kPickThreads - 1) / kPickThreads;
+    const int lo = threadIdx.x * run_of;
+    const int hi = lo + run_of < p.n_segs ? lo + run_of : p.n_segs;
     double mine = 0.0;
     int last = -1;  // the last one with a share
     for (int g = lo; g < hi; ++g) {
@@ -307,12 +400,12 @@ struct Pick {
       mine += s;
       if (s > 0.0) last = g;
     }
+    if (threadIdx.x == 0) *found = 0x7FFFFFFF;
     double all;
     const double upto = group.scan(mine, &all);
     *total = all;
-    const double target = u * all;
-    if (threadIdx.x == 0) *found = 0x7FFFFFFF;
-    last = group.largest(last);  // (has the barriers)
+    const double target = target_of(all);
+    last = group.largest(last);
     int* const slot = found;
     if (lo < hi && upto > target) atomicMin(slot, (int)threadIdx.x);
     __syncthreads();
@@ -320,7 +413,7 @@ struct Pick {
     if (who == 0x7FFFFFFF) {  // past the end by a rounding
       if (threadIdx.x == 0) {
         found[1] = last;
-        *held = -1.0;
+        held[0] = -1.0;
       }
     } else if ((int)threadIdx.x == who) {
       double run = upto - mine;
@@ -331,446 +424,622 @@ struct Pick {
         run += s;
       }
       found[1] = g;
-      *held = target - run;
+      held[0] = target - run;
     }
     __syncthreads();
     const int g = found[1];
-    const double rest = *held;
-    if (threadIdx.x < kWave) {
-      const int lane = threadIdx.x;
-      typename R::P x[R::kPacks];
-      int at[R::kPacks];
-      unsigned bits[R::kPacks];
-      row.load(g, x, at, bits);
-      int id = -1, end = -1;
+    const double rest = held[0];
+    // a wave for each lane's pack, in the order of ids
+    const int lane = threadIdx.x & (kWave - 1);
+    const int q = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    static_assert(R::kPacks <= kPickWaves, "a wave for each pack");
+    double w[R::kEpv], s = 0.0, upto_lane = 0.0;
+    int at = 0, end = -1;
+    if (q < R::kPacks) {
+      unsigned bits;
+      typename R::P x;
+      at = row.place(g, q, bits);
+      row.span.load(x, at);
+#pragma unroll
+      for (int j = 0; j < R::kEpv; ++j) {
+        w[j] = (bits >> j) & 1u ? value(x.get(j), at + j) : 0.0;
+        s += w[j];
+        if (w[j] > 0.0) end = at + j;
+        if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+      upto_lane = s;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const double t = __shfl_up(upto_lane, o, kWave);
+        if (lane >= o) upto_lane += t;
+      }
+      if (lane == kWave - 1) held[1 + q] = upto_lane;
+    }
+    if (threadIdx.x == 0) found[2] = 0x7FFFFFFF;
+    end = group.largest(end);  // (has a barrier)
+    if (q < R::kPacks) {
       double run = 0.0;
-#pragma unroll 1
-      for (int q = 0; q < R::kPacks && id < 0; ++q) {
-        typename R::P y;
-        unsigned b;
-        const int a = row.place(g, q, b);
-        row.span.load(y, a);
-        double s = 0.0;
+      for (int i = 0; i < q; ++i) run += held[1 + i];
+      const unsigned long long past = __ballot(rest >= 0.0 && run + upto_lane > rest);
+      if (past && lane == __ffsll((long long)past) - 1) {
+        int got = -1;
+        double t = run + (upto_lane - s);
 #pragma unroll
         for (int j = 0; j < R::kEpv; ++j) {
-          const float z = y.get(j);
-          if (((b >> j) & 1u) && keep(z, a + j)) {
-            const double w = weight(z);
-            s += w;
-            if (w > 0.0) end = a + j;
-          }
+          if (w[j] > 0.0 && (got < 0 || t <= rest)) got = at + j;
+          t += w[j];
         }
-        double upto_lane = s;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-          const double t = __shfl_up(upto_lane, o, kWave);
-          if (lane >= o) upto_lane += t;
-        }
-        const unsigned long long past = __ballot(rest >= 0.0 && run + upto_lane > rest);
-        if (past) {
-          const int who_lane = __ffsll((long long)past) - 1;
-          int got = -1;
-          if (lane == who_lane) {
-            double t = run + (upto_lane - s);
-#pragma unroll
-            for (int j = 0; j < R::kEpv; ++j) {
-              const float z = y.get(j);
-              if (((b >> j) & 1u) && keep(z, a + j)) {
-                const double w = weight(z);
-                if (w > 0.0 && (got < 0 || t <= rest)) got = a + j;
-                t += w;
-              }
-            }
-          }
-          id = __shfl(got, who_lane, kWave);
-        }
-        run += __shfl(upto_lane, kWave - 1, kWave);
+        int* const slot = found + 2;
+        if (got >= 0) atomicMin(slot, got);
       }
-#pragma unroll
-      for (int o = kWave / 2; o > 0; o >>= 1) {
-        const int t = __shfl_xor(end, o, kWave);
-        end = t > end ? t : end;
-      }
-      if (lane == 0) found[2] = id >= 0 ? id : end;
     }
     __syncthreads();
-    return found[2];
+    return found[2] < 0x7FFFFFFF ? found[2] : end;
+  }
+};
+
+// The border of a support in a row at large.
+template <bool kBf16, bool kRagged>
+struct Wide {
+  Pick<kBf16, kRagged>& row;
+  unsigned* bins;               // LDS, kBins
+  unsigned long long* between;  // LDS, kPickWaves x kBinHeld
+
+  // The largest order that at least `target` elements (kCount) reach, or elements of at
+  // least that mass; *above: how many, or what mass, lies above it.  kNothing where all
+  // finite elements together are too few.
+  //
+  // A histogram of 1,024 bins gives the bin that holds the border (of the mass: nearly
+  // always; what is above the bin is then summed exactly, and a neighbour is taken if need
+  // be), and up to 512 elements a wave in the bin are put aside, in a fixed order.  If they
+  // are more, the bin is cut into 1,024 again.
+  template <bool kCount>
+  __device__ __forceinline__ unsigned locate(double target, double* above) {
+    Group& group = row.group;
+    const int tid = threadIdx.x;
+    const int lane = tid & (kWave - 1);
+    const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+    // Orders in [lo, hi] are looked at; `over` lies above them.
+    unsigned lo = kNothing + 1u, hi = order_of(row.m);
+    double over = 0.0;
+    const float rate = (float)row.plan.rate;
+#pragma unroll 1
+    for (int level = 0;; ++level) {
+      // First by the logits' distance from the maximum, 1 / 16 of a power of two of weight
+      // a bin and whatever is further down in the last one, then by their orders.
+      constexpr float kWidth = 0.0625f;
+      int shift = 0;
+      while ((hi - lo) >> shift >= kBins) ++shift;
+      const double per = row.plan.rate * (1.0 / kWidth);
+      auto coordinate = [&](float z) { return (float)(((double)row.m - (double)z) * per); };
+      auto bin_of = [&](float z, unsigned o) {
+        if (level > 0) return (int)((hi - o) >> shift);
+        const float x = coordinate(z);
+        return x < kBins - 1 ? (int)x : kBins - 1;
+      };
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kPickThreads) bins[i] = 0u;
+      __syncthreads();
+      row.each(lo, [&](float z, int, bool own) {
+        const unsigned o = order_of(z);
+        if (!own || o < lo || o > hi) return;
+        const int b = bin_of(z, o);
+        unsigned n = 1;  // of masses: in 1 / 128 of the weight at the bin's edge
+        if (!kCount && level == 0) n = (unsigned)(128.0f * exp2_fast((b - coordinate(z)) * kWidth));
+        unsigned* const slot = bins + b;
+        atomicAdd(slot, n);
+      });
+      __syncthreads();
+      double v[2];
+      int filled = -1;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int b = 2 * tid + i;
+        const unsigned n = bins[b];
+        if (n) filled = b;
+        v[i] = n;
+        if constexpr (!kCount) {
+          if (n) v[i] *= level == 0 ? pow2(-(double)(b * kWidth)) * (1.0 / 128.0)
+                                    : row.weight(logit_of(hi - ((unsigned)b << shift)));
+        }
+      }
+      if (tid == 0) *row.found = 0x7FFFFFFF;
+      double all;
+      const double upto = over + group.scan(v[0] + v[1], &all);
+      const int last = group.largest(filled);
+      if (kCount && level == 0 && all < target) {
+        *above = all;
+        return kNothing;
+      }
+      int* const slot = row.found;
+      if (upto >= target) atomicMin(slot, upto - v[1] >= target ? 2 * tid : 2 * tid + 1);
+      __syncthreads();
+      int bin = *row.found < last ? *row.found : last;
+      int moved = 0;
+#pragma unroll 1
+      for (;;) {
+        // what lies above the bin, and its elements
+        double sum[2] = {0.0, 0.0};
+        int held = 0;  // of this wave
+        int least = 0x7FFFFFFF, most = -0x7FFFFFFF - 1;
+        row.each(lo, [&](float z, int id, bool own) {
+          const unsigned o = order_of(z);
+          const int b = !own || o < lo || o > hi ? kBins : bin_of(z, o);
+          if (b <= bin) {
+            const double w = kCount ? 1.0 : row.weight(z);
+            if (b < bin) {
+              sum[0] += w;
+            } else {
+              sum[1] += w;
+              const int so = signed_order(o);
+              least = so < least ? so : least;
+              most = so > most ? so : most;
+            }
+          }
+          const unsigned long long in = __ballot(b == bin);
+          const int to = held + __popcll(in & ((1ull << lane) - 1ull));
+          if (b == bin && to < kBinHeld) between[wid * kBinHeld + to] = ((unsigned long long)o << 32) | (unsigned)id;
+          held += __popcll(in);
+        });
+        group.sums(sum);
+        const double before = over + sum[0];
+        if (moved <= 0 && bin > 0 && before >= target) {
+          --bin;
+          moved = -1;
+          continue;
+        }
+        if (moved >= 0 && bin < last && before + sum[1] < target) {
+          ++bin;
+          moved = 1;
+          continue;
+        }
+        most = group.largest(most);
+        least = ~group.largest(~least);
+        const int fullest = group.largest(held);
+        if (fullest > kBinHeld) {
+          if (least == most) {  // equal, however many
+            *above = before;
+            return unsigned_order(least);
+          }
+          over = before;
+          lo = unsigned_order(least);
+          hi = unsigned_order(most);
+          break;
+        }
+        // (the largest order is found bit by bit, two at a time)
+        unsigned order[kBinEach];
+        double w[kBinEach];
+#pragma unroll
+        for (int q = 0; q < kBinEach; ++q) {
+          const int i = q * kWave + lane;
+          const unsigned long long x = i < held ? between[wid * kBinHeld + i] : 0ull;
+          order[q] = (unsigned)(x >> 32);
+          w[q] = i >= held ? 0.0 : kCount ? 1.0 : row.weight(logit_of(order[q]));
+        }
+        unsigned t = 0;
+#pragma unroll 1
+        for (int b = 30; b >= (kBf16 ? 16 : 0); b -= 2) {
+          double n[3] = {0.0, 0.0, 0.0};
+#pragma unroll
+          for (int q = 0; q < kBinEach; ++q)
+#pragma unroll
+            for (unsigned d = 0; d < 3; ++d) n[d] += order[q] >= (t | ((d + 1) << b)) ? w[q] : 0.0;
+          group.sums(n);
+          t |= (before + n[2] >= target ? 3u : before + n[1] >= target ? 2u : before + n[0] >= target ? 1u : 0u) << b;
+        }
+        // (of bf16 logits the lower half follows from the upper one: all ones below zero;
+        // past the end by a rounding: the least)
+        t = !t ? unsigned_order(least) : kBf16 && !(t >> 31) ? t | 0xFFFFu : t;
+        double n = 0.0;
+#pragma unroll
+        for (int q = 0; q < kBinEach; ++q) n += order[q] > t ? w[q] : 0.0;
+        *above = before + group.sum(n);
+        return t;
+      }
+    }
   }
 
-  // The largest t whose number of elements >= t is at least k (kCount), or whose mass is at
-  // least `least`, two bits at a time; `over` hands elements of at least an order to its
-  // argument.
-  template <bool kCount, typename Over>
-  __device__ __forceinline__ unsigned border_order(int k, double least, Over over) const {
-    unsigned t = 0;
-#pragma unroll 1
-    for (int b = 30; b >= (kBf16 ? 16 : 0); b -= 2) {
-      int n[3] = {0, 0, 0};
-      double w[3] = {0.0, 0.0, 0.0};
-      over(t | (1u << b), [&](unsigned o, int, double weight_of) {
-#pragma unroll
-        for (unsigned d = 0; d < 3; ++d)
-          if (o >= (t | ((d + 1) << b))) {
-            if constexpr (kCount) ++n[d];
-            else w[d] += weight_of;
-          }
-      });
-      unsigned digit = 0;
-#pragma unroll
-      for (unsigned d = 0; d < 3; ++d) {
-        bool enough;
-        if constexpr (kCount) enough = group.sum(n[d]) >= k;
-        else enough = group.sum(w[d]) >= least;
-        if (enough) digit = d + 1;
-      }
-      t |= digit << b;
-    }
-    // (of bf16 logits the lower half follows from the upper one: all ones below zero)
-    return kBf16 && t && !(t >> 31) ? t | 0xFFFFu : t;
-  }
-  // The id of the n-th (from 1) element of that order, in the order of ids.
-  template <typename Over>
-  __device__ __forceinline__ int nth_equal(unsigned order, int n, Over over) const {
-    int x = 0;
-#pragma unroll 1
-    for (int b = 23; b >= 0; --b) {
-      int below = 0;
-      over(order, [&](unsigned o, int id, double) { below += o == order && id < (x | (1 << b)); });
-      if (group.sum(below) < n) x |= 1 << b;
-    }
-    return x;
-  }
-  // Where the support ends by top-k and top-p.  (*whole: the mass that top-p refers to.)
-  template <typename Over>
-  __device__ __forceinline__ Border border(double row_mass, Over over) const {
+  // Where the support ends by top-k and top-p (`row_mass`: what top-p refers to without
+  // top-k).
+  __device__ __forceinline__ Border border(double row_mass) {
+    const Plan& plan = row.plan;
     Border e{0u, 0x7FFFFFFF};
-    int ties = 0x7FFFFFFF;
-    double whole = row_mass;
+    double ties = 0x7FFFFFFF, whole = row_mass;
     if (plan.k > 0) {
-      e.order = border_order<true>(plan.k, 0.0, over);
-      int above = 0;
-      double mass = 0.0;
-      over(e.order, [&](unsigned o, int, double w) {
-        if (o > e.order) {
-          ++above;
-          mass += w;
-        }
-      });
-      ties = plan.k - group.sum(above);
-      whole = group.sum(mass) + ties * weight(logit_of(e.order));
+      double above;
+      e.order = locate<true>((double)plan.k, &above);
+      ties = (double)plan.k - above;
+      if (plan.p < 1.0f) {
+        double mass = 0.0;
+        row.each(e.order, [&](float z, int, bool own) {
+          mass += own && order_of(z) > e.order ? row.weight(z) : 0.0;
+        });
+        whole = row.group.sum(mass);
+        if (e.order != kNothing) whole += ties * row.weight(logit_of(e.order));
+      }
     }
     if (plan.p < 1.0f) {
       const double least = (double)plan.p * whole;
-      const unsigned order = border_order<false>(0, least, over);
-      double mass = 0.0;
-      over(order, [&](unsigned o, int, double w) { mass += o > order ? w : 0.0; });
-      mass = group.sum(mass);
+      double above;
+      const unsigned order = locate<false>(least, &above);
       // those of this order whose predecessors hold less
-      const double w = weight(logit_of(order));
-      const double n = w > 0.0 ? ceil((least - mass) / w) : 0.0;
-      const int some = n < 1.0 ? 1 : n < 1e9 ? (int)n : 1000000000;
-      if (order > e.order || plan.k == 0) {
+      const double w = row.weight(logit_of(order));
+      const double n = w > 0.0 ? ceil((least - above) / w) : 1.0;
+      const double some = n > 1.0 ? n : 1.0;
+      if (order > e.order) {
         e.order = order;
         ties = some;
       } else if (order == e.order) {
         ties = some < ties ? some : ties;
       }
     }
-    if (e.order) {
-      int equal = 0;
-      over(e.order, [&](unsigned o, int, double) { equal += o == e.order; });
-      if (group.sum(equal) > ties) e.id = nth_equal(e.order, ties, over);
+    if (e.order > kNothing) {
+      // the id of the last one of this order that counts
+      const SampleParams& p = row.p;
+      for (int g = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); g < p.n_segs; g += kPickWaves) {
+        int n = 0;
+        if (order_of(p.seg_max[row.first + g]) >= e.order)
+          row.each_of(g, [&](float z, int, bool own) { n += own && order_of(z) == e.order; });
+        wave_exclusive_dpp(n, &n);
+        if ((threadIdx.x & (kWave - 1)) == 0) p.seg_sum[row.first + g] = (float)n;
+      }
+      __syncthreads();
+      double all;
+      const int id = row.by_segment([&](double) { return ties - 1.0; },
+                                    [&](int g) { return (double)p.seg_sum[row.first + g]; },
+                                    [&](float z, int) { return order_of(z) == e.order ? 1.0 : 0.0; }, &all);
+      if (all > ties) e.id = id;
     }
     return e;
   }
 };
 
-template <bool kBf16, bool kRagged>
-__global__ __launch_bounds__(kPickThreads) void sample_pick(SampleParams p) {
-  __shared__ double s_sum[kPickWaves];
-  __shared__ int s_scan[kPickWaves];
+// kWide: rows that the ranked candidates do not settle are finished here; otherwise they are
+// left to a second kernel, which (with p.todo) takes no others.
+template <bool kBf16, bool kRagged, bool kWide>
+__global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(SampleParams p) {
+  __shared__ double s_sum[2][kPickWaves * 3];
+  __shared__ int s_scan[2][kPickWaves * 3];
   __shared__ int s_found[4];
-  __shared__ double s_held;
-  __shared__ unsigned long long s_list[kListed];
-  __shared__ int s_unit[kUnitsHeld];
+  __shared__ double s_held[1 + kPickWaves];
+  __shared__ unsigned long long s_key[kRanked + kRankPad];
+  __shared__ unsigned long long s_ranked[kRanked];
   __shared__ double s_run[kRanked];
-  __shared__ int s_id[kRanked];
+  __shared__ int s_id[kRanked + kRankPad];
+  __shared__ int s_unit[kUnitsHeld];
   const int tid = threadIdx.x;
-  const int lane = tid & (kWave - 1);
-  const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
   using R = Row<kBf16, kRagged>;
-  const Group group{s_sum, s_scan};
-  for (long long row = blockIdx.x; row < p.n_rows; row += gridDim.x) {
-    auto write = [&](int id, float logq, float logp) {
-      if (tid != 0) return;
-      p.ids[row] = id;
-      if (p.logq) p.logq[row] = logq;
-      if (p.logp) p.logp[row] = logp;
-    };
-    if (p.mask && !p.mask[row]) {
-      write(-1, 0.0f, 0.0f);
-      continue;
-    }
-    const Plan plan = plan_of(p, row);
-    const double u = p.u[row];
-    const float nan = __builtin_nanf("");
-    if (plan.bad || !(u >= 0.0 && u < 1.0)) {
-      if (tid == 0) atomicMin(&p.hdr->err_key, err_key(row, kPrioSampling));
-      write(-1, nan, nan);
-      continue;
-    }
-    const long long first = row * p.n_segs;
-    // the row's maximum (no number where one is none)
-    float m = -INFINITY;
-    bool none = false;
-    for (int g = tid; g < p.n_segs; g += kPickThreads) {
-      const float x = p.seg_max[first + g];
-      none = none || x != x;
-      m = fmaxf(m, x);
-    }
-    m = logit_of((unsigned)group.largest((int)(order_of(m) ^ 0x80000000u)) ^ 0x80000000u);
-    if (group.sum(none ? 1 : 0) || m == INFINITY) {
-      write(-1, nan, nan);
-      continue;
-    }
-    if (m == -INFINITY) {  // nothing is allowed
-      write(-1, -INFINITY, -INFINITY);
-      continue;
-    }
-    double log_all = 0.0;
-    if (p.logp) {
-      double s = 0.0;
-      for (int g = tid; g < p.n_segs; g += kPickThreads)
-        s += p.seg_sum[first + g] * pow2(((double)p.seg_max[first + g] - m) * 1.4426950408889634074);
-      log_all = log(group.sum(s));
-    }
-    const Pick<kBf16, kRagged> pick{p, R(p, row), plan, group, first, m, s_found, &s_held, s_list};
-    auto segment = [&](int g) {
-      const double s = p.seg_mass[first + g];
-      return s > 0.0 ? s * pick.weight(p.seg_max[first + g]) : 0.0;
-    };
-    auto finish = [&](int id, double total) {
-      if (tid != 0) return;
-      const long long at = row * p.ld + id;
-      const float z = kBf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
-                            : static_cast<const float*>(p.z)[at];
-      const double x = (double)z - m;
-      write(id, (float)(x * plan.rate * 0.69314718055994530942 - log(total)), (float)(x - log_all));
-    };
-    double total;
-    if (!plan.filtered) {
-      const int id = pick.by_segment(u, segment, [](float, int) { return true; }, &total);
-      finish(id, total);
-      __syncthreads();
-      continue;
-    }
-    double row_mass = 0.0;
-    if (plan.mass) {
-      double s = 0.0;
-      for (int g = tid; g < p.n_segs; g += kPickThreads) s += segment(g);
-      row_mass = group.sum(s);
-    }
-    const unsigned short* const unit = p.unit + first * kWave;
-    const int units = p.n_segs * kWave;
-    // by min-p alone: what lies clearly below its border is not needed
-    unsigned floor = kNothing + 1u;
-    if (plan.p >= 1.0f && plan.min_p > 0.0f) {
-      const double z = m + log((double)plan.min_p) * 1.4426950408889634074 / plan.rate;
-      const float low = (float)(z - 1e-5 * (fabs(z) + fabs((double)m)) - 1e-30);
-      if (order_of(low) > floor) floor = order_of(low);
-    }
-    const bool by_mass = plan.k == 0 && plan.p < 1.0f;
-    int want = plan.k > 0 ? plan.k : by_mass ? kFirstWant : 0;
-    int listed = kListed + 1;
-    bool ended = false;
-    for (int turn = 0; turn < 2 && !ended; ++turn) {
-      // the want-th largest unit maximum
-      unsigned bound = 0;
-      if (want > 0 && want <= units) {
-#pragma unroll 1
-        for (int b = 15; b >= 0; --b) {
-          int n = 0;
-          for (int i = tid; i < units; i += kPickThreads) n += unit[i] >= (bound | (1u << b));
-          if (group.sum(n) >= want) bound |= 1u << b;
-        }
-      }
-      unsigned least = bound << 16;
-      least = least > floor ? least : floor;
-      // units that reach it
-      int count = 0, all;
-      for (int i = tid; i < units; i += kPickThreads) count += unit[i] >= (least >> 16);
-      int at = group.scan(count, &all);
-      listed = kListed + 1;
-      if (all <= kUnitsHeld) {
-        for (int i = tid; i < units; i += kPickThreads)
-          if (unit[i] >= (least >> 16)) s_unit[at++] = i;
-        __syncthreads();
-        // and their elements that do
-        listed = 0;
-        const int packs = all * R::kPacks;
-        for (int base = 0; base < packs; base += kPickThreads) {
-          const int i = base + tid;
-          typename R::P x;
-          unsigned in = 0;
-          int e = 0;
-          if (i < packs) {
-            const int what = s_unit[i / R::kPacks];
-            unsigned bits;
-            e = pick.row.span.place((what / kWave * R::kPacks + i % R::kPacks) * kWave + what % kWave, bits);
-            pick.row.span.load(x, e);
+  Group group{s_sum, s_scan};
+  const long long row = p.first_row + blockIdx.x;
+  if (kWide && p.todo && !p.todo[row]) return;
+  auto write = [&](int id, float logq, float logp) {
+    if (tid != 0) return;
+    p.ids[row] = id;
+    if (p.logq) p.logq[row] = logq;
+    if (p.logp) p.logp[row] = logp;
+  };
+  if (!kWide && tid == 0) p.todo[row] = 0;
+  if (p.mask && !p.mask[row]) {
+    write(-1, 0.0f, 0.0f);
+    return;
+  }
+  const Plan plan = plan_of(p, row);
+  const double u = p.u[row];
+  const float nan = __builtin_nanf("");
+  if (plan.bad || !(u >= 0.0 && u < 1.0)) {
+    if (tid == 0) atomicMin(&p.hdr->err_key, err_key(row, kPrioSampling));
+    write(-1, nan, nan);
+    return;
+  }
+  const long long first = row * p.n_segs;
+  const unsigned short* const unit = p.unit + first * kWave;
+  const int units = p.n_segs * kWave;
+  const bool few = units <= kUnitEach * kPickThreads;
+  // what the row's segments left, and its units, on their way together
+  const bool one_each = p.n_segs <= kPickThreads;
+  float seg_max = -INFINITY, seg_sum = 0.0f;
+  double seg_mass = 0.0;
+  if (one_each && tid < p.n_segs) {
+    seg_max = p.seg_max[first + tid];
+    seg_sum = p.seg_sum[first + tid];
+    seg_mass = p.seg_mass[first + tid];
+  }
+  unsigned held[kUnitEach];
 #pragma unroll
-            for (int j = 0; j < R::kEpv; ++j)
-              if (((bits >> j) & 1u) && order_of(x.get(j)) >= least) in |= 1u << j;
+  for (int c = 0; c < kUnitEach; ++c)
+    held[c] = plan.filtered && few && c * kPickThreads + tid < units ? unit[c * kPickThreads + tid] : 0u;
+  auto each_segment = [&](auto use) {  // use(maximum, sum, mass)
+    if (one_each) {
+      use(seg_max, seg_sum, seg_mass);
+    } else {
+      for (int g = tid; g < p.n_segs; g += kPickThreads)
+        use(p.seg_max[first + g], p.seg_sum[first + g], p.seg_mass[first + g]);
+    }
+  };
+  // the row's maximum (above all numbers where one is none)
+  int top = signed_order(kNothing);
+  each_segment([&](float x, float, double) {
+    const int o = x == x ? signed_order(order_of(x)) : 0x7FFFFFFF;
+    top = o > top ? o : top;
+  });
+  top = group.largest(top);
+  const float m = logit_of(unsigned_order(top));
+  if (!(m < INFINITY)) {
+    write(-1, nan, nan);
+    return;
+  }
+  if (m == -INFINITY) {  // nothing is allowed
+    write(-1, -INFINITY, -INFINITY);
+    return;
+  }
+  Pick<kBf16, kRagged> pick{p, R(p, row), plan, group, first, m, s_found, s_held};
+  const bool same = plan.mass && plan.rate == kLog2e64;
+  double both[2] = {0.0, 0.0};  // sums at temperature 1 and at the row's
+  each_segment([&](float x, float s, double w) {
+    if (p.logp && !same) both[0] += s * pow2(((double)x - m) * kLog2e64);
+    if (plan.mass) both[1] += w * pick.weight(x);
+  });
+  group.sums(both);
+  const double row_mass = both[1], log_all = log(same ? both[1] : both[0]);
+  auto finish = [&](int id, double total) {
+    if (tid != 0) return;
+    const long long at = row * p.ld + id;
+    const float z = kBf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
+                          : static_cast<const float*>(p.z)[at];
+    const double x = (double)z - m;
+    write(id, (float)(x * plan.rate * kLn264 - log(total)), (float)(x - log_all));
+  };
+  double total;
+  if (!plan.filtered) {
+    const int id = pick.by_segment([&](double all) { return u * all; },
+                                   [&](int g) { return p.seg_mass[first + g] * pick.weight(p.seg_max[first + g]); },
+                                   [&](float z, int) { return pick.weight(z); }, &total);
+    finish(id, total);
+    return;
+  }
+  const bool by_mass = plan.k == 0 && plan.p < 1.0f;
+  int listed = kRanked + 1;
+  if (!kWide || !p.todo) {
+    auto each_unit = [&](auto use) {  // use(upper half of its order, index)
+      if (few) {
+#pragma unroll
+        for (int c = 0; c < kUnitEach; ++c)
+          if (c * kPickThreads < units) use(held[c], c * kPickThreads + tid);
+      } else {
+        for (int i = tid; i < units; i += kPickThreads) use((unsigned)unit[i], i);
+      }
+    };
+    // the want-th largest unit maximum bounds the elements that are needed
+    const int want = plan.k > 0 ? plan.k : by_mass ? kWantByMass : 0;
+    unsigned bound = 0;
+    if (want > 0 && want <= units) {
+#pragma unroll 1
+      for (int b = 14; b >= 0; b -= 2) {
+        int n[3] = {0, 0, 0};
+        each_unit([&](unsigned o, int) {
+#pragma unroll
+          for (unsigned d = 0; d < 3; ++d) n[d] += o >= (bound | ((d + 1) << b));
+        });
+        group.sums(n);
+        bound |= (n[2] >= want ? 3u : n[1] >= want ? 2u : n[0] >= want ? 1u : 0u) << b;
+      }
+    }
+    unsigned least = bound << 16;
+    if (least <= kNothing) least = kNothing + 1u;
+    // by min-p alone: what lies clearly below its border is not needed
+    if (plan.p >= 1.0f && plan.min_p > 0.0f) {
+      const double z = m + log2((double)plan.min_p) / plan.rate;
+      const float low = (float)(z - 1e-5 * (fabs(z) + fabs((double)m)) - 1e-30);
+      if (order_of(low) > least) least = order_of(low);
+    }
+    // units that reach it
+    int count = 0, all;
+    each_unit([&](unsigned o, int i) { count += i < units && o >= (least >> 16); });
+    int at = group.scan(count, &all);
+    if (all <= kUnitsHeld) {
+      each_unit([&](unsigned o, int i) {
+        if (i < units && o >= (least >> 16)) s_unit[at++] = i;
+      });
+      __syncthreads();
+      // and their elements that do, a unit a thread
+      listed = 0;
+      for (int base = 0; base < all && listed <= kRanked; base += kPickThreads) {
+        const int what = base + tid < all ? s_unit[base + tid] : -1;
+        typename R::P x[R::kPacks];
+        int e[R::kPacks];
+        unsigned in[R::kPacks];
+#pragma unroll
+        for (int q = 0; q < R::kPacks; ++q) {
+          in[q] = 0;
+          e[q] = 0;
+          if (what >= 0) {
+            e[q] = pick.row.span.place((what / kWave * R::kPacks + q) * kWave + what % kWave, in[q]);
+            pick.row.span.load(x[q], e[q]);
           }
-          int some;
-          int to = listed + group.scan(__popc(in), &some);
+        }
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
           for (int j = 0; j < R::kEpv; ++j)
-            if ((in >> j) & 1u) {
-              if (to < kListed) s_list[to] = ((unsigned long long)order_of(x.get(j)) << 32) | (unsigned)(e + j);
+            if (((in[q] >> j) & 1u) && order_of(x[q].get(j)) < least) in[q] &= ~(1u << j);
+          n += __popc(in[q]);
+          x[q].fence();  // ordered again, rather than kept
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        int some;
+        int to = listed + group.scan(n, &some);
+#pragma unroll
+        for (int q = 0; q < R::kPacks; ++q)
+#pragma unroll
+          for (int j = 0; j < R::kEpv; ++j)
+            if ((in[q] >> j) & 1u) {
+              if (to < kRanked) s_key[to] = ((unsigned long long)order_of(x[q].get(j)) << 32) | (unsigned)~(e[q] + j);
               ++to;
+              __builtin_amdgcn_sched_barrier(0);
             }
-          listed += some;
-        }
-        __syncthreads();
+        listed += some;
       }
-      ended = true;
-      if (by_mass && listed <= kListed) {
-        double s = 0.0;
-        for (int i = tid; i < listed; i += kPickThreads) s += pick.weight(logit_of((unsigned)(s_list[i] >> 32)));
-        if (group.sum(s) < (double)plan.p * row_mass) {  // the border lies further down
-          ended = turn > 0 || want >= kMoreWant;
-          want = kMoreWant;
-          listed = kListed + 1;
-        }
-      }
+      __syncthreads();
     }
-    if (listed <= kRanked) {
-      // ranked against each other: by logits, then ids
-      unsigned long long mine = 0;
-      int rank = 0;
-      if (tid < listed) {
-        mine = s_list[tid] ^ 0xFFFFFFFFull;  // the lower id first
-        for (int j = 0; j < listed; ++j) rank += (s_list[j] ^ 0xFFFFFFFFull) > mine;
+  }
+  if (listed <= kRanked) {
+    // ranked against each other: by logits, the lower id first
+    if (tid < kRankPad) s_key[listed + tid] = 0ull;
+    __syncthreads();
+    unsigned long long mine[kRankEach];
+    int rank[kRankEach];
+#pragma unroll
+    for (int c = 0; c < kRankEach; ++c) {
+      mine[c] = c * kPickThreads + tid < listed ? s_key[c * kPickThreads + tid] : ~0ull;
+      rank[c] = 0;
+    }
+    for (int j = 0; j < listed; j += kRankPad) {
+      unsigned long long other[kRankPad];
+#pragma unroll
+      for (int i = 0; i < kRankPad; ++i) other[i] = s_key[j + i];
+#pragma unroll
+      for (int i = 0; i < kRankPad; ++i)
+#pragma unroll
+        for (int c = 0; c < kRankEach; ++c) rank[c] += other[i] > mine[c];
+    }
+#pragma unroll
+    for (int c = 0; c < kRankEach; ++c)
+      if (c * kPickThreads + tid < listed) s_ranked[rank[c]] = mine[c];
+    __syncthreads();
+    // neighbours in that order a thread
+    unsigned long long x[kRankEach];
+    double w[kRankEach];
+    bool in[kRankEach];
+    double sum = 0.0, run_all;
+#pragma unroll
+    for (int c = 0; c < kRankEach; ++c) {
+      const int i = kRankEach * tid + c;
+      x[c] = i < listed ? s_ranked[i] : 0ull;
+      w[c] = i < listed ? pick.weight(logit_of((unsigned)(x[c] >> 32))) : 0.0;
+      in[c] = i < listed && (plan.k == 0 || i < plan.k);
+      sum += in[c] ? w[c] : 0.0;
+    }
+    double before = group.scan(sum, &run_all) - sum;
+    const double whole = by_mass ? row_mass : run_all;
+    // (does the border by top-p lie among them?)
+    if (!by_mass || run_all >= (double)plan.p * whole) {
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < kRankEach; ++c) {
+        const bool was = in[c];
+        in[c] = was && (plan.p >= 1.0f || before < (double)plan.p * whole) &&
+                (plan.min_p == 0.0f || w[c] >= (double)plan.min_p);
+        in[c] = in[c] || (tid == 0 && c == 0);
+        before += was ? w[c] : 0.0;
+        n += in[c];
       }
-      __syncthreads();
-      if (tid < listed) s_list[kRanked + rank] = mine ^ 0xFFFFFFFFull;
-      __syncthreads();
-      const unsigned long long x = tid < listed ? s_list[kRanked + tid] : 0ull;
-      const double w = tid < listed ? pick.weight(logit_of((unsigned)(x >> 32))) : 0.0;
-      bool in = tid < listed && (plan.k == 0 || tid < plan.k);
-      double all;
-      const double upto = group.scan(in ? w : 0.0, &all);
-      if (plan.p < 1.0f) in = in && upto - w < (double)plan.p * (by_mass ? row_mass : all);
-      in = in && (plan.min_p == 0.0f || w >= (double)plan.min_p);
-      in = in || tid == 0;
       // the support in the order of ids
       int size;
-      const int place = group.scan(in ? 1 : 0, &size);
-      if (in) s_id[place] = (int)(unsigned)x;
+      int place = group.scan(n, &size);
+      if (tid < kRankPad) s_id[size + tid] = 0x7FFFFFFF;
+#pragma unroll
+      for (int c = 0; c < kRankEach; ++c)
+        if (in[c]) s_id[place++] = (int)~(unsigned)x[c];
       __syncthreads();
-      int before = 0;
-      if (in)
-        for (int j = 0; j < size; ++j) before += s_id[j] < (int)(unsigned)x;
-      if (in) {
-        s_run[before] = w;
-        s_list[before] = x;
+      int lower[kRankEach] = {};
+      for (int j = 0; j < size; j += kRankPad) {
+        int other[kRankPad];
+#pragma unroll
+        for (int i = 0; i < kRankPad; ++i) other[i] = s_id[j + i];
+#pragma unroll
+        for (int i = 0; i < kRankPad; ++i)
+#pragma unroll
+          for (int c = 0; c < kRankEach; ++c) lower[c] += other[i] < (int)~(unsigned)x[c];
       }
+#pragma unroll
+      for (int c = 0; c < kRankEach; ++c)
+        if (in[c]) {
+          s_run[lower[c]] = w[c];
+          s_key[lower[c]] = x[c];
+        }
+      if (tid == 0) s_found[0] = 0x7FFFFFFF;
       __syncthreads();
-      const double mine_w = tid < size ? s_run[tid] : 0.0;
-      const double run = group.scan(mine_w, &total);
-      if (tid == 0) {
-        s_found[0] = 0x7FFFFFFF;
+      double v[kRankEach];
+      int last = -1;
+      sum = 0.0;
+#pragma unroll
+      for (int c = 0; c < kRankEach; ++c) {
+        const int i = kRankEach * tid + c;
+        v[c] = i < size ? s_run[i] : 0.0;
+        sum += v[c];
+        if (v[c] > 0.0) last = i;
       }
-      const int last = group.largest(mine_w > 0.0 ? tid : -1);
-      if (tid < size && mine_w > 0.0 && run > u * total) atomicMin(&s_found[0], tid);
+      double run = group.scan(sum, &total) - sum;
+      last = group.largest(last);
+      const double target = u * total;
+#pragma unroll
+      for (int c = 0; c < kRankEach; ++c) {
+        run += v[c];
+        if (v[c] > 0.0 && run > target) {
+          atomicMin(&s_found[0], kRankEach * tid + c);
+          break;
+        }
+      }
       __syncthreads();
       const int who = s_found[0] < last ? s_found[0] : last;
-      finish((int)(unsigned)s_list[who], total);
-    } else {
-      Border e;
-      double mass = 0.0;
-      auto keep = [&](unsigned o, int id, double w) {
-        return (o > e.order || (o == e.order && id <= e.id)) && w >= (double)plan.min_p;
-      };
-      if (listed <= kListed) {
-        constexpr int kEach = kListed / kPickThreads;
-        unsigned order[kEach];
-        int id[kEach];
-        double w[kEach];
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-          const int i = q * kPickThreads + tid;
-          const unsigned long long x = i < listed ? s_list[i] : 0ull;
-          order[q] = (unsigned)(x >> 32);
-          id[q] = (int)(unsigned)x;
-          w[q] = i < listed ? pick.weight(logit_of(order[q])) : 0.0;
-        }
-        auto over = [&](unsigned least, auto use) {
-#pragma unroll
-          for (int q = 0; q < kEach; ++q)
-            if (order[q] != 0u && order[q] >= least) use(order[q], id[q], w[q]);
-        };
-        e = pick.border(row_mass, over);
-        over(0u, [&](unsigned o, int i, double v) { mass += keep(o, i, v) ? v : 0.0; });
-        total = group.sum(mass);
-        // the largest x with no more than the target before it
-        const double target = u * total;
-        int x = 0, last = -1;
-#pragma unroll 1
-        for (int b = 23; b >= 0; --b) {
-          double below = 0.0;
-          over(0u, [&](unsigned o, int i, double v) { below += i < (x | (1 << b)) && keep(o, i, v) ? v : 0.0; });
-          if (group.sum(below) <= target) x |= 1 << b;
-        }
-        over(0u, [&](unsigned o, int i, double v) {
-          if (v > 0.0 && i > last && keep(o, i, v)) last = i;
-        });
-        last = group.largest(last);
-        finish(x < last ? x : last, total);
-      } else {
-        auto over = [&](unsigned least, auto use) {
-          pick.each(least, [&](float z, int i) {
-            const unsigned o = order_of(z);
-            if (o >= least) use(o, i, pick.weight(z));
-          });
-        };
-        e = pick.border(row_mass, over);
-        // the support's mass segment by segment, in place of the whole one's
-        for (int g = wid; g < p.n_segs; g += kPickWaves) {
-          double s = 0.0;
-          pick.each_of(g, [&](float z, int i) {
-            const double w = pick.weight(z);
-            s += keep(order_of(z), i, w) ? w : 0.0;
-          });
-          s = wave_sum64(s);
-          if (lane == 0) p.seg_mass[first + g] = s;
-        }
-        __syncthreads();
-        const int id = pick.by_segment(
-            u, [&](int g) { return p.seg_mass[first + g]; },
-            [&](float z, int i) { return keep(order_of(z), i, pick.weight(z)); }, &total);
-        finish(id, total);
+      finish((int)~(unsigned)s_key[who], total);
+      return;
+    }
+  }
+  if constexpr (!kWide) {
+    if (tid == 0) p.todo[row] = 1;
+  } else {
+    __shared__ unsigned s_bins[kBins];
+    __shared__ unsigned long long s_between[kPickWaves * kBinHeld];
+    Wide<kBf16, kRagged> wide{pick, s_bins, s_between};
+    const Border e = wide.border(row_mass);
+    auto kept = [&](float z, int id) {
+      const unsigned o = order_of(z);
+      if (!(o > e.order || (o == e.order && id <= e.id))) return 0.0;
+      const double w = pick.weight(z);
+      return w >= (double)plan.min_p ? w : 0.0;
+    };
+    // the support's mass segment by segment, in place of the whole one's
+    for (int g = __builtin_amdgcn_readfirstlane(tid / kWave); g < p.n_segs; g += kPickWaves) {
+      double s = 0.0;
+      if (order_of(p.seg_max[first + g]) >= e.order) {
+        pick.each_of(g, [&](float z, int id, bool own) { s += own ? kept(z, id) : 0.0; });
+        s = wave_sum64(s);
       }
+      if ((tid & (kWave - 1)) == 0) p.seg_mass[first + g] = s;
     }
     __syncthreads();
+    const int id = pick.by_segment([&](double all) { return u * all; },
+                                   [&](int g) { return p.seg_mass[first + g]; }, kept, &total);
+    finish(id, total);
   }
 }
 
-constexpr int kPickGrid = 1 << 20;
+constexpr int kPickGrid = 1 << 20;  // rows of a launch
+constexpr int kPickApart = 256;  // rows: one for each compute unit
 
 }  // namespace
 
-hipError_t launch_sample(const SampleParams& p, hipStream_t s) {
+hipError_t launch_sample(const SampleParams& given, hipStream_t s) {
+  SampleParams p = given;
   const long long tasks = (long long)p.n_rows * p.n_segs;
   const long long blocks = (tasks + kScanWaves - 1) / kScanWaves;
   const int grid = (int)(blocks < 1 ? 1 : blocks < 2048 ? blocks : 2048);
-  const int rows = p.n_rows < kPickGrid ? p.n_rows : kPickGrid;
-#define TURNKL_SAMPLE(B, R)                                                     \
-  if ((p.bf16 != 0) == B && (p.ragged != 0) == R) {                             \
-    sample_scan<B, R><<<grid, kScanThreads, 0, s>>>(p);                         \
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || rows == 0) return e; \
-    sample_pick<B, R><<<rows, kPickThreads, 0, s>>>(p);                         \
+  // Batches that fill the card more than once leave the rows that need it to a kernel of
+  // their own, whose registers would leave room for few workgroups of all.
+  const bool apart = p.n_rows > kPickApart;
+  if (!apart) p.todo = nullptr;
+#define TURNKL_SAMPLE(B, R)                                                         \
+  if ((p.bf16 != 0) == B && (p.ragged != 0) == R) {                                 \
+    sample_scan<B, R><<<grid, kScanThreads, 0, s>>>(p);                             \
+    for (p.first_row = 0; p.first_row < p.n_rows; p.first_row += kPickGrid) {       \
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;              \
+      const long long left = p.n_rows - p.first_row;                                \
+      const int rows = (int)(left < kPickGrid ? left : kPickGrid);                  \
+      if (apart) sample_pick<B, R, false><<<rows, kPickThreads, 0, s>>>(p);         \
+      if (!apart || p.any_filter) sample_pick<B, R, true><<<rows, kPickThreads, 0, s>>>(p); \
+    }                                                                               \
   }
   TURNKL_SAMPLE(true, false) TURNKL_SAMPLE(true, true) TURNKL_SAMPLE(false, false) TURNKL_SAMPLE(false, true)
 #undef TURNKL_SAMPLE

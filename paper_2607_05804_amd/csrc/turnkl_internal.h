@@ -612,7 +612,9 @@ struct SampleParams {
   float* seg_sum;                   // of exp(z - maximum)
   double* seg_mass;                 // of exp((z - maximum) / T)
   unsigned short* unit;             // [n_rows][n_segs][64] orders of lanes' maxima, upper halves
+  unsigned char* todo;              // [n_rows] rows left to a second kernel, or null
   long long ld;
+  long long first_row;  // of a launch that picks
   int n_rows;
   int vocab;
   int n_segs;
@@ -620,6 +622,7 @@ struct SampleParams {
   float temperature;
   float top_p;
   float min_p;
+  int any_filter;  // some row may have one
   int bf16;
   int ragged;
 };
