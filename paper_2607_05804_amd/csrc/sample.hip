@@ -34,11 +34,10 @@ constexpr int kSegElems = kSampleSegment;
 constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / kWave;
 constexpr int kRankEach = 2;                           // of a thread
-constexpr int kRanked = kRankEach * kPickThreads;      // candidates that are ranked against each other
-constexpr int kRankPad = 8;
+constexpr int kRanked = kRankEach * kPickThreads;      // candidates that are sorted
 constexpr int kUnitsHeld = 2048;  // units that are read again, at most
 constexpr int kUnitEach = 16;     // units of a thread that its registers hold
-constexpr int kWantByMass = 500;  // elements that are asked for where only top-p limits a row
+constexpr int kWantByMass = 300;  // elements that are asked for where only top-p limits a row
 constexpr int kBins = 2 * kPickThreads;                // of the histogram
 constexpr int kBinEach = 8;                            // elements of a lane between two bins' edges
 constexpr int kBinHeld = kBinEach * kWave;             // of a wave
@@ -338,6 +337,39 @@ struct Group {
     return m;
   }
 };
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// Sorts the first `n` numbers of LDS, a power of two up to 2 kPickThreads, in descending
+// order: bitonic, a pair a thread; pairs up to 64 apart stay within 128 numbers that are one
+// wave's.
+__device__ __forceinline__ void sort_down(unsigned long long* s, int n) {
+  const int t = threadIdx.x;
+  __syncthreads();
+  for (int run = 2; run <= n; run *= 2) {
+    for (int apart = run / 2; apart > 0; apart /= 2) {
+      if (t < n / 2) {
+        const int i = 2 * t - (t & (apart - 1)), j = i + apart;
+        const unsigned long long a = s[i], b = s[j];
+        const bool down = (i & run) == 0;
+        if ((a < b) == down) {
+          s[i] = b;
+          s[j] = a;
+        }
+      }
+      // (of the next pairs; the first of a longer run are half of it apart)
+      const int next = apart > 1 ? apart / 2 : run;
+      if (next > kWave || apart > kWave) __syncthreads();
+      else wave_lds_order();
+    }
+  }
+  __syncthreads();
+}
+// the least power of two that is n or more, 2 at least
+__device__ __forceinline__ int power_of(int n) { return n <= 2 ? 2 : 1 << (32 - __clz(n - 1)); }
+
 // orders as signed numbers of the same order
 __device__ __forceinline__ int signed_order(unsigned o) { return (int)(o ^ 0x80000000u); }
 __device__ __forceinline__ unsigned unsigned_order(int o) { return (unsigned)o ^ 0x80000000u; }
@@ -478,12 +510,21 @@ struct Pick {
   }
 };
 
-// The border of a support in a row at large.
+// The support of a row at large.
 template <bool kBf16, bool kRagged>
 struct Wide {
   Pick<kBf16, kRagged>& row;
   unsigned* bins;               // LDS, kBins
   unsigned long long* between;  // LDS, kPickWaves x kBinHeld
+
+  // What locate() found last: its elements between two edges, in their lanes' hands (of a
+  // wave's segments the wave's lanes), and whether seg_mass holds what lies above them.
+  bool in_hand = false, by_segment = false;
+  unsigned order[kBinEach];  // 0: none
+  int id[kBinEach];
+  double w[kBinEach];
+
+  __device__ __forceinline__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
 
   // The largest order that at least `target` elements (kCount) reach, or elements of at
   // least that mass; *above: how many, or what mass, lies above it.  kNothing where all
@@ -496,13 +537,11 @@ struct Wide {
   template <bool kCount>
   __device__ __forceinline__ unsigned locate(double target, double* above) {
     Group& group = row.group;
+    const SampleParams& p = row.p;
     const int tid = threadIdx.x;
     const int lane = tid & (kWave - 1);
-    const int wid = __builtin_amdgcn_readfirstlane(tid / kWave);
-    // Orders in [lo, hi] are looked at; `over` lies above them.
-    unsigned lo = kNothing + 1u, hi = order_of(row.m);
-    double over = 0.0;
-    const float rate = (float)row.plan.rate;
+    unsigned lo = kNothing + 1u, hi = order_of(row.m);  // orders that are looked at
+    double over = 0.0;                                  // what lies above them
 #pragma unroll 1
     for (int level = 0;; ++level) {
       // First by the logits' distance from the maximum, 1 / 16 of a power of two of weight
@@ -510,22 +549,40 @@ struct Wide {
       constexpr float kWidth = 0.0625f;
       int shift = 0;
       while ((hi - lo) >> shift >= kBins) ++shift;
-      const double per = row.plan.rate * (1.0 / kWidth);
-      auto coordinate = [&](float z) { return (float)(((double)row.m - (double)z) * per); };
-      auto bin_of = [&](float z, unsigned o) {
+      const float per = (float)fmin(row.plan.rate * (1.0 / kWidth), 3e38);
+      auto coordinate = [&](float z) { return (row.m - z) * per; };
+      auto bin_of = [&](unsigned o) {
         if (level > 0) return (int)((hi - o) >> shift);
-        const float x = coordinate(z);
+        const float x = coordinate(logit_of(o));
         return x < kBins - 1 ? (int)x : kBins - 1;
+      };
+      // the least order in bins up to b
+      auto edge = [&](int b) {
+        if (b < 0) return hi + 1u;
+        unsigned t = lo, n = hi - lo;
+        while (n > 0) {  // (the order hi is in bin 0)
+          const unsigned half = n / 2;
+          if (bin_of(t + half) <= b) {
+            n = half;
+          } else {
+            t += half + 1u;
+            n -= half + 1u;
+          }
+        }
+        return t;
       };
       __syncthreads();
       for (int i = tid; i < kBins; i += kPickThreads) bins[i] = 0u;
       __syncthreads();
+      // of masses in parts of the weight at the bin's edge, as many as all elements together
+      // leave room for
+      const float part = fminf(2147483648.0f / p.vocab, 65536.0f);
       row.each(lo, [&](float z, int, bool own) {
         const unsigned o = order_of(z);
         if (!own || o < lo || o > hi) return;
-        const int b = bin_of(z, o);
-        unsigned n = 1;  // of masses: in 1 / 128 of the weight at the bin's edge
-        if (!kCount && level == 0) n = (unsigned)(128.0f * exp2_fast((b - coordinate(z)) * kWidth));
+        const int b = bin_of(o);
+        unsigned n = 1;
+        if (!kCount && level == 0) n = (unsigned)fmaf(part, exp2_fast((b - coordinate(z)) * kWidth), 0.5f);
         unsigned* const slot = bins + b;
         atomicAdd(slot, n);
       });
@@ -539,7 +596,7 @@ struct Wide {
         if (n) filled = b;
         v[i] = n;
         if constexpr (!kCount) {
-          if (n) v[i] *= level == 0 ? pow2(-(double)(b * kWidth)) * (1.0 / 128.0)
+          if (n) v[i] *= level == 0 ? pow2(-(double)(b * kWidth)) / part
                                     : row.weight(logit_of(hi - ((unsigned)b << shift)));
         }
       }
@@ -558,31 +615,40 @@ struct Wide {
       int moved = 0;
 #pragma unroll 1
       for (;;) {
-        // what lies above the bin, and its elements
+        // what lies above the bin, segment by segment, and its elements
+        const unsigned upper = edge(bin - 1), lower = edge(bin);
         double sum[2] = {0.0, 0.0};
         int held = 0;  // of this wave
         int least = 0x7FFFFFFF, most = -0x7FFFFFFF - 1;
-        row.each(lo, [&](float z, int id, bool own) {
-          const unsigned o = order_of(z);
-          const int b = !own || o < lo || o > hi ? kBins : bin_of(z, o);
-          if (b <= bin) {
-            const double w = kCount ? 1.0 : row.weight(z);
-            if (b < bin) {
-              sum[0] += w;
-            } else {
-              sum[1] += w;
-              const int so = signed_order(o);
-              least = so < least ? so : least;
-              most = so > most ? so : most;
-            }
+        for (int g = wave(); g < p.n_segs; g += kPickWaves) {
+          double mine = 0.0;
+          if (order_of(p.seg_max[row.first + g]) >= lower)
+            row.each_of(g, [&](float z, int i, bool own) {
+              const unsigned o = order_of(z);
+              const bool in = own && o >= lower && o < upper;
+              const double v = kCount ? 1.0 : row.weight(z);
+              mine += own && o >= upper ? v : 0.0;
+              sum[1] += in ? v : 0.0;
+              const unsigned long long who = __ballot(in);
+              if (who) {
+                if (in) {
+                  const int so = signed_order(o);
+                  least = so < least ? so : least;
+                  most = so > most ? so : most;
+                  const int to = held + __popcll(who & ((1ull << lane) - 1ull));
+                  if (to < kBinHeld) between[wave() * kBinHeld + to] = ((unsigned long long)o << 32) | (unsigned)i;
+                }
+                held += __popcll(who);
+              }
+            });
+          sum[0] += mine;
+          if constexpr (!kCount) {
+            mine = wave_sum64(mine);
+            if (lane == 0) p.seg_mass[row.first + g] = mine;
           }
-          const unsigned long long in = __ballot(b == bin);
-          const int to = held + __popcll(in & ((1ull << lane) - 1ull));
-          if (b == bin && to < kBinHeld) between[wid * kBinHeld + to] = ((unsigned long long)o << 32) | (unsigned)id;
-          held += __popcll(in);
-        });
+        }
         group.sums(sum);
-        const double before = over + sum[0];
+        const double before = sum[0];
         if (moved <= 0 && bin > 0 && before >= target) {
           --bin;
           moved = -1;
@@ -595,8 +661,9 @@ struct Wide {
         }
         most = group.largest(most);
         least = ~group.largest(~least);
-        const int fullest = group.largest(held);
-        if (fullest > kBinHeld) {
+        by_segment = !kCount;
+        in_hand = group.largest(held) <= kBinHeld;
+        if (!in_hand) {
           if (least == most) {  // equal, however many
             *above = before;
             return unsigned_order(least);
@@ -606,16 +673,15 @@ struct Wide {
           hi = unsigned_order(most);
           break;
         }
-        // (the largest order is found bit by bit, two at a time)
-        unsigned order[kBinEach];
-        double w[kBinEach];
 #pragma unroll
         for (int q = 0; q < kBinEach; ++q) {
           const int i = q * kWave + lane;
-          const unsigned long long x = i < held ? between[wid * kBinHeld + i] : 0ull;
+          const unsigned long long x = i < held ? between[wave() * kBinHeld + i] : 0ull;
           order[q] = (unsigned)(x >> 32);
+          id[q] = (int)(unsigned)x;
           w[q] = i >= held ? 0.0 : kCount ? 1.0 : row.weight(logit_of(order[q]));
         }
+        // the largest order bit by bit, two at a time
         unsigned t = 0;
 #pragma unroll 1
         for (int b = 30; b >= (kBf16 ? 16 : 0); b -= 2) {
@@ -639,16 +705,53 @@ struct Wide {
     }
   }
 
+  // The id of the n-th (from 1) element of that order in the order of ids, the largest
+  // number where there are no more than n.
+  __device__ __forceinline__ int nth_equal(unsigned o, double n, bool of_hand) {
+    if (of_hand) {
+      int equal = 0;
+#pragma unroll
+      for (int q = 0; q < kBinEach; ++q) equal += order[q] == o;
+      if (row.group.sum(equal) <= n) return 0x7FFFFFFF;
+      int x = 0;
+#pragma unroll 1
+      for (int b = 23; b >= 0; --b) {
+        int below = 0;
+#pragma unroll
+        for (int q = 0; q < kBinEach; ++q) below += order[q] == o && id[q] < (x | (1 << b));
+        if (row.group.sum(below) < n) x |= 1 << b;
+      }
+      return x;
+    }
+    const SampleParams& p = row.p;
+    for (int g = wave(); g < p.n_segs; g += kPickWaves) {
+      int equal = 0;
+      if (order_of(p.seg_max[row.first + g]) >= o)
+        row.each_of(g, [&](float z, int, bool own) { equal += own && order_of(z) == o; });
+      wave_exclusive_dpp(equal, &equal);
+      if ((threadIdx.x & (kWave - 1)) == 0) p.seg_sum[row.first + g] = (float)equal;
+    }
+    __syncthreads();
+    double all;
+    const int x = row.by_segment([&](double) { return n - 1.0; },
+                                 [&](int g) { return (double)p.seg_sum[row.first + g]; },
+                                 [&](float z, int) { return order_of(z) == o ? 1.0 : 0.0; }, &all);
+    return all <= n ? 0x7FFFFFFF : x;
+  }
+
   // Where the support ends by top-k and top-p (`row_mass`: what top-p refers to without
-  // top-k).
-  __device__ __forceinline__ Border border(double row_mass) {
+  // top-k), and its mass segment by segment, in seg_mass.
+  __device__ __forceinline__ Border support(double row_mass) {
     const Plan& plan = row.plan;
+    const SampleParams& p = row.p;
     Border e{0u, 0x7FFFFFFF};
     double ties = 0x7FFFFFFF, whole = row_mass;
+    bool last_ends = false;  // whether what locate() found last ends the support
     if (plan.k > 0) {
       double above;
       e.order = locate<true>((double)plan.k, &above);
       ties = (double)plan.k - above;
+      last_ends = true;
       if (plan.p < 1.0f) {
         double mass = 0.0;
         row.each(e.order, [&](float z, int, bool own) {
@@ -661,36 +764,50 @@ struct Wide {
     if (plan.p < 1.0f) {
       const double least = (double)plan.p * whole;
       double above;
-      const unsigned order = locate<false>(least, &above);
+      const unsigned o = locate<false>(least, &above);
       // those of this order whose predecessors hold less
-      const double w = row.weight(logit_of(order));
-      const double n = w > 0.0 ? ceil((least - above) / w) : 1.0;
+      const double v = row.weight(logit_of(o));
+      const double n = v > 0.0 ? ceil((least - above) / v) : 1.0;
       const double some = n > 1.0 ? n : 1.0;
-      if (order > e.order) {
-        e.order = order;
+      last_ends = o >= e.order;
+      if (o > e.order) {
+        e.order = o;
         ties = some;
-      } else if (order == e.order) {
+      } else if (o == e.order) {
         ties = some < ties ? some : ties;
       }
     }
-    if (e.order > kNothing) {
-      // the id of the last one of this order that counts
-      const SampleParams& p = row.p;
-      for (int g = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); g < p.n_segs; g += kPickWaves) {
-        int n = 0;
-        if (order_of(p.seg_max[row.first + g]) >= e.order)
-          row.each_of(g, [&](float z, int, bool own) { n += own && order_of(z) == e.order; });
-        wave_exclusive_dpp(n, &n);
-        if ((threadIdx.x & (kWave - 1)) == 0) p.seg_sum[row.first + g] = (float)n;
+    const bool of_hand = last_ends && in_hand;
+    if (e.order > kNothing) e.id = nth_equal(e.order, ties, of_hand);
+    const int lane = threadIdx.x & (kWave - 1);
+    if (of_hand && by_segment && row.weight(logit_of(e.order)) >= (double)plan.min_p) {
+      // what lies above the elements in hand is there: a wave adds those of its segments
+      for (int g = wave(); g < p.n_segs; g += kPickWaves) {
+        double s = 0.0;
+#pragma unroll
+        for (int q = 0; q < kBinEach; ++q)
+          if (order[q] && (id[q] + row.row.pre) / kSegElems == g && inside(e, order[q], id[q])) s += w[q];
+        s = wave_sum64(s);
+        if (lane == 0 && s > 0.0) p.seg_mass[row.first + g] += s;
       }
-      __syncthreads();
-      double all;
-      const int id = row.by_segment([&](double) { return ties - 1.0; },
-                                    [&](int g) { return (double)p.seg_sum[row.first + g]; },
-                                    [&](float z, int) { return order_of(z) == e.order ? 1.0 : 0.0; }, &all);
-      if (all > ties) e.id = id;
+    } else {
+      for (int g = wave(); g < p.n_segs; g += kPickWaves) {
+        double s = 0.0;
+        if (order_of(p.seg_max[row.first + g]) >= e.order) {
+          row.each_of(g, [&](float z, int i, bool own) {
+            const double v = own && inside(e, order_of(z), i) ? row.weight(z) : 0.0;
+            s += v >= (double)plan.min_p ? v : 0.0;
+          });
+          s = wave_sum64(s);
+        }
+        if (lane == 0) p.seg_mass[row.first + g] = s;
+      }
     }
+    __syncthreads();
     return e;
+  }
+  __device__ __forceinline__ static bool inside(const Border& e, unsigned o, int i) {
+    return o > e.order || (o == e.order && i <= e.id);
   }
 };
 
@@ -702,11 +819,11 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   __shared__ int s_scan[2][kPickWaves * 3];
   __shared__ int s_found[4];
   __shared__ double s_held[1 + kPickWaves];
-  __shared__ unsigned long long s_key[kRanked + kRankPad];
+  __shared__ unsigned long long s_key[kRanked];
   __shared__ unsigned long long s_ranked[kRanked];
   __shared__ double s_run[kRanked];
-  __shared__ int s_id[kRanked + kRankPad];
   __shared__ int s_unit[kUnitsHeld];
+  __shared__ int s_far[kBins];
   const int tid = threadIdx.x;
   using R = Row<kBf16, kRagged>;
   Group group{s_sum, s_scan};
@@ -809,19 +926,40 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
         for (int i = tid; i < units; i += kPickThreads) use((unsigned)unit[i], i);
       }
     };
-    // the want-th largest unit maximum bounds the elements that are needed
+    // the want-th largest unit maximum bounds the elements that are needed: by how far the
+    // maxima lie below the row's (1,023 orders or more in the last bin)
     const int want = plan.k > 0 ? plan.k : by_mass ? kWantByMass : 0;
     unsigned bound = 0;
     if (want > 0 && want <= units) {
+      const unsigned highest = order_of(m) >> 16;
+      for (int i = tid; i < kBins; i += kPickThreads) s_far[i] = 0;
+      __syncthreads();
+      each_unit([&](unsigned o, int i) {
+        const unsigned d = highest - o;
+        if (i < units) atomicAdd(&s_far[d < kBins - 1 ? d : kBins - 1], 1);
+      });
+      if (tid == 0) s_found[0] = kBins;
+      __syncthreads();
+      const int n0 = s_far[2 * tid], n1 = s_far[2 * tid + 1];
+      int all;
+      const int upto = group.scan(n0 + n1, &all) + n0;
+      if (upto < want && upto + n1 >= want) s_found[0] = 2 * tid + 1;
+      else if (upto >= want && upto - n0 < want) s_found[0] = 2 * tid;
+      __syncthreads();
+      const int far = s_found[0];
+      if (far < kBins - 1) {
+        bound = highest - far;
+      } else {
 #pragma unroll 1
-      for (int b = 14; b >= 0; b -= 2) {
-        int n[3] = {0, 0, 0};
-        each_unit([&](unsigned o, int) {
+        for (int b = 14; b >= 0; b -= 2) {
+          int n[3] = {0, 0, 0};
+          each_unit([&](unsigned o, int) {
 #pragma unroll
-          for (unsigned d = 0; d < 3; ++d) n[d] += o >= (bound | ((d + 1) << b));
-        });
-        group.sums(n);
-        bound |= (n[2] >= want ? 3u : n[1] >= want ? 2u : n[0] >= want ? 1u : 0u) << b;
+            for (unsigned d = 0; d < 3; ++d) n[d] += o >= (bound | ((d + 1) << b));
+          });
+          group.sums(n);
+          bound |= (n[2] >= want ? 3u : n[1] >= want ? 2u : n[0] >= want ? 1u : 0u) << b;
+        }
       }
     }
     unsigned least = bound << 16;
@@ -841,72 +979,54 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
         if (i < units && o >= (least >> 16)) s_unit[at++] = i;
       });
       __syncthreads();
-      // and their elements that do, a unit a thread
+      // and their elements that do, a pack a thread and turn, kPacks turns' loads together
       listed = 0;
-      for (int base = 0; base < all && listed <= kRanked; base += kPickThreads) {
-        const int what = base + tid < all ? s_unit[base + tid] : -1;
+      const int packs = all * R::kPacks;
+      for (int base = 0; base < packs && listed <= kRanked; base += kPickThreads * R::kPacks) {
         typename R::P x[R::kPacks];
         int e[R::kPacks];
         unsigned in[R::kPacks];
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q) {
+          const int i = base + q * kPickThreads + tid;
           in[q] = 0;
           e[q] = 0;
-          if (what >= 0) {
-            e[q] = pick.row.span.place((what / kWave * R::kPacks + q) * kWave + what % kWave, in[q]);
+          if (i < packs) {
+            const int what = s_unit[i / R::kPacks];
+            e[q] = pick.row.span.place((what / kWave * R::kPacks + i % R::kPacks) * kWave + what % kWave, in[q]);
             pick.row.span.load(x[q], e[q]);
           }
         }
-        int n = 0;
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q) {
+          if (base + q * kPickThreads >= packs) break;
 #pragma unroll
           for (int j = 0; j < R::kEpv; ++j)
             if (((in[q] >> j) & 1u) && order_of(x[q].get(j)) < least) in[q] &= ~(1u << j);
-          n += __popc(in[q]);
           x[q].fence();  // ordered again, rather than kept
-          __builtin_amdgcn_sched_barrier(0);
+          int some;
+          int to = listed + group.scan(__popc(in[q]), &some);
+          listed += some;
+          for (; in[q]; in[q] &= in[q] - 1) {
+            const int j = __ffs((int)in[q]) - 1;
+            float z = x[q].get(0);
+#pragma unroll
+            for (int k = 1; k < R::kEpv; ++k) z = k == j ? x[q].get(k) : z;
+            if (to < kRanked) s_key[to] = ((unsigned long long)order_of(z) << 32) | (unsigned)~(e[q] + j);
+            ++to;
+          }
         }
-        int some;
-        int to = listed + group.scan(n, &some);
-#pragma unroll
-        for (int q = 0; q < R::kPacks; ++q)
-#pragma unroll
-          for (int j = 0; j < R::kEpv; ++j)
-            if ((in[q] >> j) & 1u) {
-              if (to < kRanked) s_key[to] = ((unsigned long long)order_of(x[q].get(j)) << 32) | (unsigned)~(e[q] + j);
-              ++to;
-              __builtin_amdgcn_sched_barrier(0);
-            }
-        listed += some;
       }
       __syncthreads();
     }
   }
   if (listed <= kRanked) {
-    // ranked against each other: by logits, the lower id first
-    if (tid < kRankPad) s_key[listed + tid] = 0ull;
-    __syncthreads();
-    unsigned long long mine[kRankEach];
-    int rank[kRankEach];
-#pragma unroll
-    for (int c = 0; c < kRankEach; ++c) {
-      mine[c] = c * kPickThreads + tid < listed ? s_key[c * kPickThreads + tid] : ~0ull;
-      rank[c] = 0;
-    }
-    for (int j = 0; j < listed; j += kRankPad) {
-      unsigned long long other[kRankPad];
-#pragma unroll
-      for (int i = 0; i < kRankPad; ++i) other[i] = s_key[j + i];
-#pragma unroll
-      for (int i = 0; i < kRankPad; ++i)
-#pragma unroll
-        for (int c = 0; c < kRankEach; ++c) rank[c] += other[i] > mine[c];
-    }
-#pragma unroll
-    for (int c = 0; c < kRankEach; ++c)
-      if (c * kPickThreads + tid < listed) s_ranked[rank[c]] = mine[c];
-    __syncthreads();
+    // by logits, the lower id first (by min-p alone in any order)
+    const bool ordered = plan.k > 0 || plan.p < 1.0f;
+    const int full = power_of(listed);
+    for (int i = listed + tid; i < full; i += kPickThreads) s_key[i] = 0ull;
+    if (ordered) sort_down(s_key, full);
+    else __syncthreads();
     // neighbours in that order a thread
     unsigned long long x[kRankEach];
     double w[kRankEach];
@@ -915,7 +1035,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
 #pragma unroll
     for (int c = 0; c < kRankEach; ++c) {
       const int i = kRankEach * tid + c;
-      x[c] = i < listed ? s_ranked[i] : 0ull;
+      x[c] = i < listed ? s_key[i] : 0ull;
       w[c] = i < listed ? pick.weight(logit_of((unsigned)(x[c] >> 32))) : 0.0;
       in[c] = i < listed && (plan.k == 0 || i < plan.k);
       sum += in[c] ? w[c] : 0.0;
@@ -930,43 +1050,32 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
         const bool was = in[c];
         in[c] = was && (plan.p >= 1.0f || before < (double)plan.p * whole) &&
                 (plan.min_p == 0.0f || w[c] >= (double)plan.min_p);
-        in[c] = in[c] || (tid == 0 && c == 0);
+        // (the likeliest token always; its weight is 1, so that min-p keeps it by itself)
+        in[c] = in[c] || (ordered && tid == 0 && c == 0);
         before += was ? w[c] : 0.0;
         n += in[c];
       }
-      // the support in the order of ids
+      // the support in the order of ids (the complement of which the keys hold)
       int size;
       int place = group.scan(n, &size);
-      if (tid < kRankPad) s_id[size + tid] = 0x7FFFFFFF;
-#pragma unroll
-      for (int c = 0; c < kRankEach; ++c)
-        if (in[c]) s_id[place++] = (int)~(unsigned)x[c];
-      __syncthreads();
-      int lower[kRankEach] = {};
-      for (int j = 0; j < size; j += kRankPad) {
-        int other[kRankPad];
-#pragma unroll
-        for (int i = 0; i < kRankPad; ++i) other[i] = s_id[j + i];
-#pragma unroll
-        for (int i = 0; i < kRankPad; ++i)
-#pragma unroll
-          for (int c = 0; c < kRankEach; ++c) lower[c] += other[i] < (int)~(unsigned)x[c];
-      }
+      const int ends = power_of(size);
 #pragma unroll
       for (int c = 0; c < kRankEach; ++c)
         if (in[c]) {
-          s_run[lower[c]] = w[c];
-          s_key[lower[c]] = x[c];
+          s_run[place] = w[c];
+          s_ranked[place] = ((x[c] & 0xFFFFFFFFull) << 32) | (unsigned)place;
+          ++place;
         }
+      for (int i = size + tid; i < ends; i += kPickThreads) s_ranked[i] = 0ull;
       if (tid == 0) s_found[0] = 0x7FFFFFFF;
-      __syncthreads();
+      sort_down(s_ranked, ends);
       double v[kRankEach];
       int last = -1;
       sum = 0.0;
 #pragma unroll
       for (int c = 0; c < kRankEach; ++c) {
         const int i = kRankEach * tid + c;
-        v[c] = i < size ? s_run[i] : 0.0;
+        v[c] = i < size ? s_run[(unsigned)s_ranked[i]] : 0.0;
         sum += v[c];
         if (v[c] > 0.0) last = i;
       }
@@ -983,7 +1092,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
       }
       __syncthreads();
       const int who = s_found[0] < last ? s_found[0] : last;
-      finish((int)~(unsigned)s_key[who], total);
+      finish((int)~(unsigned)(s_ranked[who] >> 32), total);
       return;
     }
   }
@@ -993,25 +1102,14 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
     __shared__ unsigned s_bins[kBins];
     __shared__ unsigned long long s_between[kPickWaves * kBinHeld];
     Wide<kBf16, kRagged> wide{pick, s_bins, s_between};
-    const Border e = wide.border(row_mass);
-    auto kept = [&](float z, int id) {
-      const unsigned o = order_of(z);
-      if (!(o > e.order || (o == e.order && id <= e.id))) return 0.0;
-      const double w = pick.weight(z);
-      return w >= (double)plan.min_p ? w : 0.0;
-    };
-    // the support's mass segment by segment, in place of the whole one's
-    for (int g = __builtin_amdgcn_readfirstlane(tid / kWave); g < p.n_segs; g += kPickWaves) {
-      double s = 0.0;
-      if (order_of(p.seg_max[first + g]) >= e.order) {
-        pick.each_of(g, [&](float z, int id, bool own) { s += own ? kept(z, id) : 0.0; });
-        s = wave_sum64(s);
-      }
-      if ((tid & (kWave - 1)) == 0) p.seg_mass[first + g] = s;
-    }
-    __syncthreads();
-    const int id = pick.by_segment([&](double all) { return u * all; },
-                                   [&](int g) { return p.seg_mass[first + g]; }, kept, &total);
+    const Border e = wide.support(row_mass);
+    const int id = pick.by_segment(
+        [&](double all) { return u * all; }, [&](int g) { return p.seg_mass[first + g]; },
+        [&](float z, int i) {
+          const double w = wide.inside(e, order_of(z), i) ? pick.weight(z) : 0.0;
+          return w >= (double)plan.min_p ? w : 0.0;
+        },
+        &total);
     finish(id, total);
   }
 }
