@@ -394,7 +394,38 @@ struct Pick {
   double* held;           // LDS, 1 + kPickWaves
 
   __device__ __forceinline__ double weight(float z) const { return pow2(((double)z - (double)m) * plan.rate); }
+  // the same of logits whose weight is 2^-1000 at least
+  __device__ __forceinline__ double weight_tame(float z) const {
+    return pow2_tame(((double)z - (double)m) * plan.rate);
+  }
 
+  // Goes through the row, a wave a segment in turn, the next one on its way: hands each
+  // lane's packs to use(values, -inf for those that are not own ones, the id of the first),
+  // and after a segment calls end(g).
+  template <typename F, typename E>
+  __device__ __forceinline__ void walk(F use, E end) const {
+    typename R::P x[R::kPacks], next[R::kPacks];
+    int at[R::kPacks];
+    unsigned bits[R::kPacks];
+    int g = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (g < p.n_segs) row.load(g, next, at, bits);
+#pragma unroll 1
+    for (; g < p.n_segs; g += kPickWaves) {
+#pragma unroll
+      for (int q = 0; q < R::kPacks; ++q) x[q] = next[q];
+      if (g + kPickWaves < p.n_segs) row.load(g + kPickWaves, next, at, bits);
+#pragma unroll
+      for (int q = 0; q < R::kPacks; ++q) {
+        at[q] = row.place(g, q, bits[q]);
+        float z[R::kEpv];
+#pragma unroll
+        for (int j = 0; j < R::kEpv; ++j) z[j] = (bits[q] >> j) & 1u ? x[q].get(j) : -INFINITY;
+        use(z, at[q]);
+        __builtin_amdgcn_sched_barrier(0);  // not all packs' 64-bit numbers at once
+      }
+      end(g);
+    }
+  }
   // Hands the elements of segment g to use(value, id, whether it is an own one) in all lanes.
   template <typename F>
   __device__ __forceinline__ void each_of(int g, F use) const {
@@ -513,8 +544,9 @@ struct Pick {
 // The support of a row at large.
 template <bool kBf16, bool kRagged>
 struct Wide {
+  using R = Row<kBf16, kRagged>;
   Pick<kBf16, kRagged>& row;
-  unsigned* bins;               // LDS, kBins
+  unsigned* bins;               // LDS, kBins + kWave
   unsigned long long* between;  // LDS, kPickWaves x kBinHeld
 
   // What locate() found last: its elements between two edges, in their lanes' hands (of a
@@ -550,10 +582,9 @@ struct Wide {
       int shift = 0;
       while ((hi - lo) >> shift >= kBins) ++shift;
       const float per = (float)fmin(row.plan.rate * (1.0 / kWidth), 3e38);
-      auto coordinate = [&](float z) { return (row.m - z) * per; };
-      auto bin_of = [&](unsigned o) {
-        if (level > 0) return (int)((hi - o) >> shift);
-        const float x = coordinate(logit_of(o));
+      auto bin_of = [&](float z) {
+        if (level > 0) return (int)((hi - order_of(z)) >> shift);
+        const float x = (row.m - z) * per;
         return x < kBins - 1 ? (int)x : kBins - 1;
       };
       // the least order in bins up to b
@@ -562,7 +593,7 @@ struct Wide {
         unsigned t = lo, n = hi - lo;
         while (n > 0) {  // (the order hi is in bin 0)
           const unsigned half = n / 2;
-          if (bin_of(t + half) <= b) {
+          if (bin_of(logit_of(t + half)) <= b) {
             n = half;
           } else {
             t += half + 1u;
@@ -577,15 +608,34 @@ struct Wide {
       // of masses in parts of the weight at the bin's edge, as many as all elements together
       // leave room for
       const float part = fminf(2147483648.0f / p.vocab, 65536.0f);
-      row.each(lo, [&](float z, int, bool own) {
-        const unsigned o = order_of(z);
-        if (!own || o < lo || o > hi) return;
-        const int b = bin_of(o);
-        unsigned n = 1;
-        if (!kCount && level == 0) n = (unsigned)fmaf(part, exp2_fast((b - coordinate(z)) * kWidth), 0.5f);
-        unsigned* const slot = bins + b;
-        atomicAdd(slot, n);
-      });
+      // (what is not looked at goes to bins of the lanes' own, which takes no branch)
+      const float from = logit_of(lo), to = logit_of(hi);
+      auto fill = [&](auto first) {
+        constexpr bool kFirst = decltype(first)::value;
+        row.walk(
+            [&](const float (&z)[R::kEpv], int) {
+#pragma unroll
+            for (int j = 0; j < R::kEpv; ++j) {
+              unsigned n = 1;
+              int b;
+              if constexpr (kFirst) {
+                // (2^-x within a bin by its chord)
+                const float x = fminf((row.m - z[j]) * per, (float)(kBins - 1));
+                b = (int)x;
+                if constexpr (!kCount)
+                  n = (unsigned)fmaf(x - truncf(x), part * -0.04239f, part + 0.5f);
+                b = z[j] >= from ? b : kBins + lane;
+              } else {
+                b = z[j] >= from && z[j] <= to ? (int)((hi - order_of(z[j])) >> shift) : kBins + lane;
+              }
+              unsigned* const slot = bins + b;
+              atomicAdd(slot, n);
+            }
+            },
+            [](int) {});
+      };
+      if (level == 0) fill(std::true_type{});
+      else fill(std::false_type{});
       __syncthreads();
       double v[2];
       int filled = -1;
@@ -617,36 +667,56 @@ struct Wide {
       for (;;) {
         // what lies above the bin, segment by segment, and its elements
         const unsigned upper = edge(bin - 1), lower = edge(bin);
+        const float upper_z = logit_of(upper), lower_z = logit_of(lower);
+        const bool tame = ((double)row.m - (double)lower_z) * row.plan.rate < 1000.0;
         double sum[2] = {0.0, 0.0};
         int held = 0;  // of this wave
         int least = 0x7FFFFFFF, most = -0x7FFFFFFF - 1;
-        for (int g = wave(); g < p.n_segs; g += kPickWaves) {
-          double mine = 0.0;
-          if (order_of(p.seg_max[row.first + g]) >= lower)
-            row.each_of(g, [&](float z, int i, bool own) {
-              const unsigned o = order_of(z);
-              const bool in = own && o >= lower && o < upper;
-              const double v = kCount ? 1.0 : row.weight(z);
-              mine += own && o >= upper ? v : 0.0;
-              sum[1] += in ? v : 0.0;
-              const unsigned long long who = __ballot(in);
-              if (who) {
-                if (in) {
+        double mine = 0.0;
+        auto add = [&](auto tamed) {
+          row.walk(
+              [&](const float (&z)[R::kEpv], int i) {
+                unsigned in = 0;
+#pragma unroll
+                for (int j = 0; j < R::kEpv; ++j) {
+                  const bool above = z[j] >= upper_z, here = z[j] >= lower_z && !above;
+                  double v = 1.0;
+                  if constexpr (!kCount) {
+                    const float near = fmaxf(z[j], lower_z);  // others' weights are not used
+                    if constexpr (decltype(tamed)::value) v = row.weight_tame(near);
+                    else v = row.weight(near);
+                  }
+                  mine += above ? v : 0.0;
+                  sum[1] += here ? v : 0.0;
+                  in |= here ? 1u << j : 0u;
+                }
+                if (!__any(in != 0u)) return;
+                int all;
+                int to = held + wave_exclusive_dpp(__popc(in), &all);
+                held += all;
+                for (; in; in &= in - 1, ++to) {
+                  const int j = __ffs((int)in) - 1;
+                  float one = z[0];
+#pragma unroll
+                  for (int k = 1; k < R::kEpv; ++k) one = k == j ? z[k] : one;
+                  const unsigned o = order_of(one);
                   const int so = signed_order(o);
                   least = so < least ? so : least;
                   most = so > most ? so : most;
-                  const int to = held + __popcll(who & ((1ull << lane) - 1ull));
-                  if (to < kBinHeld) between[wave() * kBinHeld + to] = ((unsigned long long)o << 32) | (unsigned)i;
+                  if (to < kBinHeld) between[wave() * kBinHeld + to] = ((unsigned long long)o << 32) | (unsigned)(i + j);
                 }
-                held += __popcll(who);
-              }
-            });
-          sum[0] += mine;
-          if constexpr (!kCount) {
-            mine = wave_sum64(mine);
-            if (lane == 0) p.seg_mass[row.first + g] = mine;
-          }
-        }
+              },
+              [&](int g) {
+                sum[0] += mine;
+                if constexpr (!kCount) {
+                  mine = wave_sum64(mine);
+                  if (lane == 0) p.seg_mass[row.first + g] = mine;
+                }
+                mine = 0.0;
+              });
+        };
+        if (tame) add(std::true_type{});
+        else add(std::false_type{});
         group.sums(sum);
         const double before = sum[0];
         if (moved <= 0 && bin > 0 && before >= target) {
@@ -1099,7 +1169,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   if constexpr (!kWide) {
     if (tid == 0) p.todo[row] = 1;
   } else {
-    __shared__ unsigned s_bins[kBins];
+    __shared__ unsigned s_bins[kBins + kWave];
     __shared__ unsigned long long s_between[kPickWaves * kBinHeld];
     Wide<kBf16, kRagged> wide{pick, s_bins, s_between};
     const Border e = wide.support(row_mass);
