@@ -140,10 +140,40 @@ struct Row {
   }
 };
 
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+// The sum of a wave's lanes up to and with this one, by data-parallel moves between lanes
+// (through LDS a step takes ten times as long), and of all lanes.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double lane_move64(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), kCtrl, kRows, 0xF, false),
+                          __builtin_amdgcn_update_dpp(0, __double2loint(v), kCtrl, kRows, 0xF, false));
+}
+__device__ __forceinline__ double wave_scan64(double v) {
+  v += lane_move64<0x111, 0xF>(v);  // row_shr:1, 2, 4, 8
+  v += lane_move64<0x112, 0xF>(v);
+  v += lane_move64<0x114, 0xF>(v);
+  v += lane_move64<0x118, 0xF>(v);
+  v += lane_move64<0x142, 0xA>(v);  // row_bcast:15 into rows 1 and 3
+  v += lane_move64<0x143, 0xC>(v);  // row_bcast:31 into rows 2 and 3
   return v;
+}
+__device__ __forceinline__ double last_lane64(double v) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), kWave - 1),
+                          __builtin_amdgcn_readlane(__double2loint(v), kWave - 1));
+}
+__device__ __forceinline__ double wave_sum64(double v) { return last_lane64(wave_scan64(v)); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int larger_of_lane(int v) {
+  const int u = __builtin_amdgcn_update_dpp(v, v, kCtrl, kRows, 0xF, false);
+  return u > v ? u : v;
+}
+__device__ __forceinline__ int wave_largest(int v) {
+  v = larger_of_lane<0x111, 0xF>(v);
+  v = larger_of_lane<0x112, 0xF>(v);
+  v = larger_of_lane<0x114, 0xF>(v);
+  v = larger_of_lane<0x118, 0xF>(v);
+  v = larger_of_lane<0x142, 0xA>(v);
+  v = larger_of_lane<0x143, 0xC>(v);
+  return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 
 // The largest of three, NaN where one is.
@@ -287,11 +317,7 @@ struct Group {
   __device__ __forceinline__ double scan(double v, double* total) {
     turn ^= 1;
     const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const double u = __shfl_up(v, o, kWave);
-      if (lane >= o) v += u;
-    }
+    v = wave_scan64(v);
     if (lane == kWave - 1) lds[turn][wid] = v;
     __syncthreads();
     double before = 0.0, all = 0.0;
@@ -324,11 +350,7 @@ struct Group {
   }
   __device__ __forceinline__ int largest(int v) {
     turn ^= 1;
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      const int u = __shfl_xor(v, o, kWave);
-      v = u > v ? u : v;
-    }
+    v = wave_largest(v);
     if ((threadIdx.x & (kWave - 1)) == 0) ilds[turn][threadIdx.x / kWave] = v;
     __syncthreads();
     int m = ilds[turn][0];
@@ -510,12 +532,7 @@ struct Pick {
         if (w[j] > 0.0) end = at + j;
         if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
-      upto_lane = s;
-#pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const double t = __shfl_up(upto_lane, o, kWave);
-        if (lane >= o) upto_lane += t;
-      }
+      upto_lane = wave_scan64(s);
       if (lane == kWave - 1) held[1 + q] = upto_lane;
     }
     if (threadIdx.x == 0) found[2] = 0x7FFFFFFF;
