@@ -188,81 +188,81 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
   using R = Row<kBf16, kRagged>;
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.hdr->err_key = kNoError;
-  const long long tasks = (long long)p.n_rows * p.n_segs;
-  for (long long task = (long long)blockIdx.x * kScanWaves + wid; task < tasks;
-       task += (long long)gridDim.x * kScanWaves) {
-    const long long row = task / p.n_segs;
-    const int g = (int)(task - row * p.n_segs);
-    if (p.mask && !p.mask[row]) continue;
-    const Plan plan = plan_of(p, row);
-    if (plan.bad) continue;
-    const R r(p, row);
-    typename R::P x[R::kPacks];
-    int at[R::kPacks];
-    unsigned bits[R::kPacks];
-    r.load(g, x, at, bits);
-    auto sums = [&](auto edge) {
-      constexpr bool kEdge = decltype(edge)::value;
-      auto value = [&](int q, int j) {
-        return !kEdge || ((bits[q] >> j) & 1u) ? x[q].get(j) : -INFINITY;
-      };
-      float best = -INFINITY;
+  if (p.first_row == 0 && blockIdx.x == 0 && threadIdx.x == 0) p.hdr->err_key = kNoError;
+  // a segment a wave: task = row of this launch x segment
+  const unsigned index = blockIdx.x * kScanWaves + wid;
+  const unsigned of_launch = index / (unsigned)p.n_segs;
+  const int g = (int)(index - of_launch * (unsigned)p.n_segs);
+  const long long row = p.first_row + of_launch;
+  if (row >= p.n_rows || (p.mask && !p.mask[row])) return;
+  const long long task = row * p.n_segs + g;
+  const Plan plan = plan_of(p, row);
+  if (plan.bad) return;
+  const R r(p, row);
+  typename R::P x[R::kPacks];
+  int at[R::kPacks];
+  unsigned bits[R::kPacks];
+  r.load(g, x, at, bits);
+  auto sums = [&](auto edge) {
+    constexpr bool kEdge = decltype(edge)::value;
+    auto value = [&](int q, int j) {
+      return !kEdge || ((bits[q] >> j) & 1u) ? x[q].get(j) : -INFINITY;
+    };
+    float best = -INFINITY;
 #pragma unroll
-      for (int q = 0; q < R::kPacks; ++q) {
+    for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
-        for (int j = 0; j < R::kEpv; j += 2) best = most3(best, value(q, j), value(q, j + 1));
-        x[q].fence();
-      }
-      const bool none = __any(best != best);  // one is no number
-      if (plan.filtered) p.unit[task * kWave + lane] = (unsigned short)(order_of(best) >> 16);
-      const float m = none ? __builtin_nanf("") : wave_max_dpp(best);
-      double mass = 0.0;
-      float sum = 0.0f;
-      const bool numbers = fabsf(m) < INFINITY;
-      if (plan.mass && numbers) {
-        const double shift = -(double)m * plan.rate;
-        if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0) {
-          // x = z rate - m rate: the product of the maximum is rounded (1e-13 at most, the
-          // same for the whole segment).  Nothing below 2^-1000 counts, nor does it here.
-          const float low = (float)((double)m - 1000.0 / plan.rate);
+      for (int j = 0; j < R::kEpv; j += 2) best = most3(best, value(q, j), value(q, j + 1));
+      x[q].fence();
+    }
+    const bool none = __any(best != best);  // one is no number
+    if (plan.filtered) p.unit[task * kWave + lane] = (unsigned short)(order_of(best) >> 16);
+    const float m = none ? __builtin_nanf("") : wave_max_dpp(best);
+    double mass = 0.0;
+    float sum = 0.0f;
+    const bool numbers = fabsf(m) < INFINITY;
+    if (plan.mass && numbers) {
+      const double shift = -(double)m * plan.rate;
+      if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0) {
+        // x = z rate - m rate: the product of the maximum is rounded (1e-13 at most, the
+        // same for the whole segment).  Nothing below 2^-1000 counts, nor does it here.
+        const float low = (float)((double)m - 1000.0 / plan.rate);
 #pragma unroll
-          for (int q = 0; q < R::kPacks; ++q) {
+        for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
-            for (int j = 0; j < R::kEpv; ++j) {
-              mass += pow2_tame(fma((double)fmaxf(value(q, j), low), plan.rate, shift));
-              if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // not all 64-bit numbers at once
-            }
-            x[q].fence();
+          for (int j = 0; j < R::kEpv; ++j) {
+            mass += pow2_tame(fma((double)fmaxf(value(q, j), low), plan.rate, shift));
+            if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // not all 64-bit numbers at once
           }
-        } else {
-#pragma unroll
-          for (int q = 0; q < R::kPacks; ++q)
-#pragma unroll
-            for (int j = 0; j < R::kEpv; ++j) {
-              mass += pow2(((double)value(q, j) - (double)m) * plan.rate);
-              __builtin_amdgcn_sched_barrier(0);
-            }
+          x[q].fence();
         }
-        mass = wave_sum64(mass);
-      }
-      if (p.logp && numbers && !(plan.mass && plan.rate == kLog2e64)) {
+      } else {
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q)
 #pragma unroll
-          for (int j = 0; j < R::kEpv; ++j) sum += exp2_fast((value(q, j) - m) * kLog2e);
-        sum = wave_sum_dpp(sum);
+          for (int j = 0; j < R::kEpv; ++j) {
+            mass += pow2(((double)value(q, j) - (double)m) * plan.rate);
+            __builtin_amdgcn_sched_barrier(0);
+          }
       }
-      if (lane == 0) {
-        p.seg_max[task] = m;
-        p.seg_sum[task] = sum;
-        p.seg_mass[task] = mass;
-      }
-    };
-    const int first = g * kSegElems - r.pre;
-    if (first >= 0 && first + kSegElems <= p.vocab) sums(std::false_type{});
-    else sums(std::true_type{});
-  }
+      mass = wave_sum64(mass);
+    }
+    if (p.logp && numbers && !(plan.mass && plan.rate == kLog2e64)) {
+#pragma unroll
+      for (int q = 0; q < R::kPacks; ++q)
+#pragma unroll
+        for (int j = 0; j < R::kEpv; ++j) sum += exp2_fast((value(q, j) - m) * kLog2e);
+      sum = wave_sum_dpp(sum);
+    }
+    if (lane == 0) {
+      p.seg_max[task] = m;
+      p.seg_sum[task] = sum;
+      p.seg_mass[task] = mass;
+    }
+  };
+  const int first = g * kSegElems - r.pre;
+  if (first >= 0 && first + kSegElems <= p.vocab) sums(std::false_type{});
+  else sums(std::true_type{});
 }
 
 // ---------------------------------------------------------------------------
@@ -1208,22 +1208,24 @@ constexpr int kPickApart = 256;  // rows: one for each compute unit
 
 hipError_t launch_sample(const SampleParams& given, hipStream_t s) {
   SampleParams p = given;
-  const long long tasks = (long long)p.n_rows * p.n_segs;
-  const long long blocks = (tasks + kScanWaves - 1) / kScanWaves;
-  const int grid = (int)(blocks < 1 ? 1 : blocks < 2048 ? blocks : 2048);
   // Batches that fill the card more than once leave the rows that need it to a kernel of
   // their own, whose registers would leave room for few workgroups of all.
   const bool apart = p.n_rows > kPickApart;
   if (!apart) p.todo = nullptr;
+  // rows of a launch, whose waves are fewer than 2^25
+  const long long by_waves = (1 << 25) / p.n_segs;
+  const long long most = by_waves < kPickGrid ? by_waves : kPickGrid;
 #define TURNKL_SAMPLE(B, R)                                                         \
   if ((p.bf16 != 0) == B && (p.ragged != 0) == R) {                                 \
-    sample_scan<B, R><<<grid, kScanThreads, 0, s>>>(p);                             \
-    for (p.first_row = 0; p.first_row < p.n_rows; p.first_row += kPickGrid) {       \
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;              \
+    for (p.first_row = 0; p.first_row == 0 || p.first_row < p.n_rows; p.first_row += most) { \
       const long long left = p.n_rows - p.first_row;                                \
-      const int rows = (int)(left < kPickGrid ? left : kPickGrid);                  \
-      if (apart) sample_pick<B, R, false><<<rows, kPickThreads, 0, s>>>(p);         \
-      if (!apart || p.any_filter) sample_pick<B, R, true><<<rows, kPickThreads, 0, s>>>(p); \
+      const long long rows = left < most ? left : most;                             \
+      const long long waves = rows > 0 ? rows * p.n_segs : 1;                       \
+      sample_scan<B, R><<<(int)((waves + kScanWaves - 1) / kScanWaves), kScanThreads, 0, s>>>(p); \
+      if (hipError_t e = hipGetLastError(); e != hipSuccess || rows == 0) return e; \
+      if (apart) sample_pick<B, R, false><<<(int)rows, kPickThreads, 0, s>>>(p);    \
+      if (!apart || p.any_filter) sample_pick<B, R, true><<<(int)rows, kPickThreads, 0, s>>>(p); \
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;              \
     }                                                                               \
   }
   TURNKL_SAMPLE(true, false) TURNKL_SAMPLE(true, true) TURNKL_SAMPLE(false, false) TURNKL_SAMPLE(false, true)
