@@ -391,9 +391,11 @@ __global__ __launch_bounds__(kThreads) void block_norm_bwd_rows(BlockNormParams 
   float sw[kUnits][kEl], sb[kUnits][kEl], sp[kUnits][kEl], sg[kUnits][kEl];
   auto parameters = [&](int q) {
     const int i = kHold ? q : 0;
-    load_vector<kRagged>(p.weight, p.param_bf16, 1.0f, r.at[q], p.width, w[i]);
-    if constexpr (kPost) load_vector<kRagged>(p.post_weight, p.param_bf16, 1.0f, r.at[q], p.width, wp[i]);
-    if constexpr (!kGateMatrix) load_vector<kRagged>(p.gate, p.param_bf16, 1.0f, r.at[q], p.width, gv[i]);
+    Place<kEl> at = r.at[q];
+    if constexpr (!kHold) asm volatile("" : "+v"(at.at));  // addresses made here, not held over the rows
+    load_vector<kRagged>(p.weight, p.param_bf16, 1.0f, at, p.width, w[i]);
+    if constexpr (kPost) load_vector<kRagged>(p.post_weight, p.param_bf16, 1.0f, at, p.width, wp[i]);
+    if constexpr (!kGateMatrix) load_vector<kRagged>(p.gate, p.param_bf16, 1.0f, at, p.width, gv[i]);
   };
 #pragma unroll
   for (int q = 0; q < kUnits; ++q) {

@@ -87,7 +87,7 @@ SampleLayout sample_layout(int64_t n_tokens, int64_t vocab) {
   L.mass = align256(sizeof(Header));
   L.most = align256(L.mass + segs * sizeof(double));
   L.sum = align256(L.most + segs * sizeof(float));
-  L.unit = align256(L.sum + segs * sizeof(float));
+  L.unit = align256(L.sum + segs * sizeof(double));
   L.todo = align256(L.unit + segs * 64 * sizeof(unsigned short));
   L.total = align256(L.todo + (size_t)n_tokens);
   return L;
@@ -403,7 +403,7 @@ int turnkl_sample_tokens(const void* logits, int64_t ld, int dtype, int64_t n_to
   p.hdr = reinterpret_cast<Header*>(ws);
   p.seg_mass = reinterpret_cast<double*>(ws + L.mass);
   p.seg_max = reinterpret_cast<float*>(ws + L.most);
-  p.seg_sum = reinterpret_cast<float*>(ws + L.sum);
+  p.seg_sum = reinterpret_cast<double*>(ws + L.sum);
   p.unit = reinterpret_cast<unsigned short*>(ws + L.unit);
   p.todo = reinterpret_cast<unsigned char*>(ws + L.todo);
   p.ld = ld;

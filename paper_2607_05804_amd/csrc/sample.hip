@@ -86,6 +86,17 @@ __device__ __forceinline__ double pow2_tame(double x) {
   return __hiloint2double(hi, __double2loint(f));
 }
 
+// e^x for x <= 0: 2^t for t = x log2 e, and the part of t that its rounding lost in the
+// slope of 2^t (an argument of -30 is rounded by up to 2^-20)
+__device__ __forceinline__ float exp_fast(float x) {
+  constexpr float kLow = (float)(kLog2e64 - (double)kLog2e);
+  x = fmaxf(x, -1e4f);  // 0 from there on, -inf included
+  const float t = x * kLog2e;
+  const float lost = fmaf(x, kLow, fmaf(x, kLog2e, -t));
+  const float e = exp2_fast(t);
+  return fmaf(e, lost * (float)kLn264, e);
+}
+
 // What a row's parameters ask for.
 struct Plan {
   double rate;      // log2 e / T
@@ -219,7 +230,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
     if (plan.filtered) p.unit[task * kWave + lane] = (unsigned short)(order_of(best) >> 16);
     const float m = none ? __builtin_nanf("") : wave_max_dpp(best);
     double mass = 0.0;
-    float sum = 0.0f;
+    double sum = 0.0;
     const bool numbers = fabsf(m) < INFINITY;
     if (plan.mass && numbers) {
       const double shift = -(double)m * plan.rate;
@@ -248,11 +259,17 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
       mass = wave_sum64(mass);
     }
     if (p.logp && numbers && !(plan.mass && plan.rate == kLog2e64)) {
+      // 32-bit exponentials of arguments with their rounding, added in 64 bits: where one
+      // token has nearly all of a row, log p is what the others add to 1
 #pragma unroll
-      for (int q = 0; q < R::kPacks; ++q)
+      for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
-        for (int j = 0; j < R::kEpv; ++j) sum += exp2_fast((value(q, j) - m) * kLog2e);
-      sum = wave_sum_dpp(sum);
+        for (int j = 0; j < R::kEpv; ++j) {
+          sum += (double)exp_fast(value(q, j) - m);
+          if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      sum = wave_sum64(sum);
     }
     if (lane == 0) {
       p.seg_max[task] = m;
@@ -816,12 +833,12 @@ struct Wide {
       if (order_of(p.seg_max[row.first + g]) >= o)
         row.each_of(g, [&](float z, int, bool own) { equal += own && order_of(z) == o; });
       wave_exclusive_dpp(equal, &equal);
-      if ((threadIdx.x & (kWave - 1)) == 0) p.seg_sum[row.first + g] = (float)equal;
+      if ((threadIdx.x & (kWave - 1)) == 0) p.seg_sum[row.first + g] = (double)equal;
     }
     __syncthreads();
     double all;
     const int x = row.by_segment([&](double) { return n - 1.0; },
-                                 [&](int g) { return (double)p.seg_sum[row.first + g]; },
+                                 [&](int g) { return p.seg_sum[row.first + g]; },
                                  [&](float z, int) { return order_of(z) == o ? 1.0 : 0.0; }, &all);
     return all <= n ? 0x7FFFFFFF : x;
   }
@@ -941,8 +958,8 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   const bool few = units <= kUnitEach * kPickThreads;
   // what the row's segments left, and its units, on their way together
   const bool one_each = p.n_segs <= kPickThreads;
-  float seg_max = -INFINITY, seg_sum = 0.0f;
-  double seg_mass = 0.0;
+  float seg_max = -INFINITY;
+  double seg_sum = 0.0, seg_mass = 0.0;
   if (one_each && tid < p.n_segs) {
     seg_max = p.seg_max[first + tid];
     seg_sum = p.seg_sum[first + tid];
@@ -962,7 +979,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   };
   // the row's maximum (above all numbers where one is none)
   int top = signed_order(kNothing);
-  each_segment([&](float x, float, double) {
+  each_segment([&](float x, double, double) {
     const int o = x == x ? signed_order(order_of(x)) : 0x7FFFFFFF;
     top = o > top ? o : top;
   });
@@ -979,7 +996,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   Pick<kBf16, kRagged> pick{p, R(p, row), plan, group, first, m, s_found, s_held};
   const bool same = plan.mass && plan.rate == kLog2e64;
   double both[2] = {0.0, 0.0};  // sums at temperature 1 and at the row's
-  each_segment([&](float x, float s, double w) {
+  each_segment([&](float x, double s, double w) {
     if (p.logp && !same) both[0] += s * pow2(((double)x - m) * kLog2e64);
     if (plan.mass) both[1] += w * pick.weight(x);
   });

@@ -609,7 +609,7 @@ struct SampleParams {
   float* logp;
   Header* hdr;
   float* seg_max;                   // [n_rows][n_segs] each
-  float* seg_sum;                   // of exp(z - maximum)
+  double* seg_sum;                  // of exp(z - maximum)
   double* seg_mass;                 // of exp((z - maximum) / T)
   unsigned short* unit;             // [n_rows][n_segs][64] orders of lanes' maxima, upper halves
   unsigned char* todo;              // [n_rows] rows left to a second kernel, or null
