@@ -880,7 +880,8 @@ def sample_tokens(logits: torch.Tensor, uniforms: torch.Tensor, *, temperature: 
         if isinstance(x, torch.Tensor):
             setattr(given, "row_" + name, _per_row(x, n, name, index, dtype))
         else:
-            setattr(given, name, x)
+            # (as many as the field can hold are more than any row has)
+            setattr(given, name, min(max(x, -2 ** 31), 2 ** 31 - 1) if name == "top_k" else x)
     u_at = _per_row(uniforms, n, "uniforms", index, torch.float64)
     mask_at = _per_row(mask, n, "mask", index, torch.uint8)
     if out is None:

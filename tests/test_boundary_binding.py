@@ -68,3 +68,19 @@ def test_buffers_for_gradients():
     assert T.new_block_norm_grads(3, 8, gate="vector", weight=False, device="cpu").gate.shape == (8,)
     with pytest.raises(ValueError):
         T.new_block_norm_grads(3, 8, gate="scalar", device="cpu")
+
+
+@pytest.mark.parametrize("given,passed", [(0, 0), (7, 7), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 32 + 5, 2 ** 31 - 1),
+                                          (-2 ** 40, -2 ** 31)])
+def test_top_k_does_not_wrap(given, passed, library, monkeypatch):  # noqa: F811
+    seen = []
+
+    def call(*a):
+        seen.extend(x.top_k for x in a if isinstance(x, T.Sampling))
+        return T.OK
+
+    library.turnkl_sample_tokens = call
+    T.sample_tokens(X, U, top_k=given, check=False)
+    assert seen == [passed]
+    with pytest.raises(TypeError):
+        T.sample_tokens(X, U, top_k=2.5, check=False)
