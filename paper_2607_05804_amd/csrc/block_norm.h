@@ -12,7 +12,12 @@
 // after the other (layer: mean first, then squared differences).  Rows of up to 64 units
 // share a wave, as many as fit; others take a workgroup each.  Workgroups go from row to
 // row with the next row on its way, and keep parameters and, backward, their columns' sums
-// in registers; a second kernel adds the workgroups' sums in their order.  Bound: HBM.
+// in registers; a second kernel adds the workgroups' sums in their order.
+//
+// Bound: HBM.  65,536 bf16 rows of 4,096 with both norms and a vector's gate, forward: 428
+// us, 5.0 TB/s over two streams in and two out, as a copy; backward 32,768 of them: 363 us,
+// 4.4 TB/s over five streams, one workgroup of 162 VGPRs a CU and more of eight waves not
+// fitting (at 128 VGPRs it spills: 1,033).  64 rows of 2,048: 4 us, two chains of sums.
 #pragma once
 
 #include "units.h"

@@ -35,9 +35,14 @@ constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / kWave;
 constexpr int kRankEach = 2;                           // of a thread
 constexpr int kRanked = kRankEach * kPickThreads;      // candidates that are sorted
+constexpr int kUnitElems = kSegElems / kWave;
 constexpr int kUnitsHeld = 2048;  // units that are read again, at most
 constexpr int kUnitEach = 16;     // units of a thread that its registers hold
-constexpr int kWantByMass = 300;  // elements that are asked for where only top-p limits a row
+// Elements that are asked for where only top-p limits a row: 64 rows of 151,936 with settings
+// of their own take 173, 164 and 166 us with 400, 600 and 800 (with 300 units 172), 512 rows
+// of 32,000 at top-p 0.9 153, 126 and 133.  As many units would be more than a row of 5,752
+// has, whose candidates would then be all its elements: 39 such rows 53 us, for 28.
+constexpr double kWantByMass = 600;
 constexpr int kBins = 2 * kPickThreads;                // of the histogram
 constexpr int kBinEach = 8;                            // elements of a lane between two bins' edges
 constexpr int kBinHeld = kBinEach * kWave;             // of a wave
@@ -192,8 +197,10 @@ __device__ __forceinline__ float most3(float a, float b, float c) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
-// Bound: the 64-bit exponentials, some twenty operations an element (they run at the rate
-// of 32-bit ones here); HBM where only top-k or min-p limit the rows.
+// Bound: the 64-bit exponentials, some twenty operations an element (they run at the
+// rate of 32-bit ones here): 1,024 rows of 151,936 in 136 us, of which HBM would need 48;
+// of rows that only top-k or min-p limits log p's sum (300 fp32 rows of 50,257: 19 us).
+// The next task's loads ahead of a wave's sums gave nothing: other waves fill their time.
 template <bool kBf16, bool kRagged>
 __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
   using R = Row<kBf16, kRagged>;
@@ -917,6 +924,12 @@ struct Wide {
 
 // kWide: rows that the ranked candidates do not settle are finished here; otherwise they are
 // left to a second kernel, which (with p.todo) takes no others.
+//
+// Bound: the chain of its steps.  One row of 151,936, top 50: 14 us (a bound, its units read
+// again, two sorts in LDS and five scans over the workgroup).  Rows at large: 64 with
+// settings of their own 126 to 166 us, most of it the histogram's LDS atomics and the exact
+// sum's 64-bit exponentials over a row by one compute unit; 1,024 threads a row took 168 for
+// 150 then, and one row 28 for 24.
 template <bool kBf16, bool kRagged, bool kWide>
 __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(SampleParams p) {
   __shared__ double s_sum[2][kPickWaves * 3];
@@ -1032,7 +1045,7 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
     };
     // the want-th largest unit maximum bounds the elements that are needed: by how far the
     // maxima lie below the row's (1,023 orders or more in the last bin)
-    const int want = plan.k > 0 ? plan.k : by_mass ? kWantByMass : 0;
+    const int want = plan.k > 0 ? plan.k : by_mass ? p.units_by_mass : 0;
     unsigned bound = 0;
     if (want > 0 && want <= units) {
       const unsigned highest = order_of(m) >> 16;
@@ -1219,12 +1232,18 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
 }
 
 constexpr int kPickGrid = 1 << 20;  // rows of a launch
-constexpr int kPickApart = 256;  // rows: one for each compute unit
+// Rows: one for each compute unit.  Past it the rows at large are a kernel's of their own
+// (1,024 unfiltered rows of 151,936: 149 us so, 164 with all in one; 300 fp32 rows of 50,257
+// by min-p: 62 and 63).
+constexpr int kPickApart = 256;
 
 }  // namespace
 
 hipError_t launch_sample(const SampleParams& given, hipStream_t s) {
   SampleParams p = given;
+  // As many units as kWantByMass elements strewn among them would hit.
+  const double units = (p.vocab + kUnitElems - 1) / kUnitElems;
+  p.units_by_mass = (int)(units * -expm1(-kWantByMass / units));
   // Batches that fill the card more than once leave the rows that need it to a kernel of
   // their own, whose registers would leave room for few workgroups of all.
   const bool apart = p.n_rows > kPickApart;
