@@ -79,36 +79,47 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(EmbedParams p) {
 // zeroing the table beside the sort
 
 constexpr int kSortThreads = 512;
+constexpr int kFillLine = 128;  // bytes
+
+// 16 bytes of zeros at `from` of a run of `size` bytes, or as many of them as are its own.
+template <int kEs, typename Vec>
+__device__ __forceinline__ void zero_pack(char* run, long long size, long long from, bool stream) {
+  const Vec z = {0u, 0u, 0u, 0u};
+  if (from >= 0 && from + 16 <= size) {
+    if (stream) __builtin_nontemporal_store(z, reinterpret_cast<Vec*>(run + from));
+    else *reinterpret_cast<Vec*>(run + from) = z;
+  } else {
+    const long long end = from + 16 < size ? from + 16 : size;
+    for (long long b = from > 0 ? from : 0; b < end; b += kEs) {
+      if constexpr (kEs == 2) *reinterpret_cast<unsigned short*>(run + b) = 0;
+      else *reinterpret_cast<unsigned*>(run + b) = 0u;
+    }
+  }
+}
 
 // The share of one of the sort's launches in zeroing the whole table, by the workgroups
 // behind the p.n_tiles that sort: 16 bytes a thread, in address order, and nothing loaded
-// before (2.5 GB: 6.9 TB/s; longer-lived workgroups write 5.7).
+// before (2.5 GB: 6.9 TB/s; longer-lived workgroups write 5.7).  A table without padding is
+// one run.  With it a row's packs are counted from the line that it starts in, so that waves
+// write whole lines wherever rows start (93,051 bf16 rows of 6,688 at a stride of 6,782, with
+// 798 tokens: 287 us, 324 from the rows' starts; of one run the arithmetic would cost more
+// than it gives: 2.5 GB, with its sums, 650 us for 598).
 template <int kEs>
 __device__ inline void zero_share(const EmbedGradParams& p) {
   const unsigned per_row = p.fill_per_row;
-  const u32x4_any z = {0u, 0u, 0u, 0u};
+  char* const table = static_cast<char*>(p.table);
   const long long stride = (long long)(gridDim.x - p.n_tiles) * kSortThreads;
   for (long long i = p.fill_from + (long long)(blockIdx.x - p.n_tiles) * kSortThreads; i < p.fill_to; i += stride) {
-    // (of a table without padding per_row is 0: one row)
-    const long long row0 = per_row ? i / per_row : 0;
-    const long long q0 = i - row0 * per_row + threadIdx.x;
     if (i + threadIdx.x >= p.fill_to) continue;
-    long long row = row0, q = q0;
-    if (per_row) {
-      row += (unsigned)q0 / per_row;
-      q = (unsigned)q0 % per_row;
+    if (!per_row) {
+      zero_pack<kEs, u32x4_any>(table, p.fill_elems * kEs, (i + threadIdx.x) * 16, p.fill_stream);
+      continue;
     }
-    char* const at = static_cast<char*>(p.table) + row * p.ld_table * kEs + q * 16;
-    const long long rest = (per_row ? (long long)p.width : p.fill_elems) * kEs - q * 16;
-    if (rest >= 16) {
-      if (p.fill_stream) __builtin_nontemporal_store(z, reinterpret_cast<u32x4_any*>(at));
-      else *reinterpret_cast<u32x4_any*>(at) = z;
-    } else {
-      for (int j = 0; j < (int)rest / kEs; ++j) {
-        if constexpr (kEs == 2) reinterpret_cast<unsigned short*>(at)[j] = 0;
-        else reinterpret_cast<unsigned*>(at)[j] = 0u;
-      }
-    }
+    const long long row0 = i / per_row;
+    const unsigned q = (unsigned)(i - row0 * per_row) + threadIdx.x;
+    char* const row = table + (row0 + q / per_row) * p.ld_table * kEs;
+    const int skew = (int)(reinterpret_cast<uintptr_t>(row) & (kFillLine - 1));
+    zero_pack<kEs, u32x4>(row, (long long)p.width * kEs, (long long)(q % per_row) * 16 - skew, p.fill_stream);
   }
 }
 __device__ inline bool zeroes_instead(const EmbedGradParams& p) {
@@ -633,7 +644,7 @@ hipError_t launch_embed_bwd(const EmbedGradParams& given, hipStream_t s) {
   const int launches = small ? 1 : 2 * turns;
   long long packs = 0, fills = 0;  // of the table, and workgroups of a launch for them
   if (whole) {
-    const long long row = ((long long)p.width * es + 15) / 16;
+    const long long row = ((long long)p.width * es + 2 * kFillLine - 2) / kFillLine * (kFillLine / 16);
     p.fill_per_row = p.ld_table == p.width ? 0 : (unsigned)row;
     p.fill_elems = (long long)p.vocab * p.width;
     packs = p.fill_per_row ? row * p.vocab : (p.fill_elems * es + 15) / 16;

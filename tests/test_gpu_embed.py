@@ -326,3 +326,26 @@ def test_refusals(gpu):
         T.embed_bwd(rows(900, 8, "f32", 1), tokens(900, 9, 1), torch.empty((9, 8), device="cuda"),
                     workspace=T.EmbedWorkspace(1, 1, 1))
     assert e.value.code == T.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("n", [40, 3000])  # of both sorts
+@pytest.mark.parametrize("dtype,v,d,pad,start", [
+    ("bf16", 40001, 1003, 0, 0), ("bf16", 40001, 1003, 0, 5), ("bf16", 40001, 1003, 94, 0), ("bf16", 40000, 1001, 3, 7),
+    ("bf16", 600000, 61, 1, 3), ("f32", 20011, 1009, 0, 1), ("f32", 20011, 1009, 3, 2), ("f32", 20000, 1024, 32, 0),
+    ("bf16", 5000000, 7, 2, 1), ("f32", 17000000 // 4, 4, 1, 0)])
+def test_large_tables_are_zeroed_from_any_start(dtype, v, d, pad, start, n, gpu):
+    """Tables that are zeroed whole, lines that rows share included: the rows without a
+    token are zeros, those with one have their tokens' gradient, and nothing beside the rows
+    is written."""
+    table = rows(v, d, dtype, 1, pad=pad, start=start)
+    whole = torch.empty(0, dtype=DT[dtype], device="cuda").set_(table.untyped_storage())
+    whole.fill_(7.0)
+    g = torch.ones(n, d, device="cuda", dtype=DT[dtype])
+    ids = (torch.arange(n, device="cuda") * (v // n)).int()
+    ids[-1] = v - 1
+    T.embed_bwd(g, ids, table)
+    want = torch.zeros(v, device="cuda").index_add_(0, ids.long(), torch.ones(n, device="cuda")).to(DT[dtype])
+    assert torch.equal(table.amin(1), want) and torch.equal(table.amax(1), want)
+    if pad:
+        assert bool((torch.as_strided(whole, (v - 1, pad), (d + pad, 1), start + d) == 7.0).all())
+    assert bool((whole[:start] == 7.0).all()) and bool((whole[start + (v - 1) * (d + pad) + d:] == 7.0).all())
