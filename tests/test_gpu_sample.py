@@ -365,3 +365,24 @@ def test_refusals(gpu):
     with pytest.raises(T.TurnKLError) as e:
         T.sample_tokens(z, u, out=T.SampledTokens(torch.empty(4, dtype=torch.int32, device="cuda"), whole[:4], whole[2:6]))
     assert e.value.code == T.ERR_ALIAS
+
+
+@pytest.mark.parametrize("kw", [dict(top_k=50, temperature=0.7), dict(min_p=0.01), dict(temperature=1.3), dict()])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_log_p_of_a_token_with_nearly_all_of_a_row(dtype, kw, gpu):
+    """log p = -log(1 + s) for the others' sum s is accurate relative to itself.  The logits
+    are multiples of 1/8, so that their differences are exact: 2^-23 for an exponential,
+    2^-24 for its correction and for the output, and what the 64-bit sums add: 2^-21."""
+    n, v = 40, 20011
+    z = (torch.randn(n, v, device="cuda", generator=gen(5)) * 16).round().clamp(-64, 64) / 8
+    z[torch.arange(n), torch.arange(n) * 7] = torch.arange(n, device="cuda") / 8 + 17.0
+    z = z.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    u = torch.full((n,), 0.5, dtype=torch.float64, device="cuda")
+    got = T.sample_tokens(z, u, **kw)
+    ids = torch.arange(n, device="cuda") * 7
+    rest = z.double() - z.double().amax(1, keepdim=True)
+    rest[torch.arange(n), ids] = -math.inf
+    ref = -torch.log1p(rest.exp().sum(1))
+    assert bool((got.ids == ids).sum() > n // 2)
+    took = got.ids == ids
+    assert bool(((got.logp.double() - ref).abs() <= 2.0 ** -21 * ref.abs())[took].all())
