@@ -69,11 +69,17 @@ BlockShape block_norm_shape(long long n_rows, long long width, int el, bool bwd,
   return s;
 }
 
-hipError_t launch_block_norm(const BlockNormParams& p, bool bwd, hipStream_t s) {
-  const hipError_t e = p.branch_bf16 ? (p.residual_bf16 ? launch_block_norm_bf16(p, bwd, s)
-                                                        : launch_block_norm_mixed(p, bwd, s))
-                                     : launch_block_norm_f32(p, bwd, s);
-  if (e != hipSuccess || !bwd || !p.sums) return e;
+hipError_t launch_block_norm(const BlockNormParams& given, bool bwd, hipStream_t s) {
+  BlockNormParams p = given;
+  if (p.n_rows == 0) {
+    p.n_groups = 0;  // no row, no partial sums: the join's are zeros
+  } else {
+    const hipError_t e = p.branch_bf16 ? (p.residual_bf16 ? launch_block_norm_bf16(p, bwd, s)
+                                                          : launch_block_norm_mixed(p, bwd, s))
+                                       : launch_block_norm_f32(p, bwd, s);
+    if (e != hipSuccess) return e;
+  }
+  if (!bwd || !p.sums) return hipSuccess;
   block_norm_join<<<dim3((p.width + kWave - 1) / kWave, 4), kJoinThreads, 0, s>>>(p);
   return hipGetLastError();
 }

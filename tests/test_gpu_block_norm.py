@@ -447,3 +447,23 @@ def test_refusals(gpu):
         with pytest.raises(T.TurnKLError) as e:
             call()
         assert e.value.code == code, (e.value.code, code)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("d,post", [(40, True), (700, False), (4097, True), (8192, False), (8193, False), (16384, True)])
+def test_no_rows_of_every_form(d, post, types, gpu):
+    """The sums over no rows are zeros, or what was there, whatever the workspace holds."""
+    c = Case(0, d, types, 1, "vector", post)
+    hn, stats, post_stats = c.given()
+    ws = T.BlockNormWorkspace(300, d)
+    for accumulate in (False, True):
+        ws.tensor.fill_(0xFF)  # NaN
+        out = T.new_block_norm_grads(0, d, c.f.dtype, c.h.dtype, gate="vector", bias=True, post_weight=post)
+        sums = [x for x in out if x is not None and x.dim() == 1]
+        assert len(sums) == (4 if post else 3)
+        for x in sums:
+            x.copy_(torch.arange(d))
+        T.block_norm_bwd(c.gy, c.gh, hn, stats, c.f, c.w, post_stats=post_stats, out=out, accumulate=accumulate,
+                         workspace=ws, **c.kw())
+        for x in sums:
+            assert torch.equal(x, torch.arange(d, device="cuda") * (1.0 if accumulate else 0.0))
