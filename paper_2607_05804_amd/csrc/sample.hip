@@ -241,10 +241,12 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
     const bool numbers = fabsf(m) < INFINITY;
     if (plan.mass && numbers) {
       const double shift = -(double)m * plan.rate;
-      if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0) {
+      // Nothing below 2^-1000 counts: -inf is taken for this number.  (Where temperatures
+      // are so high that it has none, from 4.9e35, x would have to be -inf itself.)
+      const float low = (float)((double)m - 1000.0 / plan.rate);
+      if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0 && low > -INFINITY) {
         // x = z rate - m rate: the product of the maximum is rounded (1e-13 at most, the
-        // same for the whole segment).  Nothing below 2^-1000 counts, nor does it here.
-        const float low = (float)((double)m - 1000.0 / plan.rate);
+        // same for the whole segment)
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll

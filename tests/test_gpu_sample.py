@@ -386,3 +386,22 @@ def test_log_p_of_a_token_with_nearly_all_of_a_row(dtype, kw, gpu):
     assert bool((got.ids == ids).sum() > n // 2)
     took = got.ids == ids
     assert bool(((got.logp.double() - ref).abs() <= 2.0 ** -21 * ref.abs())[took].all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [50, 2048, 2049, 5000, 151936])
+def test_the_highest_temperatures(v, dtype, gpu):
+    """Forbidden tokens, and the places behind a row's end, weigh nothing where all others
+    weigh the same."""
+    n = 6
+    z = logits(n, v, dtype, v)
+    z[:, ::3] = -math.inf
+    z[2, 1:-1], z[2, -1] = -math.inf, 1.0
+    z[3] = logits(1, v, dtype, 1)[0]
+    z[4, -1] = -3e38
+    for heat in (4.7e35, 5e35, 1e36, 3e38, 3.4028234e38):
+        for i, kw in enumerate((dict(), dict(top_p=0.9), dict(top_k=9), dict(top_k=900, top_p=0.7), dict(min_p=0.3))):
+            check(z, uniforms(n, i), temperature=heat, **kw)
+        ends = torch.tensor([0.0, 1 - 2.0 ** -53] * (n // 2), dtype=torch.float64, device="cuda")
+        check(z, ends, temperature=heat)
+        check(z, ends, temperature=torch.full((n,), heat, device="cuda"), top_p=0.99)
