@@ -517,8 +517,11 @@ struct Pick {
     *total = all;
     const double target = target_of(all);
     last = group.largest(last);
+    // (A scan's sums are made in trees of their own: at a border the one of a thread without
+    // a share may pass it by a rounding.  Such threads, and below such segments and lanes,
+    // are never the place, so that a rounding leads to a border's other side at most.)
     int* const slot = found;
-    if (lo < hi && upto > target) atomicMin(slot, (int)threadIdx.x);
+    if (mine > 0.0 && upto > target) atomicMin(slot, (int)threadIdx.x);
     __syncthreads();
     const int who = *found;
     if (who == 0x7FFFFFFF) {  // past the end by a rounding
@@ -527,15 +530,18 @@ struct Pick {
         held[0] = -1.0;
       }
     } else if ((int)threadIdx.x == who) {
-      double run = upto - mine;
-      int g = lo;
-      for (; g < hi - 1; ++g) {
+      double run = upto - mine, before = run;
+      int at = lo;
+      for (int g = lo; g < hi; ++g) {
         const double s = share(g);
-        if (run + s > target) break;
+        if (!(s > 0.0)) continue;
+        at = g;
+        before = run;
         run += s;
+        if (run > target) break;
       }
-      found[1] = g;
-      held[0] = target - run;
+      found[1] = at;
+      held[0] = fmax(target - before, 0.0);
     }
     __syncthreads();
     const int g = found[1];
@@ -566,7 +572,7 @@ struct Pick {
     if (q < R::kPacks) {
       double run = 0.0;
       for (int i = 0; i < q; ++i) run += held[1 + i];
-      const unsigned long long past = __ballot(rest >= 0.0 && run + upto_lane > rest);
+      const unsigned long long past = __ballot(rest >= 0.0 && s > 0.0 && run + upto_lane > rest);
       if (past && lane == __ffsll((long long)past) - 1) {
         int got = -1;
         double t = run + (upto_lane - s);
@@ -1019,6 +1025,10 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
   const double row_mass = both[1], log_all = log(same ? both[1] : both[0]);
   auto finish = [&](int id, double total) {
     if (tid != 0) return;
+    if (id < 0) {  // (no sum leads here; nothing before the row would be read if one did)
+      write(-1, nan, nan);
+      return;
+    }
     const long long at = row * p.ld + id;
     const float z = kBf16 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p.z)[at] << 16)
                           : static_cast<const float*>(p.z)[at];

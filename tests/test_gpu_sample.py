@@ -405,3 +405,30 @@ def test_the_highest_temperatures(v, dtype, gpu):
         ends = torch.tensor([0.0, 1 - 2.0 ** -53] * (n // 2), dtype=torch.float64, device="cuda")
         check(z, ends, temperature=heat)
         check(z, ends, temperature=torch.full((n,), heat, device="cuda"), top_p=0.99)
+
+
+@pytest.mark.parametrize("n,repeats,kw", [
+    (3000, 2, dict()), (3000, 4, dict()), (200, 2, dict()), (3000, 2, dict(min_p=1e-5)), (250, 2, dict(min_p=1e-5)),
+    (3000, 4, dict(min_p=1e-5, temperature=1.7)), (40, 256, dict()), (40, 256, dict(min_p=1e-5))])
+def test_random_numbers_on_a_border_between_segments(n, repeats, kw, gpu):
+    """Rows of the same segments over and over, some of them without a token, and random
+    numbers that lie exactly between two repetitions: the first token behind the border
+    follows from the definition, the last one before it from a rounding; nothing else does.
+    256 repetitions are more segments than the workgroup that picks has threads."""
+    period, filled = 5, 3
+    v = repeats * period * 2048
+    z = torch.full((n, repeats, period * 2048), -math.inf, device="cuda")
+    each = 300 if repeats < 9 else 4
+    at = torch.rand((n, filled, 2048), generator=gen(repeats), device="cuda").topk(each, dim=2).indices
+    at += torch.arange(filled, device="cuda")[:, None] * 2048
+    at = at.reshape(n, 1, -1).expand(n, repeats, -1)
+    z.scatter_(2, at, (-2 * torch.rand((n, 1, filled * each), generator=gen(n), device="cuda")).expand(at.shape).contiguous())
+    first, last = at[:, 0].amin(1), at[:, 0].amax(1)
+    z = z.view(n, v)
+    for k in {1, repeats // 2, repeats - 1}:
+        u = torch.full((n,), k / repeats, dtype=torch.float64, device="cuda")
+        got = T.sample_tokens(z, u, **kw)
+        behind, before = first + k * period * 2048, last + (k - 1) * period * 2048
+        good = (got.ids == behind) | (got.ids == before)
+        assert bool(good.all()), (k, int((~good).sum()), got.ids[~good][:5].tolist(), behind[~good][:5].tolist())
+        assert bool((got.ids == behind).any())
