@@ -768,18 +768,22 @@ struct Wide {
         else add(std::false_type{});
         group.sums(sum);
         const double before = sum[0];
-        if (moved <= 0 && bin > 0 && before >= target) {
+        most = group.largest(most);
+        least = ~group.largest(~least);
+        // (A target between this bin's sums and the same elements' sum from the next bin on
+        // would end a search between the two, where the bin may be empty: the direction is
+        // kept until one is not, as the first and the last one are not.)
+        const bool empty = least > most;
+        if (moved <= 0 && bin > 0 && (before >= target || (empty && moved < 0))) {
           --bin;
           moved = -1;
           continue;
         }
-        if (moved >= 0 && bin < last && before + sum[1] < target) {
+        if (moved >= 0 && bin < last && (before + sum[1] < target || empty)) {
           ++bin;
           moved = 1;
           continue;
         }
-        most = group.largest(most);
-        least = ~group.largest(~least);
         by_segment = !kCount;
         in_hand = group.largest(held) <= kBinHeld;
         if (!in_hand) {
@@ -813,8 +817,9 @@ struct Wide {
           t |= (before + n[2] >= target ? 3u : before + n[1] >= target ? 2u : before + n[0] >= target ? 1u : 0u) << b;
         }
         // (of bf16 logits the lower half follows from the upper one: all ones below zero;
-        // past the end by a rounding: the least)
+        // past an end by a rounding: the least or the largest one)
         t = !t ? unsigned_order(least) : kBf16 && !(t >> 31) ? t | 0xFFFFu : t;
+        t = t < unsigned_order(most) ? t : unsigned_order(most);
         double n = 0.0;
 #pragma unroll
         for (int q = 0; q < kBinEach; ++q) n += order[q] > t ? w[q] : 0.0;

@@ -9,6 +9,7 @@ half: 45 units of 2^-24), all else is double, and both outputs are rounded to fl
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -432,3 +433,43 @@ def test_random_numbers_on_a_border_between_segments(n, repeats, kw, gpu):
         good = (got.ids == behind) | (got.ids == before)
         assert bool(good.all()), (k, int((~good).sum()), got.ids[~good][:5].tolist(), behind[~good][:5].tolist())
         assert bool((got.ids == behind).any())
+
+
+@pytest.mark.parametrize("n", [250, 1500])
+def test_top_p_within_a_rounding_of_a_border(n, gpu):
+    """Rows whose border by top-p lies between 1,500 likely tokens and unlikely ones a gap
+    below, with the row's mass tuned so that p times it is those tokens' own mass up to a few
+    roundings: the support is the likely tokens, or one more."""
+    rng = np.random.default_rng(n)
+    p, k, v = float(np.float32(0.9)), 1500, 6000
+    z = np.full((n, v), -np.inf, np.float32)
+    for row in range(n):
+        head = -rng.random(k).astype(np.float32)
+        head[0] = 0.0
+        mass = math.fsum(np.exp(head.astype(np.float64)))
+        tail = (-2.2 + 0.2 * rng.random(700)).astype(np.float32)
+        left = mass / p * (1 + rng.integers(-8, 9) * 2.0 ** -53) - mass - math.fsum(np.exp(tail.astype(np.float64)))
+        more = []
+        while left > 1e-17 * mass and len(more) < 1500:
+            x = np.float32(min(-2.05, math.log(left)))
+            if math.exp(x) > left:
+                x = np.nextafter(x, np.float32(-np.inf))
+            more.append(x)
+            left -= math.exp(x)
+        assert len(more) < 1500
+        every = np.concatenate([head, tail, np.array(more, np.float32)])
+        z[row, rng.permutation(v)[:every.size]] = every
+    z = torch.from_numpy(z).cuda()
+    u = uniforms(n, 1)
+    got = T.sample_tokens(z, u, top_p=0.9)
+    w = z.double().exp()
+    likely = z >= -1.0
+    next_one = torch.where(likely, -math.inf, z).argmax(1, keepdim=True)
+    good = torch.zeros(n, dtype=torch.bool, device="cuda")
+    for keep in (likely, likely.scatter(1, next_one, True)):
+        run = torch.where(keep, w, 0.0).cumsum(1)
+        at = (run <= u[:, None] * run[:, -1:]).sum(1).int()
+        one = got.ids == at
+        logq = (w.gather(1, at.long()[:, None])[:, 0] / run[:, -1]).log()
+        good |= one & ((got.logq.double() - logq).abs() <= 1e-6)
+    assert bool(good.all()), (int((~good).sum()), got.ids[~good][:5].tolist())
