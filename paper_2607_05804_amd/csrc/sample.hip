@@ -245,8 +245,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
       // are so high that it has none, from 4.9e35, x would have to be -inf itself.)
       const float low = (float)((double)m - 1000.0 / plan.rate);
       if (plan.rate <= 0x1p20 && fabs(shift) <= 1024.0 && low > -INFINITY) {
-        // x = z rate - m rate: the product of the maximum is rounded (1e-13 at most, the
-        // same for the whole segment)
+        // x = z rate - m rate
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q) {
 #pragma unroll
@@ -256,6 +255,10 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan(SampleParams p) {
           }
           x[q].fence();
         }
+        // What the maximum's product lost by its rounding (6e-14 at most) is a factor of the
+        // whole segment: 2^-lost, of which its first two terms leave 1e-27.
+        const double lost = fma((double)m, plan.rate, shift);
+        mass = fma(mass, lost * -kLn264, mass);
       } else {
 #pragma unroll
         for (int q = 0; q < R::kPacks; ++q)

@@ -7,7 +7,10 @@ together.  logq and logp: the kernel's sums of exp(z - M) are float within a seg
 half: 45 units of 2^-24), all else is double, and both outputs are rounded to float once:
 |d| <= 3e-6 + 2^-23 |log|.
 """
+import decimal
 import math
+from decimal import Decimal
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -473,3 +476,28 @@ def test_top_p_within_a_rounding_of_a_border(n, gpu):
         logq = (w.gather(1, at.long()[:, None])[:, 0] / run[:, -1]).log()
         good |= one & ((got.logq.double() - logq).abs() <= 1e-6)
     assert bool(good.all()), (int((~good).sum()), got.ids[~good][:5].tolist())
+
+
+@pytest.mark.parametrize("heat", [1.0, 0.5, 64.0])
+def test_random_numbers_close_to_a_border_between_segments(heat, gpu):
+    """Two tokens, in segments of their own, whose logits over the temperature are so large
+    that their products with the rate are rounded by up to 6e-14: a random number 1e-14 on
+    either side of the border between them, which is computed to 50 digits."""
+    rate = 1.4426950408889634074 / heat
+    lost = lambda m: Fraction(-(m * rate)) + Fraction(m) * Fraction(rate)  # noqa: E731
+    rows, u, want = [], [], []
+    for low in (600, 640, 680, -700):
+        z = [torch.tensor((low + i * 0.013) * heat, dtype=torch.float32).item() for i in range(60)]
+        z.sort(key=lost)
+        for a, b in ((z[0], z[-1]), (z[-1], z[0]), (z[1], z[-2])):
+            with decimal.localcontext() as c:
+                c.prec = 50
+                border = 1 / (1 + ((Decimal(b) - Decimal(a)) / Decimal(heat)).exp())
+            for off, at in ((-1e-14, 1000), (1e-14, 3000)):
+                rows.append((a, b))
+                u.append(float(border + Decimal(off)))
+                want.append(at)
+    logit = torch.full((len(rows), 4096), -math.inf, device="cuda")
+    logit[:, 1000], logit[:, 3000] = torch.tensor(rows, device="cuda").t()
+    got = T.sample_tokens(logit, torch.tensor(u, dtype=torch.float64, device="cuda"), temperature=heat)
+    assert got.ids.tolist() == want
