@@ -538,7 +538,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
   __shared__ float s_sum[kWaves][kSumCols];
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int run = blockIdx.x / p.col_tiles, tile = blockIdx.x % p.col_tiles;
+  const long long task = p.first_join + blockIdx.x;
+  const int run = (int)(task / p.col_tiles), tile = (int)(task % p.col_tiles);
   const int* const keys = p.key_in;
   const long long end = (long long)(run + 1) * p.run;  // of the run, the next one's start
   if (end >= p.n_rows) return;
@@ -689,9 +690,15 @@ hipError_t launch_embed_bwd(const EmbedGradParams& given, hipStream_t s) {
   else embed_sum<false, false><<<grid, kEmbThreads, 0, s>>>(p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (p.n_runs > 1) {
-    const int join = (p.n_runs - 1) * p.col_tiles;
-    if (p.table_bf16) embed_join<true><<<join, kEmbThreads, 0, s>>>(p);
-    else embed_join<false><<<join, kEmbThreads, 0, s>>>(p);
+    // (a workgroup for each of 2^24 runs would be more threads than a launch can hold)
+    const long long joins = (p.n_runs - 1ll) * p.col_tiles;
+    for (p.first_join = 0; p.first_join < joins; p.first_join += kEmbedJoinBlocks) {
+      const long long left = joins - p.first_join;
+      const int grid = (int)(left < kEmbedJoinBlocks ? left : kEmbedJoinBlocks);
+      if (p.table_bf16) embed_join<true><<<grid, kEmbThreads, 0, s>>>(p);
+      else embed_join<false><<<grid, kEmbThreads, 0, s>>>(p);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
   }
   return hipGetLastError();
 }

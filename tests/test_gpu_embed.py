@@ -349,3 +349,20 @@ def test_large_tables_are_zeroed_from_any_start(dtype, v, d, pad, start, n, gpu)
     if pad:
         assert bool((torch.as_strided(whole, (v - 1, pad), (d + pad, 1), start + d) == 7.0).all())
     assert bool((whole[:start] == 7.0).all()) and bool((whole[start + (v - 1) * (d + pad) + d:] == 7.0).all())
+
+
+def test_more_tokens_than_a_launch_has_workgroups_to_join(gpu):
+    """2^30 and some tokens of one column: 2^24 runs of 64, a workgroup of 256 threads for
+    each of which would be more than the 2^32 threads of a launch.  Every table row's tokens
+    go over 256 runs or more, so that all of them are joined; counts are exact in float."""
+    if torch.cuda.mem_get_info()[0] < 120e9:
+        pytest.skip("takes 100 GB")
+    each = 16400  # of a row
+    n = 2 ** 30 + 4 * each
+    v = -(-n // each)
+    ids = torch.arange(n, dtype=torch.int32, device="cuda").div_(each, rounding_mode="floor")
+    g = torch.ones((n, 1), dtype=torch.bfloat16, device="cuda")
+    want = torch.full((v, 1), float(each), device="cuda")
+    want[-1] = n - (v - 1) * each
+    got = T.embed_bwd(g, ids, torch.empty((v, 1), device="cuda"))
+    assert torch.equal(got, want)
