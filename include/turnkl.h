@@ -652,7 +652,8 @@ int turnkl_block_norm_bwd(const void* grad_y, int64_t ld_gy, const void* grad_re
 /* ------------------------------------------------------------------------
  * Rows of an embedding table for tokens, and the table's gradient:
  *   y_i  = s E[t_i],      dE[v] (+)= s sum over the tokens i with t_i = v of g_i.
- * Products and sums are float; y and dE are rounded to nearest even once.
+ * Products are float; up to 64 gradients of a row are added in float, the sums of more of
+ * them in double.  y and dE are rounded to nearest even once.
  * ------------------------------------------------------------------------ */
 
 /* The widest table row, in elements. */
@@ -689,8 +690,8 @@ size_t turnkl_embed_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t wid
  *                overwrites all of it (rows that no token has with zeros); otherwise
  *                the rows that occur are added to, once each, and the others are not
  *                touched.  Elements between width and ld_table are never written.
- * A row's gradients are summed in the order of its tokens in a tree that depends on the
- * ids alone: the same bits from call to call.
+ * A row's gradients are summed in an order that depends on the ids, the mask, n_tokens and
+ * width alone: the same bits from call to call.
  */
 int turnkl_embed_bwd(const void* grad_out, int64_t ld_grad, int grad_dtype, int64_t n_tokens,
                      int64_t width, const int32_t* token_ids, const uint8_t* mask, int64_t vocab,

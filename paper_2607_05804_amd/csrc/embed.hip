@@ -3,14 +3,14 @@
 // Forward: y_i = s E[t_i], one pass.  Bound: HBM, at the rate of a copy (65,536 bf16 rows
 // of 4,096 out of 151,936: 141 us, 5.0 TB/s); 64 rows of 2,048: 4 us, a chain of three loads.
 //
-// Backward: dE[v] = s sum over the tokens i with t_i = v, in the order of i, of g_i.  The
+// Backward: dE[v] = s sum over the tokens i with t_i = v of g_i.  The
 // tokens are sorted by id first (a stable radix sort of (id, token) pairs: in LDS by one
 // workgroup for short batches, else two kernels a digit), so that every table row is one
 // segment of the sorted order and no atomic decides in which order a row is summed.  The
 // order is cut into runs of equal length whatever the segments: a token that fills a tenth
 // of a batch then takes no longer than others.  A wave sums a run for 512 columns; a
 // segment inside one run is written to the table, pieces of segments that cross from run
-// to run go to the workspace, and a second kernel adds them in the order of the runs.
+// to run go to the workspace, and a second kernel adds them, a fixed share a wave.
 //
 // The table's zeros are most of what is written.  Where the batch is small beside a large
 // table all of it is zeroed beside the sort, which leaves the card idle (151,936 x 4,096
@@ -531,11 +531,13 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum(EmbedGradParams p) {
 }
 
 // Adds the pieces of the segment that begins in a run and goes on in the next ones: a
-// workgroup per run and 512 columns, whose waves take the pieces in turn.
+// workgroup per run and 512 columns, whose waves take the pieces in turn.  They are added in
+// 64 bits: a token may have thousands of them (1,024 in sequence a wave in floats: a sum of
+// 32,768 equal numbers off by 255 2^-24).
 template <bool kTab16>
 __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
   constexpr int kWaves = kEmbThreads / kWave;
-  __shared__ float s_sum[kWaves][kSumCols];
+  __shared__ double s_sum[kWaves][kSumCols];
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const long long task = p.first_join + blockIdx.x;
@@ -559,7 +561,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
   const float* const part = p.part + tile * kSumCols + lane * kSumEl;
   SumPlace at[kSumUnits];
   sum_places(tile, lane, p.width, at);
-  float sum[kSumUnits][kSumEl] = {};
+  double sum[kSumUnits][kSumEl] = {};
 #pragma unroll 4
   for (int r = run + wid; r <= last; r += kWaves) {
     const char* const from = reinterpret_cast<const char*>(part + ((long long)r * 2 + (r == run ? 1 : 0)) * p.part_ld);
@@ -577,13 +579,16 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
     for (int j = 0; j < kSumEl; ++j) s_sum[wid][(q * kSumEl + j) * kWave + lane] = sum[q][j];
   __syncthreads();
   if (wid != 0) return;
+  float joined[kSumUnits][kSumEl];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w)
+  for (int q = 0; q < kSumUnits; ++q)
 #pragma unroll
-    for (int q = 0; q < kSumUnits; ++q)
+    for (int j = 0; j < kSumEl; ++j) {
 #pragma unroll
-      for (int j = 0; j < kSumEl; ++j) sum[q][j] += s_sum[w][(q * kSumEl + j) * kWave + lane];
-  write_table<kTab16>(p, id, at, sum);
+      for (int w = 1; w < kWaves; ++w) sum[q][j] += s_sum[w][(q * kSumEl + j) * kWave + lane];
+      joined[q][j] = (float)sum[q][j];
+    }
+  write_table<kTab16>(p, id, at, joined);
 }
 
 }  // namespace

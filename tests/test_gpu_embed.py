@@ -366,3 +366,19 @@ def test_more_tokens_than_a_launch_has_workgroups_to_join(gpu):
     want[-1] = n - (v - 1) * each
     got = T.embed_bwd(g, ids, torch.empty((v, 1), device="cuda"))
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n", [32768, 32009, 70001])
+@pytest.mark.parametrize("bits", [0xBC100, 0x1330FF, 0x51100, 0x7F1020])
+def test_long_sums_of_one_number(n, bits, gpu):
+    """A token that takes a whole batch, with gradients whose sums are rounded the same way
+    at nearly every step (in one sequence a wave of float pieces: off by up to 268 u).  Its n
+    terms are added in runs of 8, or 16 of 70,001, the runs' sums in 64 bits, which are
+    rounded to float once, like the product with the scale: (16 - 1) + 2 u."""
+    x = torch.tensor(0x3F800000 + bits, dtype=torch.int32).view(torch.float32).item()
+    g = torch.full((n, 24), x, device="cuda")
+    ids = torch.full((n,), 3, dtype=torch.int32, device="cuda")
+    got = T.embed_bwd(g, ids, torch.empty((5, 24), device="cuda"))
+    assert not bool(got[:3].any()) and not bool(got[4:].any())
+    err = (got[3].double() - n * x).abs() / (n * x)
+    assert float(err.max()) <= 17 * U, float(err.max()) / U
