@@ -501,3 +501,27 @@ def test_random_numbers_close_to_a_border_between_segments(heat, gpu):
     logit[:, 1000], logit[:, 3000] = torch.tensor(rows, device="cuda").t()
     got = T.sample_tokens(logit, torch.tensor(u, dtype=torch.float64, device="cuda"), temperature=heat)
     assert got.ids.tolist() == want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_log_probabilities_to_their_rounding(dtype, gpu):
+    """log q is computed in 64 bits throughout and rounded once: 2^-24 of itself.  So is
+    log p where the row's mass at temperature 1 is that of all its tokens; otherwise its sum is
+    made of 32-bit exponentials, off by 2^-23 and by 2^-24 for their correction, which are
+    added in 64 bits.  (The logits are multiples of 1/8, so that their differences are exact;
+    2^-40 stands for the 64-bit sums on either side.)"""
+    n, v = 30, 60001
+    z = (torch.randn((n, v), generator=gen(9), device="cuda") * 16).round().clamp(-64, 64) / 8
+    z[:10] = z[:10].clamp(max=0.125)
+    z[:, 77] += 3.0
+    z = z.to(DT[dtype])
+    u = uniforms(n, 9)
+    for kw in FILTERS + [dict(top_k=2000), dict(top_p=0.8, temperature=0.9), dict(min_p=0.2, temperature=2.0)]:
+        got = T.sample_tokens(z, u, **kw)
+        ids, logq, logp = reference(z, u, **kw)
+        assert torch.equal(got.ids, ids), kw
+        exact = 2.0 ** -24 * logq.abs() + 2.0 ** -40
+        assert bool(((got.logq.double() - logq).abs() <= exact).all()), (kw, "logq")
+        plain = not kw or (list(kw) == ["top_p"])
+        bound = 2.0 ** -24 * logp.abs() + 2.0 ** -40 + (0.0 if plain else 3 * 2.0 ** -24)
+        assert bool(((got.logp.double() - logp).abs() <= bound).all()), (kw, "logp")
