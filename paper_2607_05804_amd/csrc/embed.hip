@@ -540,8 +540,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
   __shared__ double s_sum[kWaves][kSumCols];
   const int lane = threadIdx.x & (kWave - 1);
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const long long task = p.first_join + blockIdx.x;
-  const int run = (int)(task / p.col_tiles), tile = (int)(task % p.col_tiles);
+  const int run = p.first_join + blockIdx.x / p.col_tiles, tile = blockIdx.x % p.col_tiles;
   const int* const keys = p.key_in;
   const long long end = (long long)(run + 1) * p.run;  // of the run, the next one's start
   if (end >= p.n_rows) return;
@@ -579,15 +578,18 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join(EmbedGradParams p) {
     for (int j = 0; j < kSumEl; ++j) s_sum[wid][(q * kSumEl + j) * kWave + lane] = sum[q][j];
   __syncthreads();
   if (wid != 0) return;
+  // (one wave's at a time: with all of them in registers the kernel takes 14 us for 11)
+#pragma unroll 1
+  for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+    for (int q = 0; q < kSumUnits; ++q)
+#pragma unroll
+      for (int j = 0; j < kSumEl; ++j) sum[q][j] += s_sum[w][(q * kSumEl + j) * kWave + lane];
   float joined[kSumUnits][kSumEl];
 #pragma unroll
   for (int q = 0; q < kSumUnits; ++q)
 #pragma unroll
-    for (int j = 0; j < kSumEl; ++j) {
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum[q][j] += s_sum[w][(q * kSumEl + j) * kWave + lane];
-      joined[q][j] = (float)sum[q][j];
-    }
+    for (int j = 0; j < kSumEl; ++j) joined[q][j] = (float)sum[q][j];
   write_table<kTab16>(p, id, at, joined);
 }
 
@@ -696,10 +698,10 @@ hipError_t launch_embed_bwd(const EmbedGradParams& given, hipStream_t s) {
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (p.n_runs > 1) {
     // (a workgroup for each of 2^24 runs would be more threads than a launch can hold)
-    const long long joins = (p.n_runs - 1ll) * p.col_tiles;
-    for (p.first_join = 0; p.first_join < joins; p.first_join += kEmbedJoinBlocks) {
-      const long long left = joins - p.first_join;
-      const int grid = (int)(left < kEmbedJoinBlocks ? left : kEmbedJoinBlocks);
+    const int most = kEmbedJoinBlocks / p.col_tiles;
+    for (p.first_join = 0; p.first_join < p.n_runs - 1; p.first_join += most) {
+      const int left = p.n_runs - 1 - p.first_join;
+      const int grid = (left < most ? left : most) * p.col_tiles;
       if (p.table_bf16) embed_join<true><<<grid, kEmbThreads, 0, s>>>(p);
       else embed_join<false><<<grid, kEmbThreads, 0, s>>>(p);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

@@ -488,7 +488,7 @@ constexpr int kEmbedWaves = 4096;      // that sum at once, at least where there
 constexpr int kEmbedFillRows = 1024;   // table rows that a workgroup looks after, at most
 constexpr int kEmbedFillElems = 1 << 15;  // and elements
 constexpr long long kEmbedFillBlocks = 1 << 22;  // of a launch, which holds fewer than 2^32 threads
-constexpr long long kEmbedJoinBlocks = 1 << 23;  // of a launch, as above
+constexpr int kEmbedJoinBlocks = 1 << 23;  // of a launch, as above
 constexpr double kEmbedWholeFill = 64.0 * (1 << 20);  // bytes of a table zeroed whole, at least
 constexpr double kEmbedCachedFill = 192.0 * (1 << 20);  // and through the caches, at most
 
@@ -532,7 +532,7 @@ struct EmbedGradParams {
   int turn;        // set at launch, like the next two
   int sum_blocks;  // workgroups that sum, before those that zero
   int fill_rows;   // table rows of one of those
-  long long first_join;  // run and tile that a launch of the join begins with
+  int first_join;  // run that a launch of the join begins with
   long long fill_from;  // 16-byte packs that a launch of the sort zeroes
   long long fill_to;
   long long fill_elems;   // of a table without padding
