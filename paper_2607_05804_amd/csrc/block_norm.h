@@ -15,9 +15,10 @@
 // in registers; a second kernel adds the workgroups' sums in their order.
 //
 // Bound: HBM.  65,536 bf16 rows of 4,096 with both norms and a vector's gate, forward: 428
-// us, 5.0 TB/s over two streams in and two out, as a copy; backward 32,768 of them: 363 us,
-// 4.4 TB/s over five streams, one workgroup of 162 VGPRs a CU and more of eight waves not
-// fitting (at 128 VGPRs it spills: 1,033).  64 rows of 2,048: 4 us, two chains of sums.
+// us, 5.0 TB/s over two streams in and two out, as a copy; backward 32,768 of them: 366 us,
+// 4.4 TB/s over four streams in and two out, one workgroup of 162 VGPRs a CU and more of
+// eight waves not fitting (at 128 VGPRs it spills: 1,033).  64 rows of 2,048: 4 us, two
+// chains of sums.
 #pragma once
 
 #include "units.h"
@@ -272,7 +273,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_rows(BlockNormParams p) {
 }
 
 // The widest rows, forward: a workgroup a row, which is read from the caches again, and h'
-// in LDS.
+// in LDS.  2^27 bf16 elements with both norms and a vector's gate, in rows of 12,288: 366 us
+// (of 8,192, held in registers, 196).
 constexpr int kWideThreads = 512;
 template <bool kF16, bool kR16>
 __global__ __launch_bounds__(kWideThreads) void block_norm_wide(BlockNormParams p) {
@@ -629,6 +631,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_bwd_rows(BlockNormParams 
 // Backward of the widest rows: a workgroup a row, which is read again for each of its sums
 // (from the caches, then), and the columns' sums in the workspace, a row of the workgroup's
 // own whose elements are always the same thread's.
+//
+// Bound: the columns' sums, which every row reads and writes, and the waits after each
+// unit's stores: 2^27 bf16 elements with both norms and a vector's gate, in rows of 5,120
+// 2,558 us, of 8,192 1,930, of 16,384 1,919 (of 4,096, held in registers, 366).
 template <bool kF16, bool kR16>
 __global__ __launch_bounds__(kWideThreads) void block_norm_bwd_wide(BlockNormParams p) {
   constexpr int kEl = unit_elements(kF16, kR16);

@@ -37,7 +37,8 @@ __global__ __launch_bounds__(kJoinThreads) void block_norm_join(BlockNormParams 
 // How rows are laid out over the threads: rows of up to 64 units a part of a wave, wider
 // ones a workgroup with one unit a thread while that takes few waves, then two, then four.
 // Rows past 8,192 elements, and backward past 4,096 where the branch is normalised, would
-// not fit the registers: they are not held (units 0).
+// not fit the registers (backward with both norms, 8 bf16 elements a thread take 162 of the
+// 256 that two waves a SIMD leave each): they are not held (units 0).
 //
 // Measured with 4,096 bf16 columns, both norms and a vector's gate.  Forward, 512 units:
 // two a thread 437 us (12 waves a CU; 8: 440, 16: 486), one a thread 449 (456 with 16

@@ -15,7 +15,7 @@
 // The table's zeros are most of what is written.  Where the batch is small beside a large
 // table all of it is zeroed beside the sort, which leaves the card idle (151,936 x 4,096
 // in fp32: 362 to 395 us, 6.3 to 6.9 TB/s with the sort in it; the sums then 189 us at the
-// rate of a copy, the join 11); else further workgroups of the summing kernel zero the rows
+// rate of a copy, the join 11 to 12); else further workgroups of the summing kernel zero the rows
 // that do not occur in the sorted order.  Bound: HBM, mostly those writes; of a small
 // table three dependent kernels (1,500 tokens: 10, 10 and 4 us).
 
@@ -641,8 +641,10 @@ hipError_t launch_embed_bwd(const EmbedGradParams& given, hipStream_t s) {
   // A table is zeroed whole, beside the sort, where the tokens touch little of it and its
   // zeros are worth hiding (whole against only the absent rows: 32,000 x 2,048 fp32, 1,500
   // tokens, 57 against 63 us; 32,000 x 1,024 bf16, 4,000 tokens, 41 against 37, 15,000 of
-  // 1,000 columns 49 against 45, where the sort's launches get in each other's way); else
-  // where it has no token, beside the sums.  Past 192 MB, which the last cache holds
+  // 1,000 columns 49 against 45, where the sort's launches get in each other's way; with the
+  // sort of one launch, 1 token of 45,386 x 544 bf16, 13.6 against 16.8, 131 of 1,371 x
+  // 10,730 18.7 against 21.6, which this border by bytes gives away); else where it has no
+  // token, beside the sums.  Past 192 MB, which the last cache holds
   // beside the gradient, its zeros go past the caches.
   const double bytes = (double)p.vocab * p.width * es;
   p.fill_stream = bytes > kEmbedCachedFill;
