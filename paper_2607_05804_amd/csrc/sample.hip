@@ -1101,10 +1101,11 @@ __global__ __launch_bounds__(kPickThreads, kWide ? 2 : 4) void sample_pick(Sampl
     }
     unsigned least = bound << 16;
     if (least <= kNothing) least = kNothing + 1u;
-    // by min-p alone: what lies clearly below its border is not needed
+    // By min-p alone: what lies clearly below its border is not needed.  (Weights are rounded:
+    // by 4e-16 at most, which at high temperatures is a wide range of logits.)
     if (plan.p >= 1.0f && plan.min_p > 0.0f) {
       const double z = m + log2((double)plan.min_p) / plan.rate;
-      const float low = (float)(z - 1e-5 * (fabs(z) + fabs((double)m)) - 1e-30);
+      const float low = (float)(z - 1e-5 * (fabs(z) + fabs((double)m)) - 1e-15 / plan.rate - 1e-30);
       if (order_of(low) > least) least = order_of(low);
     }
     // units that reach it

@@ -525,3 +525,15 @@ def test_log_probabilities_to_their_rounding(dtype, gpu):
         plain = not kw or (list(kw) == ["top_p"])
         bound = 2.0 ** -24 * logp.abs() + 2.0 ** -40 + (0.0 if plain else 3 * 2.0 ** -24)
         assert bool(((got.logp.double() - logp).abs() <= bound).all()), (kw, "logp")
+
+
+@pytest.mark.parametrize("n", [6, 300])
+def test_min_p_where_weights_are_equal_in_64_bits(n, gpu):
+    """At these temperatures every weight is 1 in double, and min-p 1 keeps them all, however
+    many they are and with top-k as without."""
+    for v in (100, 1000, 5000, 60000):
+        z = logits(n, v, "f32", v)
+        z[:, ::7] = -math.inf
+        for heat in (1e20, 1e36):
+            for kw in (dict(), dict(top_k=60), dict(top_k=2000)):
+                check(z, uniforms(n, 1), temperature=heat, min_p=1.0, **kw)
